@@ -316,6 +316,163 @@ gba_status gba_set_eager_dense(gba_handle* h, int32_t on);
  */
 gba_status gba_join(gba_handle* h);
 
+/* ---- a worker's operators around pull and push --------------------------
+ *
+ * What a worker of Alg. 1 does next to the server's half of a step: it looks up
+ * the embeddings of its batch (gba_embed, gba_embed_table), normalises them
+ * (gba_layer_norm), and on the way back turns the gradient of every token into
+ * the rows of one message (gba_embed_grad) or of a whole table
+ * (gba_embed_grad_dense), forms layer norm's gradients (gba_layer_norm_grad) and
+ * clips the message by the norm of all its gradients (gba_clip_grads) before
+ * gba_push.
+ *
+ * Sums, statistics and norms are held in float32 or wider whatever the type of
+ * the data; a result is rounded to its type once.  Every sum is formed in an
+ * order fixed by the sizes: the same call gives the same bits.
+ *
+ * All work of a worker handle is issued on its stream, in call order, and uses
+ * the handle's workspace, which grows on demand (a call that grows it waits for
+ * the stream; the calls that follow at that size or below allocate nothing and
+ * may be captured into a CUDA graph).  Pointers are device memory.  A call that
+ * returns an error has enqueued nothing that writes to its outputs, except for
+ * GBA_E_CUDA.  What only a kernel can see (an id out of range, a bounded wait
+ * that gave up) is kept until gba_worker_sync reports it.
+ */
+typedef struct gba_worker gba_worker;
+
+/* Types of the data: float32, bfloat16, IEEE half. */
+typedef enum { GBA_F32 = 0, GBA_BF16 = 1, GBA_F16 = 2 } gba_dtype;
+
+/* No padding id (the value that HASH tables reserve, so no id has it). */
+#define GBA_NO_PAD INT64_MIN
+
+/* A row-major matrix in device memory: element (i, j) is data[i * stride + j]. */
+typedef struct {
+  void* data;      /* aligned to its type (NULL only if rows is 0) */
+  int64_t rows;    /* >= 0 */
+  int64_t stride;  /* elements between rows, >= cols */
+  int32_t cols;    /* 1 .. 2^20 */
+  int32_t type;    /* gba_dtype */
+} gba_matrix;
+
+/* gba_worker_create - a worker handle on the current device.  cuda_stream: the
+ * stream of all its work (NULL: the legacy default stream).
+ * gba_worker_sync - wait for the stream, then report what the kernels latched since
+ * the last gba_worker_sync: GBA_E_ID_RANGE (an id out of range) or
+ * GBA_E_DEVICE_TIMEOUT; the handle can be used on.
+ * gba_worker_last_error - text of the handle's last failure ("" if none).
+ * gba_worker_destroy - wait for the stream and free the workspace (NULL: no-op). */
+gba_status gba_worker_create(void* cuda_stream, gba_worker** out);
+gba_status gba_worker_sync(gba_worker* w);
+const char* gba_worker_last_error(gba_worker* w);
+void gba_worker_destroy(gba_worker* w);
+
+/*
+ * gba_embed - scaled embedding rows: out[i] = scale * weights[row(ids[i])].
+ *
+ * weights    the table, of any type; its rows are the rows of id_mode DIRECT or
+ *            MODULO (a worker's own weights, or a copy).
+ * ids        n device int64.  pad_id: positions holding it become rows of zeros
+ *            and read nothing (GBA_NO_PAD: none).
+ * out        n x weights->cols, of any type; must not overlap the weights.
+ * A DIRECT id outside [0, rows) gets a row of zeros and latches GBA_E_ID_RANGE.
+ */
+gba_status gba_embed(gba_worker* w, const gba_matrix* weights, int32_t id_mode,
+                     const int64_t* ids, int64_t n, float scale, int64_t pad_id,
+                     const gba_matrix* out);
+
+/*
+ * gba_embed_table - the same from table t of a server handle, in the table's
+ * id_mode (a HASH id never seen gives its initial row, as with gba_pull; the
+ * reserved id INT64_MIN counts as out of range).  Ordered, on the device, after
+ * every step of h enqueued so far and before every later one, whatever the two
+ * handles' streams.  Both handles belong to one device and are used by the
+ * calling thread.
+ */
+gba_status gba_embed_table(gba_worker* w, gba_handle* h, int32_t t, const int64_t* ids,
+                           int64_t n, float scale, int64_t pad_id, const gba_matrix* out);
+
+/*
+ * gba_embed_grad - the gradient of gba_embed by sorted tokens, as the sparse part
+ * of one message: each row that occurs, once, with the sum of its tokens'
+ * gradients.  The server counts messages that contain a row, so it takes the same
+ * step (up to rounding) as from the n single rows, from fewer of them.
+ *
+ * grad       n x cols, the gradient of gba_embed's output.  Rows at padding
+ *            positions are not read.
+ * rows, id_mode  of the table: DIRECT or MODULO, rows < 2^32 - 2.
+ * ids_out    n device int64: the rows that occur, ascending, then the last of
+ *            them repeated up to n.
+ * rows_out   n x cols device float32, 16-byte aligned, contiguous: scale * (sum of
+ *            the row's gradients), then rows of zeros up to n.
+ * n_out      device int64: how many occur.
+ * So the first *n_out entries are a message, and all n are one that changes the
+ * table in the same way, for callers that do not wait for the count.  With
+ * *n_out = 0 (all padding) ids_out holds -1 and there is nothing to push.  A
+ * DIRECT id outside [0, rows) that is not padding latches GBA_E_ID_RANGE and the
+ * call gives *n_out = 0.  n < 2^30.
+ */
+gba_status gba_embed_grad(gba_worker* w, const int64_t* ids, int64_t n, const gba_matrix* grad,
+                          int64_t rows, int32_t id_mode, float scale, int64_t pad_id,
+                          int64_t* ids_out, float* rows_out, int64_t* n_out);
+
+/*
+ * gba_embed_grad_dense - the same gradient as an array of all rows of the table.
+ * out        rows x cols, GBA_F32.  accumulate 0: overwritten (rows that do not
+ *            occur become zero); 1: the sums are added to what it holds, and
+ *            rows that do not occur are not touched.
+ * After an id out of range (latched) no sums are added.
+ */
+gba_status gba_embed_grad_dense(gba_worker* w, const int64_t* ids, int64_t n,
+                                const gba_matrix* grad, int32_t id_mode, float scale,
+                                int64_t pad_id, const gba_matrix* out, int32_t accumulate);
+
+/* One tensor of a list of gradients: n contiguous elements at grad.  out (of
+ * gba_clip_grads) receives the clipped gradient: grad itself, with the same type
+ * (in place), or memory that does not overlap it, in any type. */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;        /* 0 .. 2^40 */
+  int32_t type;     /* gba_dtype of grad */
+  int32_t out_type; /* gba_dtype of out */
+} gba_grad_part;
+
+/*
+ * gba_grad_norm - the 2-norm of all elements of n_parts (up to 2^20) tensors together,
+ * as one device float32 (out is not looked at).  Squares neither overflow nor vanish: the
+ * norm is right wherever it is a float32.
+ * gba_clip_grads - the norm N, and out = c * grad with c = min(1, max_norm / (N + 1e-6))
+ * for every part (norm may be NULL).  With a norm that is infinite c is 0, with a NaN it
+ * is NaN: the gradients of such a message are lost, and *norm says so.  max_norm >= 0.
+ * The description may be reused or freed when the call returns.  No part may overlap
+ * another part's out.
+ */
+gba_status gba_grad_norm(gba_worker* w, const gba_grad_part* parts, int32_t n_parts, float* norm);
+gba_status gba_clip_grads(gba_worker* w, const gba_grad_part* parts, int32_t n_parts,
+                          float max_norm, float* norm);
+
+/*
+ * gba_layer_norm - y = (x - mean) * rstd * gamma + beta for every row of x, with
+ * mean and rstd = 1 / sqrt(variance + eps) over the row's columns.
+ * gamma, beta  cols values of param_type (NULL: 1 and 0).
+ * y            x->rows x x->cols of x's type; x itself, or no overlap.
+ * mean, rstd   x->rows device float32, for the gradient (NULL: not kept).
+ */
+gba_status gba_layer_norm(gba_worker* w, const gba_matrix* x, const void* gamma,
+                          const void* beta, int32_t param_type, float eps, const gba_matrix* y,
+                          float* mean, float* rstd);
+
+/*
+ * gba_layer_norm_grad - from the gradient dy of y: dx, and dgamma and dbeta (cols
+ * device float32 each, overwritten; either may be NULL) summed over all rows.
+ * x, dy and dx are of one type and shape; dx may be dy.
+ */
+gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_matrix* x,
+                               const void* gamma, int32_t param_type, const float* mean,
+                               const float* rstd, const gba_matrix* dx, float* dgamma,
+                               float* dbeta);
+
 /* ---- instrumentation and test entry points ----------------------------- */
 
 /* gba_set_timing - when on, every kernel launch is bracketed by CUDA events on

@@ -29,6 +29,8 @@ STATUS_NAMES = {0: "GBA_OK", -1: "GBA_E_ARG", -2: "GBA_E_ID_RANGE", -3: "GBA_E_O
                 -7: "GBA_E_FULL"}
 ADAGRAD, ADAM = 0, 1
 DIRECT, MODULO, HASH = 0, 1, 2
+F32, BF16, F16 = 0, 1, 2
+NO_PAD = -2**63
 INT32_MAX = 2**31 - 1
 KERNEL_NAMES = ["weights", "sort_hist", "sort_pass", "seg_scan", "row_long", "row_apply",
                 "dense", "init", "other"]
@@ -76,7 +78,18 @@ class gba_kernel_times_t(ctypes.Structure):
                 ("ms", ctypes.c_double * len(KERNEL_NAMES))]
 
 
+class gba_matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("cols", ctypes.c_int32), ("type", ctypes.c_int32)]
+
+
+class gba_grad_part(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
 _P = ctypes.c_void_p
+_M = ctypes.POINTER(gba_matrix)
 _SIGNATURES = {
     "gba_create": (ctypes.c_int, [ctypes.POINTER(gba_table_desc), ctypes.c_int32, ctypes.c_int64,
                                   ctypes.POINTER(gba_opt_desc), ctypes.c_int64, ctypes.c_int32,
@@ -122,6 +135,23 @@ _SIGNATURES = {
     "gba_device_binary_version": (ctypes.c_int32, []),
     "gba_sort_ids_static": (ctypes.c_int, [_P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                            _P, _P, _P]),
+    "gba_worker_create": (ctypes.c_int, [_P, ctypes.POINTER(_P)]),
+    "gba_worker_sync": (ctypes.c_int, [_P]),
+    "gba_worker_last_error": (ctypes.c_char_p, [_P]),
+    "gba_worker_destroy": (None, [_P]),
+    "gba_embed": (ctypes.c_int, [_P, _M, ctypes.c_int32, _P, ctypes.c_int64, ctypes.c_float,
+                                 ctypes.c_int64, _M]),
+    "gba_embed_table": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, ctypes.c_int64, ctypes.c_float,
+                                       ctypes.c_int64, _M]),
+    "gba_embed_grad": (ctypes.c_int, [_P, _P, ctypes.c_int64, _M, ctypes.c_int64, ctypes.c_int32,
+                                      ctypes.c_float, ctypes.c_int64, _P, _P, _P]),
+    "gba_embed_grad_dense": (ctypes.c_int, [_P, _P, ctypes.c_int64, _M, ctypes.c_int32,
+                                            ctypes.c_float, ctypes.c_int64, _M, ctypes.c_int32]),
+    "gba_grad_norm": (ctypes.c_int, [_P, ctypes.POINTER(gba_grad_part), ctypes.c_int32, _P]),
+    "gba_clip_grads": (ctypes.c_int, [_P, ctypes.POINTER(gba_grad_part), ctypes.c_int32,
+                                      ctypes.c_float, _P]),
+    "gba_layer_norm": (ctypes.c_int, [_P, _M, _P, _P, ctypes.c_int32, ctypes.c_float, _M, _P, _P]),
+    "gba_layer_norm_grad": (ctypes.c_int, [_P, _M, _M, _P, ctypes.c_int32, _P, _P, _M, _P, _P]),
 }
 
 _lib = None
@@ -483,3 +513,231 @@ class TokenList:
             self.close()
         except Exception:
             pass
+
+
+# ---- a worker's operators -----------------------------------------------------------------
+
+def _refuse(why):
+    raise GBAError(GBA_E_ARG, why)
+
+
+def _type_of(t):
+    import torch
+    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if t.dtype not in types:
+        _refuse(f"tensors are float32, bfloat16 or float16, not {t.dtype}")
+    return types[t.dtype]
+
+
+def _on_gpu(*tensors):
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            _refuse("a tensor is not on the GPU")
+
+
+def _matrix(t):
+    """t as a gba_matrix: two dimensions, rows of consecutive elements."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        _refuse("a matrix has two dimensions, and rows of consecutive elements")
+    rows, cols = t.shape
+    stride = t.stride(0) if rows > 1 else max(cols, 1)
+    return gba_matrix(t.data_ptr() if rows else None, rows, stride, cols, _type_of(t))
+
+
+def _rows_of(t):
+    """An input of any leading shape as a matrix [n, d]; copied if its rows are not apart or
+    their elements not consecutive (an expanded tensor, a transposed one)."""
+    if t.dim() != 2:
+        t = t.reshape(t.numel() // max(1, t.shape[-1]), t.shape[-1])
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        t = t.contiguous()
+    return t
+
+
+class GradParts:
+    """A list of gradient tensors (and of what receives them clipped), as the library takes
+    it.  It refers to the tensors' memory and keeps them alive."""
+
+    def __init__(self, grads, out=None):
+        grads = list(grads)
+        out = grads if out is None else list(out)
+        if len(out) != len(grads):
+            _refuse("as many outputs as gradients")
+        for t in (*grads, *out):
+            _on_gpu(t)
+            if not t.is_contiguous():
+                _refuse("gradients and their outputs are contiguous")
+        for g, o in zip(grads, out):
+            if g.numel() != o.numel():
+                _refuse("an output has its gradient's size")
+        self.tensors = (grads, out)
+        self.n = len(grads)
+        self.array = (gba_grad_part * max(1, self.n))(*[
+            gba_grad_part(g.data_ptr(), o.data_ptr(), g.numel(), _type_of(g), _type_of(o))
+            for g, o in zip(grads, out)])
+
+
+def grad_parts(grads, out=None):
+    """The list of a program's gradient tensors, made once for tensors that stay.  out: what
+    clipping writes to (default: in place)."""
+    return GradParts(grads, out)
+
+
+class Worker:
+    """A worker's operators on the current CUDA device: lookups and their gradient, norm and
+    clipping, layer norm (see include/gba.h).
+
+    Work is issued on `stream` (default: the current one).  A call made while another stream
+    is current orders the two both ways, so tensors of the current stream can be passed and
+    results used there."""
+
+    def __init__(self, stream=None):
+        import torch
+        self.torch = torch
+        self.L = load()
+        self.h = None
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        h = _P()
+        check(self.L.gba_worker_create(self.stream.cuda_stream, ctypes.byref(h)), what="gba_worker_create")
+        self.h = h
+
+    def close(self):
+        if self.h:
+            self.L.gba_worker_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _call(self, name, *args):
+        now = self.torch.cuda.current_stream()
+        apart = now != self.stream
+        if apart:
+            self.stream.wait_stream(now)
+        status = getattr(self.L, name)(self.h, *args)
+        if apart:
+            now.wait_stream(self.stream)
+        self._check(status, name)
+
+    def _check(self, status, name):
+        if status < 0:
+            raise GBAError(status, name + " " + (self.L.gba_worker_last_error(self.h) or b"").decode())
+
+    def sync(self):
+        """Wait for the worker's stream; raises what its kernels reported since the last time."""
+        self._check(self.L.gba_worker_sync(self.h), "gba_worker_sync")
+
+    def _ids(self, ids):
+        if ids.dtype != self.torch.int64:
+            _refuse("ids are int64")
+        _on_gpu(ids)
+        return ids.contiguous()
+
+    def _embed_out(self, ids, d, dtype, out):
+        if out is None:
+            out = self.torch.empty(*ids.shape, d, dtype=dtype, device=ids.device)
+        _on_gpu(out)
+        flat = out if out.dim() == 2 else out.view(ids.numel(), d)
+        return out, _matrix(flat)
+
+    def embed(self, weights, ids, scale=1.0, pad_id=None, dtype=None, id_mode=DIRECT, out=None):
+        """scale * weights[ids] in dtype (default: the weights'); padding gives zeros."""
+        ids = self._ids(ids)
+        _on_gpu(weights)
+        out, om = self._embed_out(ids, weights.shape[-1], dtype or weights.dtype, out)
+        self._call("gba_embed", _matrix(weights), id_mode, ids.data_ptr(), ids.numel(), scale,
+                   NO_PAD if pad_id is None else pad_id, om)
+        return out
+
+    def embed_table(self, server, t, ids, scale=1.0, pad_id=None, dtype=None, out=None):
+        """The same from table t of a server (a GBA), as of every step applied so far."""
+        if not 0 <= t < len(server.dims):
+            _refuse("no such table")
+        ids = self._ids(ids)
+        out, om = self._embed_out(ids, server.dims[t], dtype or self.torch.float32, out)
+        self._call("gba_embed_table", server.h, t, ids.data_ptr(), ids.numel(), scale,
+                   NO_PAD if pad_id is None else pad_id, om)
+        return out
+
+    def embed_grad(self, ids, grad, rows, scale=1.0, pad_id=None, id_mode=DIRECT):
+        """The lookup's gradient as one message's ids and rows: (ids [n], rows [n, d] float32,
+        count).  The first `count` (a device int64) entries are the distinct rows in ascending
+        order; those after repeat the last one's id with zeros."""
+        torch = self.torch
+        ids, grad = self._ids(ids), _rows_of(grad)
+        _on_gpu(grad)
+        n, d = ids.numel(), grad.shape[1]
+        ids_out = torch.empty(n, dtype=torch.int64, device=ids.device)
+        rows_out = torch.empty(n, d, dtype=torch.float32, device=ids.device)
+        count = torch.empty((), dtype=torch.int64, device=ids.device)
+        self._call("gba_embed_grad", ids.data_ptr(), n, _matrix(grad), rows, id_mode, scale,
+                   NO_PAD if pad_id is None else pad_id, ids_out.data_ptr(), rows_out.data_ptr(),
+                   count.data_ptr())
+        return ids_out, rows_out, count
+
+    def embed_grad_dense(self, ids, grad, out, scale=1.0, pad_id=None, id_mode=DIRECT, accumulate=False):
+        """The lookup's gradient over all rows of the table, into (or added to) out."""
+        ids, grad = self._ids(ids), _rows_of(grad)
+        _on_gpu(grad, out)
+        self._call("gba_embed_grad_dense", ids.data_ptr(), ids.numel(), _matrix(grad), id_mode, scale,
+                   NO_PAD if pad_id is None else pad_id, _matrix(out), int(accumulate))
+        return out
+
+    def grad_norm(self, grads):
+        """The 2-norm of all the tensors together (a list, or grad_parts of it), on the device."""
+        p = grads if isinstance(grads, GradParts) else GradParts(grads)
+        norm = self.torch.empty((), dtype=self.torch.float32, device="cuda")
+        self._call("gba_grad_norm", p.array, p.n, norm.data_ptr())
+        return norm
+
+    def clip_grads(self, grads, max_norm):
+        """Scales the tensors (a list, or grad_parts of it) by min(1, max_norm / (norm + 1e-6)),
+        in place or into the parts' outputs; returns the norm."""
+        p = grads if isinstance(grads, GradParts) else GradParts(grads)
+        norm = self.torch.empty((), dtype=self.torch.float32, device="cuda")
+        self._call("gba_clip_grads", p.array, p.n, max_norm, norm.data_ptr())
+        return norm
+
+    def _params(self, d, *params):
+        types = {_type_of(p) for p in params if p is not None}
+        if len(types) > 1:
+            _refuse("the parameters of a layer norm have one type")
+        _on_gpu(*params)
+        for p in params:
+            if p is not None and (p.numel() != d or not p.is_contiguous()):
+                _refuse("a parameter has a value per column")
+        return [None if p is None else p.data_ptr() for p in params], types.pop() if types else F32
+
+    def layer_norm(self, x, gamma=None, beta=None, eps=1e-5):
+        """(y, mean, rstd) of the rows of x (its last dimension)."""
+        torch = self.torch
+        _on_gpu(x)
+        rows = _rows_of(x)
+        n, d = rows.shape
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        mean = torch.empty(n, dtype=torch.float32, device=x.device)
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+        (pg, pb), ptype = self._params(d, gamma, beta)
+        self._call("gba_layer_norm", _matrix(rows), pg, pb, ptype, eps, _matrix(y.view(n, d)),
+                   mean.data_ptr(), rstd.data_ptr())
+        return y, mean, rstd
+
+    def layer_norm_grad(self, dy, x, gamma, mean, rstd):
+        """(dx, dgamma, dbeta) from the gradient of layer_norm's y and its mean and rstd."""
+        torch = self.torch
+        _on_gpu(dy, x, mean, rstd)
+        xr, dr = _rows_of(x), _rows_of(dy)
+        n, d = xr.shape
+        if mean.numel() != n or rstd.numel() != n or {mean.dtype, rstd.dtype} != {torch.float32}:
+            _refuse("mean and rstd are float32, one for each row")
+        mean, rstd = mean.contiguous(), rstd.contiguous()
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dgamma = torch.empty(d, dtype=torch.float32, device=x.device)
+        dbeta = torch.empty(d, dtype=torch.float32, device=x.device)
+        (pg,), ptype = self._params(d, gamma)
+        self._call("gba_layer_norm_grad", _matrix(dr), _matrix(xr), pg, ptype, mean.data_ptr(),
+                   rstd.data_ptr(), _matrix(dx.view(n, d)), dgamma.data_ptr(), dbeta.data_ptr())
+        return dx, dgamma, dbeta

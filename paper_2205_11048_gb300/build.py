@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgba.so")
 SOURCES = ["gba_host.cu", "gba_sort.cu", "gba_rows.cu", "gba_dense.cu", "gba_misc.cu",
-           "gba_noalloc.cu", "gba_pull.cu", "gba_push.cu", "gba_tokens.cu"]
+           "gba_noalloc.cu", "gba_pull.cu", "gba_push.cu", "gba_tokens.cu",
+           "gba_worker.cu", "gba_embed.cu", "gba_norm.cu", "gba_layernorm.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include")]
 
@@ -32,7 +33,8 @@ def nvcc() -> str:
 def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
-    deps = [src, os.path.join(CSRC, "gba_internal.cuh"), os.path.join(ROOT, "include", "gba.h")]
+    deps = [src, os.path.join(CSRC, "gba_internal.cuh"), os.path.join(CSRC, "gba_worker.cuh"),
+            os.path.join(ROOT, "include", "gba.h")]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps)
 
 

@@ -1,0 +1,665 @@
+// Scaled embedding lookup, and its gradient by sorted tokens.
+//
+// Lookup: out_i = s * W[row(id_i)], a gather like k_pull_rows with a scale, types and
+// strides.  Bound by HBM bandwidth: the rows that occur are read (repeated ones from L2)
+// and n rows written.
+//
+// Gradient: G[r] = s * sum over the positions i with row(id_i) = r of g_i.  The rows of the
+// ids are sorted with their positions as payload (the step's onesweep passes; stable, so
+// a row's positions stay ascending and its sum has one order), and then each gradient row
+// is read once, where it lies:
+//  - items: a run of equal rows is cut at the sorted positions p = 0 mod CUT whose row
+//    stood at p - CUT too, so runs shorter than CUT stay whole and no item is longer than
+//    2 CUT - 1 positions;
+//  - sums: one lane group per item and column slab adds the item's gradient rows; a run of
+//    one item goes straight to the output, the others leave float32 sums of their items
+//    (in slots that follow from the cut's position: 2 p / CUT for the item before the first
+//    cut p, one more for the item that starts at p);
+//  - merge: one block per cut run and slab adds the items' sums in their order.
+#include <algorithm>
+
+#include "gba_worker.cuh"
+
+namespace gba {
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr uint32_t FULL = 0xffffffffu;
+constexpr int CUT = 64;
+constexpr int ITEM_TILE = 2048;  // sorted positions per tile of the item scan
+constexpr int MAX_RADIX = 512;   // of a sort pass
+
+__device__ __forceinline__ unsigned long long ld_relaxed_u64(const unsigned long long* p) {
+  unsigned long long v;
+  asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_relaxed_u64(unsigned long long* p, unsigned long long v) {
+  asm volatile("st.relaxed.gpu.global.u64 [%0], %1;" ::"l"(p), "l"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t lanemask_lt() {
+  uint32_t m;
+  asm("mov.u32 %0, %%lanemask_lt;" : "=r"(m));
+  return m;
+}
+
+// ---- lookup -----------------------------------------------------------------------
+
+// A lane group of 1 << lg lanes per token and slab of K * V columns a lane.
+template <typename TI, typename TO, int V, int K>
+__global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
+  follow();
+  const int L = 1 << lg;
+  const int l = threadIdx.x & (L - 1);
+  const int64_t groups = (int64_t)gridDim.x * (THREADS >> lg);
+  const int64_t g0 = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> lg;
+  const int64_t c0 = ((int64_t)blockIdx.y * K * L + l) * V;
+  for (int64_t i = g0; i < a.n; i += groups) {
+    const int64_t id = a.ids[i];
+    bool zero = id == a.pad_id && a.pad_id != GBA_NO_PAD;
+    bool fresh = false;  // HASH: an id never seen has its initial values
+    uint64_t row = 0;
+    if (!zero) {
+      bool bad = false;
+      if (a.id_mode == GBA_ID_DIRECT) {
+        bad = id < 0 || id >= a.V;
+        row = (uint64_t)id;
+      } else if (a.id_mode == GBA_ID_MODULO) {
+        row = mod_u64((uint64_t)id, (uint64_t)a.V, a.mod_magic);
+      } else {
+        bad = (unsigned long long)id == HASH_EMPTY;
+        if (!bad) {
+          row = hash_find(*a.hinfo, id);
+          fresh = row > a.hinfo->mask;
+        }
+      }
+      if (bad) {
+        if (l == 0 && blockIdx.y == 0) raise_error(a.err, ERR_ID_RANGE);
+        zero = true;
+      }
+    }
+    const TI* src = static_cast<const TI*>(a.w) + row * (uint64_t)a.w_stride;
+    TO* dst = static_cast<TO*>(a.out) + (uint64_t)i * (uint64_t)a.out_stride;
+    Pack<TI, V> in[K];
+    if (!zero && !fresh) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int64_t c = c0 + (int64_t)k * L * V;
+        if (c < a.d) in[k].load(src + c);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t c = c0 + (int64_t)k * L * V;
+      if (c >= a.d) continue;
+      float x[V];
+      if (zero) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] = 0.f;
+      } else {
+        if (fresh) {
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            x[j] = init_weight(a.hinfo->seed, a.hinfo->tag, (uint64_t)id * (uint64_t)a.d + (uint64_t)(c + j));
+        } else {
+          in[k].get(x);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] *= a.scale;
+      }
+      Pack<TO, V> o;
+      o.set(x);
+      o.store(dst + c);
+    }
+  }
+}
+
+template <typename TI, typename TO, int V>
+cudaError_t embed_as(const EmbedArgs& a, int num_sms, cudaStream_t s) {
+  const int64_t pieces = (a.d + V - 1) / V;
+  int lg = 0;
+  while ((1 << lg) < pieces && lg < 5) ++lg;
+  constexpr int K = 4;
+  // four pieces a lane in flight, unless that leaves SMs without work
+  const bool wide = a.n * pieces / (32 * K) >= (int64_t)num_sms * 16;
+  const int64_t slab = (int64_t)(wide ? K : 1) << lg;
+  const int64_t slabs = (pieces + slab - 1) / slab;
+  const int64_t blocks = (a.n + (THREADS >> lg) - 1) / (THREADS >> lg);
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * 32), (unsigned)slabs);
+  return wide ? launch_following(k_embed<TI, TO, V, K>, grid, THREADS, 0, s, a, lg)
+              : launch_following(k_embed<TI, TO, V, 1>, grid, THREADS, 0, s, a, lg);
+}
+
+template <typename TI, typename TO>
+cudaError_t embed_types(const EmbedArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int most = 16 / (int)std::min(sizeof(TI), sizeof(TO));
+  const int v = std::min(vector_of(most, a.w, a.w_stride, a.d, sizeof(TI)),
+                         vector_of(most, a.out, a.out_stride, a.d, sizeof(TO)));
+  if constexpr (most == 8)
+    if (v == 8) return embed_as<TI, TO, 8>(a, num_sms, s);
+  if (v == 4) return embed_as<TI, TO, 4>(a, num_sms, s);
+  if (v == 2) return embed_as<TI, TO, 2>(a, num_sms, s);
+  return embed_as<TI, TO, 1>(a, num_sms, s);
+}
+
+// ---- gradient: workspace -------------------------------------------------------------
+
+struct Counters {
+  uint32_t step;     // the call's error word
+  uint32_t tickets[MAX_PASSES];
+  uint32_t scan_ticket;
+  uint32_t n_items, n_runs, n_cut;
+  uint32_t P;        // positions that are no padding: the first P of the sorted ones
+  uint32_t pad[6];
+};
+static_assert(sizeof(Counters) == 64, "the histograms follow it");
+
+struct Item {
+  uint32_t start;  // position << 1 | starts its run
+  uint32_t run;    // run << 1 | the run has several items
+};
+
+// Where the parts of the workspace are; what must start at zero comes first.
+struct GradPlan {
+  SortPlan sort;
+  size_t counters, hist, sort_status, scan_status, cleared;  // cleared: bytes from 0 on
+  size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, bytes;
+  int64_t tiles;
+};
+
+GradPlan plan_of(const EmbedGradArgs& a) {
+  GradPlan p{};
+  const uint64_t top = (uint64_t)a.V;  // the key that stands for padding
+  int bits = 1;
+  while (bits < 32 && (top >> bits) != 0) ++bits;
+  p.sort = make_sort_plan(bits, 9);
+  p.tiles = (a.n + ITEM_TILE - 1) / ITEM_TILE;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return o;
+  };
+  const size_t n = (size_t)a.n;
+  p.counters = take(sizeof(Counters));
+  p.hist = take((size_t)MAX_PASSES * MAX_RADIX * 4);
+  p.sort_status = take(sort_status_words(a.n, p.sort.radix) * 8);
+  p.scan_status = take((size_t)p.tiles * 8);
+  p.cleared = at;
+  for (int i = 0; i < 2; ++i) {
+    p.keys[i] = take(n * 4);
+    p.vals[i] = take(n * 4);
+  }
+  p.items = take(n * sizeof(Item));
+  p.run_row = take(n * 4);
+  p.run_start = take(n * 4);
+  p.cuts = take((n / CUT + 1) * 8);
+  p.parts = take((2 * (n / CUT) + 2) * (size_t)a.d * 4);
+  p.bytes = at;
+  return p;
+}
+
+// ---- gradient: sort --------------------------------------------------------------------
+
+__global__ void __launch_bounds__(THREADS) k_token_clear(uint4* p, int64_t n) {
+  follow();
+  for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS)
+    p[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+struct KeyArgs {
+  const int64_t* ids;
+  uint32_t n;
+  int32_t id_mode;
+  int64_t pad_id;
+  int64_t V;
+  uint64_t mod_magic;
+  uint32_t* hist;  // [passes][radix]
+  uint32_t* keys;
+};
+
+// The row of every id (V at padding positions, so that they sort last) and the digit
+// counts of every pass.
+__global__ void __launch_bounds__(THREADS) k_token_keys(KeyArgs a, SortPlan plan, ErrSink err) {
+  __shared__ uint32_t h[MAX_PASSES * MAX_RADIX];
+  const int words = plan.passes * plan.radix;
+  for (int i = threadIdx.x; i < words; i += THREADS) h[i] = 0u;
+  follow();
+  __syncthreads();
+  const uint32_t stride = gridDim.x * THREADS;
+  for (uint32_t i = blockIdx.x * THREADS + threadIdx.x; i < a.n; i += stride) {
+    const int64_t id = a.ids[i];
+    uint32_t key;
+    if (id == a.pad_id && a.pad_id != GBA_NO_PAD) {
+      key = (uint32_t)a.V;
+    } else if (a.id_mode == GBA_ID_MODULO) {
+      key = (uint32_t)mod_u64((uint64_t)id, (uint64_t)a.V, a.mod_magic);
+    } else {
+      key = (uint32_t)id;
+      if (id < 0 || id >= a.V) {
+        raise_error(err, ERR_ID_RANGE);
+        key = (uint32_t)a.V;
+      }
+    }
+    a.keys[i] = key;
+    for (int p = 0; p < plan.passes; ++p)
+      atomicAdd(h + p * plan.radix + ((key >> plan.shift[p]) & plan.mask[p]), 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < words; i += THREADS)
+    if (h[i]) atomicAdd(a.hist + i, h[i]);
+}
+
+// ---- gradient: items ---------------------------------------------------------------------
+
+struct ItemArgs {
+  const uint32_t* keys;  // sorted rows
+  uint32_t n;
+  uint32_t pad_key;
+  Counters* ctr;
+  unsigned long long* status;  // [tiles]
+  Item* items;
+  uint32_t* run_row;
+  uint32_t* run_start;
+  uint2* cuts;       // (run, first cut)
+  int64_t* ids_out;  // message form
+};
+
+// Look-back word: [61:60] flag, [59:30] items, [29:0] runs.
+constexpr unsigned long long SCAN_AGG = 1ull << 60;
+constexpr unsigned long long SCAN_INCL = 2ull << 60;
+constexpr unsigned long long SCAN_VALUE = (1ull << 60) - 1;
+
+// Heads of runs and items, numbered over the whole array by one pass with decoupled
+// look-back (Merrill & Garland 2016), tiles by ticket.  Every wait is bounded.
+__global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err, int64_t wait_ns) {
+  constexpr int WARPS = THREADS / 32, PER_WARP = ITEM_TILE / WARPS, ROUNDS = PER_WARP / 32;
+  __shared__ uint32_t s_tile, s_failed;
+  __shared__ unsigned long long s_warp[WARPS];
+  __shared__ unsigned long long s_prefix;
+  follow();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) {
+    s_tile = atomicAdd(&a.ctr->scan_ticket, 1u);
+    s_failed = *(const volatile uint32_t*)err.step;
+  }
+  __syncthreads();
+  if (s_failed != 0u) return;  // the counters stay zero: no items, no runs
+  const uint32_t tile = s_tile;
+  const uint32_t base = tile * (uint32_t)ITEM_TILE + (uint32_t)(warp * PER_WARP);
+
+  uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS];
+  unsigned long long sum = 0ull;
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const uint32_t p = base + (uint32_t)(j * 32 + lane);
+    bool head = false, start = false;
+    key[j] = a.pad_key;
+    if (p < a.n) {
+      key[j] = a.keys[p];
+      const uint32_t before = p > 0 ? a.keys[p - 1] : ~0u;
+      const bool real = key[j] != a.pad_key;
+      head = real && key[j] != before;
+      start = head || (real && p % CUT == 0 && p >= CUT && a.keys[p - CUT] == key[j]);
+      if (real && (p + 1 == a.n || a.keys[p + 1] == a.pad_key)) a.ctr->P = p + 1;
+    }
+    heads[j] = __ballot_sync(FULL, head);
+    starts[j] = __ballot_sync(FULL, start);
+    sum += (unsigned long long)__popc(starts[j]) << 30 | (unsigned long long)__popc(heads[j]);
+  }
+  if (lane == 0) s_warp[warp] = sum;
+  __syncthreads();
+  unsigned long long before = 0ull, total = 0ull;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) {
+    if (w < warp) before += s_warp[w];
+    total += s_warp[w];
+  }
+  if (warp == 0) {
+    unsigned long long prefix = 0ull;
+    if (lane == 0) st_relaxed_u64(a.status + tile, (tile == 0 ? SCAN_INCL : SCAN_AGG) | total);
+    if (tile > 0) {
+      int64_t j = (int64_t)tile - 1 - lane;
+      const uint64_t t0 = globaltimer_ns();
+      for (;;) {
+        const unsigned long long v = j >= 0 ? ld_relaxed_u64(a.status + j) : SCAN_INCL;
+        const uint32_t incl = __ballot_sync(FULL, (v & SCAN_INCL) != 0ull);
+        const uint32_t ready = __ballot_sync(FULL, v >> 60 != 0ull);
+        const uint32_t used = incl ? (incl & (0u - incl)) * 2u - 1u : FULL;  // up to the nearest inclusive one
+        if ((ready & used) == used) {
+          unsigned long long x = used >> lane & 1u ? v & SCAN_VALUE : 0ull;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(FULL, x, o);
+          prefix += x;
+          if (incl) break;
+          j -= 32;
+          continue;
+        }
+        const bool give_up = (int64_t)(globaltimer_ns() - t0) > wait_ns;
+        if (__any_sync(FULL, give_up)) {
+          if (lane == 0) raise_error(err, ERR_TIMEOUT);
+          break;
+        }
+        __nanosleep(LOOKBACK_SLEEP_NS);
+      }
+      if (lane == 0) st_relaxed_u64(a.status + tile, SCAN_INCL | ((prefix + total) & SCAN_VALUE));
+    }
+    if (lane == 0) {
+      s_prefix = prefix;
+      if (tile + 1 == gridDim.x) {
+        a.ctr->n_items = (uint32_t)((prefix + total) >> 30) & 0x3FFFFFFFu;
+        a.ctr->n_runs = (uint32_t)(prefix + total) & 0x3FFFFFFFu;
+      }
+    }
+  }
+  __syncthreads();
+  before += s_prefix;
+  uint32_t item = (uint32_t)(before >> 30) & 0x3FFFFFFFu, run = (uint32_t)before & 0x3FFFFFFFu;
+  const uint32_t lt = lanemask_lt();
+#pragma unroll
+  for (int j = 0; j < ROUNDS; ++j) {
+    const uint32_t p = base + (uint32_t)(j * 32 + lane);
+    const uint32_t me = 1u << lane;
+    const uint32_t at = item + __popc(starts[j] & lt);
+    const bool head = (heads[j] & me) != 0u;
+    const uint32_t r = run + __popc(heads[j] & (lt | me)) - 1u;  // the run p belongs to
+    if ((starts[j] & me) && at < a.n && r < a.n) {  // the bounds hold unless a wait gave up
+      bool several = !head;
+      if (head) {
+        // the first cut of this run, if it has one
+        const uint32_t q = (p + CUT - 1) / CUT * CUT + CUT;
+        several = q < a.n && a.keys[q] == key[j];
+        a.run_row[r] = key[j];
+        a.run_start[r] = p;
+        if (a.ids_out) a.ids_out[r] = (int64_t)key[j];
+      } else if (p < 2 * CUT || a.keys[p - 2 * CUT] != key[j]) {
+        const uint32_t c = atomicAdd(&a.ctr->n_cut, 1u);
+        if (c <= a.n / CUT) a.cuts[c] = make_uint2(r, p);
+      }
+      a.items[at] = Item{p << 1 | (head ? 1u : 0u), r << 1 | (several ? 1u : 0u)};
+    }
+    item += __popc(starts[j]);
+    run += __popc(heads[j]);
+  }
+}
+
+// ---- gradient: sums ------------------------------------------------------------------------
+
+struct SumArgs {
+  const void* grad;
+  int64_t stride;
+  int32_t d;
+  int32_t accumulate;
+  float scale;
+  uint32_t n;
+  const uint32_t* order;
+  const Counters* ctr;
+  const Item* items;
+  const uint32_t* run_row;
+  const uint32_t* run_start;
+  const uint2* cuts;
+  float* parts;
+  int64_t* ids_out;  // message form: rows_out, n rows of d
+  int64_t* n_out;
+  float* out;
+  int64_t out_stride;
+};
+
+template <int V>
+__device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t run, int64_t c, float (&x)[V]) {
+  const uint64_t row = a.ids_out ? run : a.run_row[run];
+  float* dst = a.out + row * (uint64_t)a.out_stride + c;
+#pragma unroll
+  for (int j = 0; j < V; ++j) x[j] *= a.scale;
+  Pack<float, V> o;
+  if (a.accumulate) {
+    float y[V];
+    o.load(dst);
+    o.get(y);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] += y[j];
+  }
+  o.set(x);
+  o.store(dst);
+}
+
+// A lane group of 1 << lg lanes per item and slab.  Adds the item's gradient rows in
+// ascending order of their positions.
+template <typename T, int V>
+__global__ void __launch_bounds__(THREADS) k_token_sums(SumArgs a, int lg, ErrSink err) {
+  follow();
+  const bool failed = *(const volatile uint32_t*)err.step != 0u;
+  const uint32_t n_items = failed ? 0u : a.ctr->n_items, n_runs = failed ? 0u : a.ctr->n_runs, P = a.ctr->P;
+  const int L = 1 << lg;
+  const int l = threadIdx.x & (L - 1);
+  const uint32_t groups = gridDim.x * (uint32_t)(THREADS >> lg);
+  const int64_t c = ((int64_t)blockIdx.y * L + l) * V;
+  // the message form's slots that no row needs come after the items
+  const uint32_t units = a.ids_out ? n_items + (a.n - n_runs) : n_items;
+  if (a.n_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.n_out = n_runs;
+  const T* grad = static_cast<const T*>(a.grad);
+  for (uint64_t unit = ((uint64_t)blockIdx.x * THREADS + threadIdx.x) >> lg; unit < units; unit += groups) {
+    if (unit >= n_items) {
+      const uint32_t slot = n_runs + (uint32_t)(unit - n_items);
+      if (l == 0 && blockIdx.y == 0) a.ids_out[slot] = n_runs > 0 ? (int64_t)a.run_row[n_runs - 1] : -1;
+      if (c < a.d) {
+        float z[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = 0.f;
+        Pack<float, V> o;
+        o.set(z);
+        o.store(a.out + (uint64_t)slot * (uint64_t)a.out_stride + c);
+      }
+      continue;
+    }
+    if (c >= a.d) continue;
+    const Item it = a.items[unit];
+    const uint32_t s = it.start >> 1;
+    const uint32_t e = unit + 1 < n_items ? a.items[unit + 1].start >> 1 : P;
+    float x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = 0.f;
+    uint32_t p = s;
+    for (; p + 4 <= e; p += 4) {
+      Pack<T, V> g[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i].load(grad + (uint64_t)a.order[p + i] * (uint64_t)a.stride + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y[V];
+        g[i].get(y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] += y[j];
+      }
+    }
+    for (; p < e; ++p) {
+      Pack<T, V> g;
+      float y[V];
+      g.load(grad + (uint64_t)a.order[p] * (uint64_t)a.stride + c);
+      g.get(y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) x[j] += y[j];
+    }
+    if (it.run & 1u) {
+      // the item before the first cut, or the one that starts at a cut
+      const uint32_t slot = it.start & 1u ? 2u * ((s + CUT - 1) / CUT + 1u) : 2u * (s / CUT) + 1u;
+      Pack<float, V> o;
+      o.set(x);
+      o.store(a.parts + (uint64_t)slot * (uint64_t)a.d + c);
+    } else {
+      write_sum<V>(a, it.run >> 1, c, x);
+    }
+  }
+}
+
+// One block per cut run and slab of 32 * V columns: each warp adds a share of the items'
+// sums in order, and the warps' sums are added in order (compensated, so that a row of
+// a million tokens is as exact as one of a hundred).
+template <int V>
+__global__ void __launch_bounds__(THREADS) k_token_merge(SumArgs a, ErrSink err) {
+  constexpr int WARPS = THREADS / 32;
+  __shared__ float s_hi[WARPS][32 * V], s_lo[WARPS][32 * V];
+  follow();
+  if (*(const volatile uint32_t*)err.step != 0u) return;
+  const uint32_t n_cut = a.ctr->n_cut, n_runs = a.ctr->n_runs, P = a.ctr->P;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t c = ((int64_t)blockIdx.y * 32 + lane) * V;
+  for (uint32_t i = blockIdx.x; i < n_cut; i += gridDim.x) {
+    const uint2 cut = a.cuts[i];
+    const uint32_t end = cut.x + 1 < n_runs ? a.run_start[cut.x + 1] : P;
+    const uint32_t parts = 1u + (end - cut.y + CUT - 1) / CUT;  // before the first cut, and from each on
+    const uint32_t each = (parts + WARPS - 1) / WARPS;
+    const uint32_t lo = min(parts, warp * each), hi = min(parts, lo + each);
+    CSum x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = CSum{0.f, 0.f};
+    if (c < a.d) {
+#pragma unroll 4
+      for (uint32_t k = lo; k < hi; ++k) {
+        const uint64_t slot = 2ull * (cut.y / CUT) + (k == 0 ? 0u : 2u * k - 1u);
+        Pack<float, V> g;
+        float y[V];
+        g.load(a.parts + slot * (uint64_t)a.d + c);
+        g.get(y);
+#pragma unroll
+        for (int j = 0; j < V; ++j) csum_add(x[j], y[j]);
+      }
+    }
+    __syncthreads();  // the block is done with the run before
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      s_hi[warp][lane * V + j] = x[j].hi;
+      s_lo[warp][lane * V + j] = x[j].lo;
+    }
+    __syncthreads();
+    if (warp == 0 && c < a.d) {
+      for (int w = 1; w < WARPS; ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) csum_merge(x[j], s_hi[w][lane * V + j], s_lo[w][lane * V + j]);
+      float y[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = csum_value(x[j]);
+      write_sum<V>(a, cut.x, c, y);
+    }
+  }
+}
+
+template <typename T, int V>
+cudaError_t sums_as(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) {
+  const int64_t pieces = (a.d + V - 1) / V;
+  int lg = 0;
+  while ((1 << lg) < pieces && lg < 5) ++lg;
+  const int64_t slabs = (pieces + (1 << lg) - 1) >> lg;
+  const int64_t units = (int64_t)a.n + a.n / CUT;
+  const int64_t blocks = (units + (THREADS >> lg) - 1) / (THREADS >> lg);
+  const dim3 grid((unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * 16), (unsigned)slabs);
+  const cudaError_t e = launch_following(k_token_sums<T, V>, grid, THREADS, 0, s, a, lg, err);
+  if (e != cudaSuccess || a.n <= CUT) return e;  // no run can be cut
+  const dim3 mgrid((unsigned)std::min<int64_t>(a.n / CUT, (int64_t)num_sms * 4),
+                   (unsigned)((pieces + 31) / 32));
+  return launch_following(k_token_merge<V>, mgrid, THREADS, 0, s, a, err);
+}
+
+template <typename T>
+cudaError_t sums_type(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) {
+  constexpr int most = 16 / (int)sizeof(T);
+  const int v = std::min(vector_of(most, a.grad, a.stride, a.d, sizeof(T)),
+                         vector_of(most, a.out, a.out_stride, a.d, 4));
+  if constexpr (most == 8)
+    if (v == 8) return sums_as<T, 8>(a, err, num_sms, s);
+  if (v == 4) return sums_as<T, 4>(a, err, num_sms, s);
+  if (v == 2) return sums_as<T, 2>(a, err, num_sms, s);
+  return sums_as<T, 1>(a, err, num_sms, s);
+}
+
+}  // namespace
+
+cudaError_t launch_embed(const EmbedArgs& a, int32_t type, int32_t out_type, int num_sms,
+                         cudaStream_t s) {
+  if (type == GBA_F32) {
+    if (out_type == GBA_F32) return embed_types<float, float>(a, num_sms, s);
+    if (out_type == GBA_BF16) return embed_types<float, bf16>(a, num_sms, s);
+    return embed_types<float, f16>(a, num_sms, s);
+  }
+  if (type == GBA_BF16)
+    return out_type == GBA_F32 ? embed_types<bf16, float>(a, num_sms, s)
+                               : embed_types<bf16, bf16>(a, num_sms, s);
+  return out_type == GBA_F32 ? embed_types<f16, float>(a, num_sms, s)
+                             : embed_types<f16, f16>(a, num_sms, s);
+}
+
+size_t embed_grad_workspace(const EmbedGradArgs& a, size_t* step_word) {
+  const GradPlan p = plan_of(a);
+  *step_word = p.counters + offsetof(Counters, step);
+  return p.bytes;
+}
+
+cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns, int num_sms,
+                              cudaStream_t s) {
+  if (a.dense && !a.accumulate) {
+    const cudaError_t e =
+        a.dense_stride == a.d
+            ? cudaMemsetAsync(a.dense, 0, (size_t)a.V * a.d * 4, s)
+            : cudaMemset2DAsync(a.dense, (size_t)a.dense_stride * 4, 0, (size_t)a.d * 4, (size_t)a.V, s);
+    if (e != cudaSuccess) return e;
+  }
+  if (a.n == 0) return cudaSuccess;
+  const GradPlan p = plan_of(a);
+  auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
+  Counters* ctr = reinterpret_cast<Counters*>(ws + p.counters);
+  const int64_t words = (int64_t)p.cleared / 16;
+  cudaError_t e = launch_following(
+      k_token_clear, dim3((unsigned)std::min<int64_t>((words + THREADS - 1) / THREADS, num_sms * 4)),
+      THREADS, 0, s, reinterpret_cast<uint4*>(ws), words);
+  if (e != cudaSuccess) return e;
+  const KeyArgs ka{a.ids, (uint32_t)a.n, a.id_mode, a.pad_id, a.V, a.mod_magic, at(p.hist), at(p.keys[0])};
+  e = launch_following(k_token_keys, dim3((unsigned)std::min<int64_t>((a.n + 1023) / 1024, num_sms * 6)),
+                       THREADS, 0, s, ka, p.sort, a.err);
+  if (e != cudaSuccess) return e;
+  int in = 0;
+  for (int i = 0; i < p.sort.passes; ++i, in ^= 1) {
+    SortPass sp{};
+    sp.N = (uint32_t)a.n;
+    sp.hist = at(p.hist) + i * p.sort.radix;
+    sp.ticket = &ctr->tickets[i];
+    sp.keys_in = at(p.keys[in]);
+    sp.vals_in = at(p.vals[in]);
+    sp.keys_out = at(p.keys[in ^ 1]);
+    sp.vals_out = at(p.vals[in ^ 1]);
+    sp.status = reinterpret_cast<unsigned long long*>(ws + p.sort_status);
+    sp.epoch = (uint32_t)i + 1u;
+    launch_onesweep(p.sort, i, sp, a.err, wait_ns, s);
+  }
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const ItemArgs ia{at(p.keys[in]), (uint32_t)a.n, (uint32_t)a.V, ctr,
+                    reinterpret_cast<unsigned long long*>(ws + p.scan_status),
+                    reinterpret_cast<Item*>(ws + p.items), at(p.run_row), at(p.run_start),
+                    reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out};
+  e = launch_following(k_token_items, dim3((unsigned)p.tiles), THREADS, 0, s, ia, a.err, wait_ns);
+  if (e != cudaSuccess) return e;
+  SumArgs sa{};
+  sa.grad = a.grad;
+  sa.stride = a.stride;
+  sa.d = a.d;
+  sa.accumulate = a.accumulate;
+  sa.scale = a.scale;
+  sa.n = (uint32_t)a.n;
+  sa.order = at(p.vals[in]);
+  sa.ctr = ctr;
+  sa.items = ia.items;
+  sa.run_row = ia.run_row;
+  sa.run_start = ia.run_start;
+  sa.cuts = ia.cuts;
+  sa.parts = reinterpret_cast<float*>(ws + p.parts);
+  sa.ids_out = a.ids_out;
+  sa.n_out = a.n_out;
+  sa.out = a.dense ? a.dense : a.rows_out;
+  sa.out_stride = a.dense ? a.dense_stride : a.d;
+  if (a.type == GBA_F32) return sums_type<float>(sa, a.err, num_sms, s);
+  if (a.type == GBA_BF16) return sums_type<bf16>(sa, a.err, num_sms, s);
+  return sums_type<f16>(sa, a.err, num_sms, s);
+}
+
+}  // namespace gba

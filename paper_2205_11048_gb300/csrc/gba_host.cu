@@ -16,6 +16,7 @@
 
 #include "gba.h"
 #include "gba_internal.cuh"
+#include "gba_worker.cuh"
 
 using namespace gba;
 
@@ -828,6 +829,17 @@ gba_status push_common(gba_handle* h, int64_t token, const gba_sparse_grad* per_
 }
 
 }  // namespace
+
+gba_status gba::table_view(gba_handle* h, int32_t t, TableView* v) {
+  if (!h || t < 0 || t >= h->T) return GBA_E_ARG;
+  if (h->failed) return set_err(h, GBA_E_STATE, "handle failed earlier");
+  cudaSetDevice(h->device);
+  join_steps(h);
+  const TableState& ts = h->tables[t];
+  *v = TableView{ts.w, ts.desc.rows, ts.desc.dim, ts.desc.id_mode, h->h_tinfo[t].mod_magic,
+                 h->d_hinfo + t, h->stream, h->device};
+  return GBA_OK;
+}
 
 extern "C" {
 
