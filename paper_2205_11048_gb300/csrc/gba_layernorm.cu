@@ -4,10 +4,9 @@
 //
 // Bound by HBM bandwidth: a row is read once, stays in registers while its statistics are
 // formed (mean first, then the squares of the differences, so a large mean costs no digits),
-// and is written once.  A row is held by 1 << lg threads of 16 columns each.  Backward, a
-// block keeps its threads' shares of dgamma and dbeta in registers over all the rows it
-// takes and leaves one partial row per group of threads; a second kernel adds the partial
-// rows in order.  Rows too wide for a block's registers are read again from L2 instead.
+// and is written once.  A row is held by 1 << lg threads of up to 16 columns each.  Backward,
+// a block keeps its threads' shares of dgamma and dbeta in registers over all the rows it
+// takes and leaves one partial row; a second kernel adds the partial rows in order.  Rows too wide for a block's registers are read again from L2 instead.
 #include <algorithm>
 
 #include "gba_worker.cuh"
@@ -17,9 +16,8 @@ namespace gba {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int EPT = 16;          // columns a thread holds
-constexpr int MOST_LG = 10;      // forward: rows of up to 16,384 columns in registers
-constexpr int MOST_LG_GRAD = 9;  // backward: 8,192
+constexpr int EPT = 16;      // columns a thread holds, forward
+constexpr int MOST_LG = 10;  // so rows of up to 16,384 columns stay in registers
 constexpr uint32_t FULL = 0xffffffffu;
 
 __device__ __forceinline__ float param_at(const void* p, int32_t type, int64_t i, float missing) {
@@ -27,6 +25,30 @@ __device__ __forceinline__ float param_at(const void* p, int32_t type, int64_t i
   if (type == GBA_F32) return static_cast<const float*>(p)[i];
   if (type == GBA_BF16) return to_float(static_cast<const bf16*>(p)[i]);
   return to_float(static_cast<const f16*>(p)[i]);
+}
+
+// V consecutive ones, c a multiple of V.
+template <int V>
+__device__ __forceinline__ void params_at(const void* p, int32_t type, int64_t c, float missing,
+                                          float (&x)[V]) {
+  if (p && (uintptr_t)p % 16 == 0) {
+    if (type == GBA_F32) {
+      Pack<float, V> w;
+      w.load(static_cast<const float*>(p) + c);
+      w.get(x);
+    } else if (type == GBA_BF16) {
+      Pack<bf16, V> w;
+      w.load(static_cast<const bf16*>(p) + c);
+      w.get(x);
+    } else {
+      Pack<f16, V> w;
+      w.load(static_cast<const f16*>(p) + c);
+      w.get(x);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = param_at(p, type, c + j, missing);
+  }
 }
 
 // Sums of N values over the 1 << lg threads of a row, in every one of them.  s: a word per
@@ -51,25 +73,42 @@ __device__ __forceinline__ void row_sum(float (&x)[N], int lg, float (*s)[N]) {
     for (int i = 0; i < N; ++i) x[i] += s[first + w][i];
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(1024) k_layer_norm(LayerNormArgs a, int lg) {
+// KEEP: a thread's parameters stay in registers over all the rows its block takes.  The next
+// row's loads are in flight while this one is reduced.
+template <typename T, int V, bool KEEP>
+__global__ void __launch_bounds__(KEEP ? 512 : 1024) k_layer_norm(LayerNormArgs a, int lg) {
   constexpr int K = EPT / V;
   __shared__ float s_sum[2][32][1];
   follow();
   const int tpr = 1 << lg, t = threadIdx.x & (tpr - 1);
-  const int per_block = (int)blockDim.x >> lg;
+  const int64_t per_pass = (int64_t)gridDim.x * ((int)blockDim.x >> lg);
   const float inv_d = 1.f / (float)a.d;
-  for (int64_t r0 = (int64_t)blockIdx.x * per_block; r0 < a.n; r0 += (int64_t)gridDim.x * per_block) {
-    const int64_t row = r0 + (threadIdx.x >> lg);
-    const bool live = row < a.n;
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    T* y = static_cast<T*>(a.y) + row * a.y_stride;
-    Pack<T, V> in[K];
+  float gamma[KEEP ? K : 1][V], beta[KEEP ? K : 1][V];
+  if (KEEP)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * tpr + t) * V;
-      if (live && c < a.d) in[k].load(x + c);
+      if (c < a.d) {
+        params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[k]);
+        params_at<V>(a.beta, a.param_type, c, 0.f, beta[k]);
+      }
     }
+  Pack<T, V> in[K];
+  auto fetch = [&](int64_t row) {
+    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * tpr + t) * V;
+      if (row < a.n && c < a.d) in[k].load(x + c);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * ((int)blockDim.x >> lg) + (threadIdx.x >> lg);
+  // all threads of a block go round equally often: they meet in the sums
+  int64_t first = (int64_t)blockIdx.x * ((int)blockDim.x >> lg);
+  fetch(row);
+  for (; first < a.n; first += per_pass, row += per_pass) {
+    const bool live = row < a.n;
+    T* y = static_cast<T*>(a.y) + row * a.y_stride;
     float v[K][V];
     float sum[1] = {0.f};
 #pragma unroll
@@ -83,6 +122,7 @@ __global__ void __launch_bounds__(1024) k_layer_norm(LayerNormArgs a, int lg) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += v[k][j];
     }
+    fetch(row + per_pass);
     row_sum<1>(sum, lg, s_sum[0]);
     const float mean = sum[0] * inv_d;
     sum[0] = 0.f;
@@ -106,10 +146,14 @@ __global__ void __launch_bounds__(1024) k_layer_norm(LayerNormArgs a, int lg) {
     for (int k = 0; k < K; ++k) {
       const int c = (k * tpr + t) * V;
       if (!live || c >= a.d) continue;
+      float* gk = gamma[KEEP ? k : 0];
+      float* bk = beta[KEEP ? k : 0];
+      if (!KEEP) {
+        params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[0]);
+        params_at<V>(a.beta, a.param_type, c, 0.f, beta[0]);
+      }
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        v[k][j] = fmaf(v[k][j] * rstd, param_at(a.gamma, a.param_type, c + j, 1.f),
-                       param_at(a.beta, a.param_type, c + j, 0.f));
+      for (int j = 0; j < V; ++j) v[k][j] = fmaf(v[k][j] * rstd, gk[j], bk[j]);
       Pack<T, V> o;
       o.set(v[k]);
       o.store(y + c);
@@ -153,94 +197,153 @@ __global__ void __launch_bounds__(1024) k_layer_norm_wide(LayerNormArgs a) {
     for (int64_t c = (int64_t)threadIdx.x * V; c < a.d; c += step) {
       w.load(x + c);
       w.get(v);
+      float gamma[V], beta[V];
+      params_at<V>(a.gamma, a.param_type, c, 1.f, gamma);
+      params_at<V>(a.beta, a.param_type, c, 0.f, beta);
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        v[j] = fmaf((v[j] - mean) * rstd, param_at(a.gamma, a.param_type, c + j, 1.f),
-                    param_at(a.beta, a.param_type, c + j, 0.f));
+      for (int j = 0; j < V; ++j) v[j] = fmaf((v[j] - mean) * rstd, gamma[j], beta[j]);
       w.set(v);
       w.store(y + c);
     }
   }
 }
 
-// Partial rows of dgamma and dbeta: [2][parts][d].
+// Columns that a thread of the gradient holds: as many as leave room for the weights, the two
+// sums, and the loads of this row and the next one.
 template <typename T, int V>
-__global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, int lg) {
-  constexpr int K = EPT / V;
-  __shared__ float s_sum[2][16][2];
+constexpr int EPT_GRAD = sizeof(T) == 2 && V > 1 ? 16 : 8;
+
+// One partial row of dgamma and dbeta per block: [2][blocks][d].  What a thread keeps of a row
+// while its sums are formed is its loads; h and g are formed from them twice.  FETCH: the
+// next row's loads are in flight meanwhile.
+template <typename T, int V, bool FETCH>
+__global__ void __launch_bounds__(FETCH ? 512 : 1024) k_layer_norm_grad(LayerNormArgs a, int lg) {
+  constexpr int EPT_ = EPT_GRAD<T, V>, K = EPT_ / V;
+  __shared__ float s_sum[2][32][2];
+  __shared__ float s_part[THREADS * EPT_];
   follow();
-  const int tpr = 1 << lg, t = threadIdx.x & (tpr - 1), group = (int)threadIdx.x >> lg;
+  const int tpr = 1 << lg, t = threadIdx.x & (tpr - 1);
   const int per_block = (int)blockDim.x >> lg;
+  const int64_t per_pass = (int64_t)gridDim.x * per_block;
   const float inv_d = 1.f / (float)a.d;
   float gamma[K][V], dg[K][V], db[K][V];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * tpr + t) * V;
+    if (c < a.d) params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[k]);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (k * tpr + t) * V + j;
-      gamma[k][j] = c < a.d ? param_at(a.gamma, a.param_type, c, 1.f) : 0.f;
-      dg[k][j] = db[k][j] = 0.f;
-    }
-  int flip = 0;
-  for (int64_t r0 = (int64_t)blockIdx.x * per_block; r0 < a.n; r0 += (int64_t)gridDim.x * per_block) {
-    const int64_t row = r0 + group;
-    const bool live = row < a.n;
+    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
+  }
+  Pack<T, V> xin[K], din[K], xnext[FETCH ? K : 1], dnext[FETCH ? K : 1];
+  float mean = 0.f, rstd = 0.f, mnext = 0.f, rnext = 0.f;
+  auto fetch = [&](int64_t row, Pack<T, V>* xs, Pack<T, V>* ds, float& m, float& r) {
+    if (row >= a.n) return;
     const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
     const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
-    T* dx = static_cast<T*>(a.y) + row * a.y_stride;
-    Pack<T, V> xin[K], din[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * tpr + t) * V;
-      if (live && c < a.d) {
-        xin[k].load(x + c);
-        din[k].load(dy + c);
+      if (c < a.d) {
+        xs[k].load(x + c);
+        ds[k].load(dy + c);
       }
     }
-    const float mean = live ? a.mean[row] : 0.f, rstd = live ? a.rstd[row] : 0.f;
-    float h[K][V], g[K][V];
+    m = a.mean[row];
+    r = a.rstd[row];
+  };
+  int64_t first = (int64_t)blockIdx.x * per_block;
+  int64_t row = first + ((int)threadIdx.x >> lg);
+  if (FETCH) fetch(row, xnext, dnext, mnext, rnext);
+  int flip = 0;
+  for (; first < a.n; first += per_pass, row += per_pass) {
+    const bool live = row < a.n;
+    if constexpr (FETCH) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        xin[k] = xnext[k];
+        din[k] = dnext[k];
+      }
+      mean = mnext;
+      rstd = rnext;
+      fetch(row + per_pass, xnext, dnext, mnext, rnext);
+    } else {
+      fetch(row, xin, din, mean, rstd);
+    }
     float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * tpr + t) * V;
-      if (live && c < a.d) {
-        xin[k].get(h[k]);
-        din[k].get(g[k]);
+      if (!live || c >= a.d) continue;
+      float x[V], g[V];
+      xin[k].get(x);
+      din[k].get(g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          h[k][j] = (h[k][j] - mean) * rstd;
-          db[k][j] += g[k][j];
-          dg[k][j] = fmaf(g[k][j], h[k][j], dg[k][j]);
-          g[k][j] *= gamma[k][j];
-          sum[0] += g[k][j];
-          sum[1] = fmaf(g[k][j], h[k][j], sum[1]);
-        }
+      for (int j = 0; j < V; ++j) {
+        const float h = (x[j] - mean) * rstd;
+        db[k][j] += g[j];
+        dg[k][j] = fmaf(g[j], h, dg[k][j]);
+        g[j] *= gamma[k][j];
+        sum[0] += g[j];
+        sum[1] = fmaf(g[j], h, sum[1]);
       }
     }
     row_sum<2>(sum, lg, s_sum[flip]);
     flip ^= 1;
     const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
+    T* dx = static_cast<T*>(a.y) + row * a.y_stride;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int c = (k * tpr + t) * V;
       if (!live || c >= a.d) continue;
+      float x[V], g[V];
+      xin[k].get(x);
+      din[k].get(g);
 #pragma unroll
-      for (int j = 0; j < V; ++j) g[k][j] = rstd * (g[k][j] - mg - h[k][j] * mgh);
+      for (int j = 0; j < V; ++j) {
+        const float h = (x[j] - mean) * rstd;
+        g[j] = rstd * (g[j] * gamma[k][j] - mg - h * mgh);
+      }
       Pack<T, V> o;
-      o.set(g[k]);
+      o.set(g);
       o.store(dx + c);
     }
   }
-  const int64_t part = (int64_t)blockIdx.x * per_block + group, parts = (int64_t)gridDim.x * per_block;
+  // the block's groups of threads, in order: first those within a warp, then through shared memory
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = (k * tpr + t) * V;
-    if (c >= a.d) continue;
+  for (int k = 0; k < K; ++k)
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      a.parts[part * a.d + c + j] = dg[k][j];
-      a.parts[(parts + part) * a.d + c + j] = db[k][j];
+    for (int j = 0; j < V; ++j)
+      for (int o = tpr; o < 32; o <<= 1) {
+        dg[k][j] += __shfl_xor_sync(FULL, dg[k][j], o);
+        db[k][j] += __shfl_xor_sync(FULL, db[k][j], o);
+      }
+  const int lgw = lg < 5 ? 5 : lg;
+  const int groups = (int)blockDim.x >> lgw, group = (int)threadIdx.x >> lgw, width = tpr * EPT_;
+  const bool one_of = lg >= 5 || (threadIdx.x & 31) < tpr;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* out = a.parts + ((int64_t)which * gridDim.x + blockIdx.x) * a.d;
+    float(*mine)[V] = which == 0 ? dg : db;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * tpr + t) * V;
+      if (!one_of || c >= a.d) continue;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (groups == 1)
+          out[c + j] = mine[k][j];
+        else
+          s_part[group * width + c + j] = mine[k][j];
+      }
     }
+    if (groups == 1) continue;
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+      float x = 0.f;
+      for (int g = 0; g < groups; ++g) x += s_part[g * width + c];
+      out[c] = x;
+    }
+    __syncthreads();
   }
 }
 
@@ -264,9 +367,11 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad_wide(LayerNormArgs a) {
       w.get(h);
       w.load(dy + c);
       w.get(g);
+      float gamma[V];
+      params_at<V>(a.gamma, a.param_type, c, 1.f, gamma);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float gj = g[j] * param_at(a.gamma, a.param_type, c + j, 1.f);
+        const float gj = g[j] * gamma[j];
         sum[0] += gj;
         sum[1] = fmaf(gj, (h[j] - mean) * rstd, sum[1]);
       }
@@ -279,9 +384,11 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad_wide(LayerNormArgs a) {
       w.get(h);
       w.load(dy + c);
       w.get(g);
+      float gamma[V];
+      params_at<V>(a.gamma, a.param_type, c, 1.f, gamma);
 #pragma unroll
       for (int j = 0; j < V; ++j)
-        g[j] = rstd * (g[j] * param_at(a.gamma, a.param_type, c + j, 1.f) - mg - (h[j] - mean) * rstd * mgh);
+        g[j] = rstd * (g[j] * gamma[j] - mg - (h[j] - mean) * rstd * mgh);
       w.set(g);
       w.store(dx + c);
     }
@@ -319,10 +426,10 @@ __global__ void __launch_bounds__(THREADS) k_layer_norm_columns(LayerNormArgs a)
   }
 }
 
-// The partial rows, added in order: a block takes 32 columns, its 8 warps a share of the rows
-// each.  blockIdx.y: dgamma or dbeta.
-__global__ void __launch_bounds__(THREADS) k_layer_norm_params(LayerNormArgs a, int64_t parts) {
-  constexpr int WARPS = THREADS / 32;
+// The partial rows, added in order: a block takes 32 columns, each of its warps a share of
+// the rows.  blockIdx.y: dgamma or dbeta.
+__global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int parts) {
+  constexpr int WARPS = 32;
   __shared__ float s[WARPS][33];
   follow();
   float* out = blockIdx.y == 0 ? a.dgamma : a.dbeta;
@@ -330,23 +437,24 @@ __global__ void __launch_bounds__(THREADS) k_layer_norm_params(LayerNormArgs a, 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   const float* p = a.parts + (int64_t)blockIdx.y * parts * a.d;
-  const int64_t each = (parts + WARPS - 1) / WARPS;
-  const int64_t lo = warp * each, hi = lo + each < parts ? lo + each : parts;
+  const int each = (parts + WARPS - 1) / WARPS;
+  const int lo = min(parts, warp * each), hi = min(parts, lo + each);
   float x = 0.f;
   if (c < a.d)
 #pragma unroll 8
-    for (int64_t i = lo; i < hi; ++i) x += p[i * a.d + c];
+    for (int i = lo; i < hi; ++i) x += p[(int64_t)i * a.d + c];
   s[warp][lane] = x;
   __syncthreads();
   if (warp == 0 && c < a.d) {
+#pragma unroll 8
     for (int w = 1; w < WARPS; ++w) x += s[w][lane];
     out[c] = x;
   }
 }
 
-int lg_of(int32_t d) {
+int lg_of(int32_t d, int ept) {
   int lg = 0;
-  while (((int64_t)EPT << lg) < d) ++lg;
+  while (((int64_t)ept << lg) < d) ++lg;
   return lg;
 }
 
@@ -359,92 +467,114 @@ Shape shape_of(int64_t n, int lg, int num_sms, int threads_per_sm) {
   const int64_t blocks = (n + (threads >> lg) - 1) / (threads >> lg);
   return Shape{(unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * (threads_per_sm / (int)threads)), threads};
 }
-constexpr int GRAD_THREADS_PER_SM = 512;
+// Threads of a kernel that an SM holds, in blocks of so many.
+template <typename F>
+int threads_per_sm(F* kernel, int threads) {
+  int blocks = 0;
+  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, 0) != cudaSuccess || blocks < 1)
+    blocks = 1;
+  return blocks * threads;
+}
 constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns
 
 template <typename T, int V>
 cudaError_t norm_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  const int lg = lg_of(a.d);
+  const int lg = lg_of(a.d, EPT);
   if (lg > MOST_LG)
     return launch_following(k_layer_norm_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 2)), 1024,
                             0, s, a);
-  const Shape sh = shape_of(a.n, lg, num_sms, 2048);
-  return launch_following(k_layer_norm<T, V>, dim3(sh.grid), sh.threads, 0, s, a, lg);
+  if (lg == MOST_LG) {
+    const Shape sh = shape_of(a.n, lg, num_sms, 1024);
+    return launch_following(k_layer_norm<T, V, false>, dim3(sh.grid), sh.threads, 0, s, a, lg);
+  }
+  static const int held[2] = {threads_per_sm(k_layer_norm<T, V, true>, THREADS),
+                              threads_per_sm(k_layer_norm<T, V, true>, 2 * THREADS)};
+  const Shape sh = shape_of(a.n, lg, num_sms, held[lg == 9]);
+  return launch_following(k_layer_norm<T, V, true>, dim3(sh.grid), sh.threads, 0, s, a, lg);
+}
+
+// The kernel of a gradient: rows of up to 8,192 columns stay in registers.
+enum class Way { FETCH, PLAIN, WIDE };
+struct GradShape {
+  Way way;
+  int lg;
+  Shape shape;
+  int parts;  // partial rows
+};
+
+template <typename T, int V>
+GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
+  GradShape g{};
+  g.lg = lg_of(a.d, EPT_GRAD<T, V>);
+  if (a.d > 8192) {
+    g.way = Way::WIDE;
+    g.parts = (int)std::min(a.n, WIDE_SPLIT);
+    return g;
+  }
+  g.way = g.lg <= 9 ? Way::FETCH : Way::PLAIN;
+  static const int held[2] = {threads_per_sm(k_layer_norm_grad<T, V, true>, THREADS),
+                              threads_per_sm(k_layer_norm_grad<T, V, true>, 2 * THREADS)};
+  g.shape = shape_of(a.n, g.lg, num_sms, g.way == Way::PLAIN ? 1024 : held[g.lg == 9]);
+  g.parts = (int)g.shape.grid;
+  return g;
 }
 
 template <typename T, int V>
 cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  const int lg = lg_of(a.d);
-  int64_t parts;
+  const GradShape g = grad_shape<T, V>(a, num_sms);
   cudaError_t e;
-  if (lg > MOST_LG_GRAD) {
-    parts = std::min(a.n, WIDE_SPLIT);
+  if (g.way == Way::WIDE) {
     const int64_t per = (int64_t)THREADS * V;
-    e = launch_following(k_layer_norm_columns<T, V>, dim3((unsigned)((a.d + per - 1) / per), (unsigned)parts),
+    e = launch_following(k_layer_norm_columns<T, V>, dim3((unsigned)((a.d + per - 1) / per), (unsigned)g.parts),
                          THREADS, 0, s, a);
     if (e == cudaSuccess)
       e = launch_following(k_layer_norm_grad_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 4)),
                            512, 0, s, a);
   } else {
-    const Shape sh = shape_of(a.n, lg, num_sms, GRAD_THREADS_PER_SM);
-    parts = (int64_t)sh.grid * (sh.threads >> lg);
-    e = launch_following(k_layer_norm_grad<T, V>, dim3(sh.grid), sh.threads, 0, s, a, lg);
+    auto kernel = k_layer_norm_grad<T, V, true>;
+    if constexpr (EPT_GRAD<T, V> == 8)  // the others hold 8,192 columns in 512 threads
+      if (g.way == Way::PLAIN) kernel = k_layer_norm_grad<T, V, false>;
+    e = launch_following(kernel, dim3(g.shape.grid), g.shape.threads, 0, s, a, g.lg);
   }
   if (e != cudaSuccess || (!a.dgamma && !a.dbeta)) return e;
-  return launch_following(k_layer_norm_params, dim3((unsigned)((a.d + 31) / 32), 2), THREADS, 0, s, a, parts);
+  return launch_following(k_layer_norm_params, dim3((unsigned)((a.d + 31) / 32), 2), 1024, 0, s, a, g.parts);
 }
 
-template <typename T>
-int vector_for(const LayerNormArgs& a) {
+// Calls f with the vector width of a's matrices.
+template <typename T, typename F>
+auto with_vector(const LayerNormArgs& a, F f) {
   constexpr int most = 16 / (int)sizeof(T);
   int v = std::min(vector_of(most, a.x, a.x_stride, a.d, sizeof(T)),
                    vector_of(most, a.y, a.y_stride, a.d, sizeof(T)));
-  return a.dy ? std::min(v, vector_of(most, a.dy, a.dy_stride, a.d, sizeof(T))) : v;
+  if (a.dy) v = std::min(v, vector_of(most, a.dy, a.dy_stride, a.d, sizeof(T)));
+  if constexpr (most == 8)
+    if (v == 8) return f(std::integral_constant<int, 8>());
+  if (v == 4) return f(std::integral_constant<int, 4>());
+  if (v == 2) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
 }
 
-template <typename T>
-cudaError_t norm_type(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  const int v = vector_for<T>(a);
-  if constexpr (sizeof(T) == 2)
-    if (v == 8) return norm_as<T, 8>(a, num_sms, s);
-  if (v == 4) return norm_as<T, 4>(a, num_sms, s);
-  if (v == 2) return norm_as<T, 2>(a, num_sms, s);
-  return norm_as<T, 1>(a, num_sms, s);
-}
-
-template <typename T>
-cudaError_t grad_type(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  const int v = vector_for<T>(a);
-  if constexpr (sizeof(T) == 2)
-    if (v == 8) return grad_as<T, 8>(a, num_sms, s);
-  if (v == 4) return grad_as<T, 4>(a, num_sms, s);
-  if (v == 2) return grad_as<T, 2>(a, num_sms, s);
-  return grad_as<T, 1>(a, num_sms, s);
+template <typename F>
+auto with_type(int32_t type, const LayerNormArgs& a, F f) {
+  if (type == GBA_F32) return with_vector<float>(a, [&](auto v) { return f(float(), v); });
+  if (type == GBA_BF16) return with_vector<bf16>(a, [&](auto v) { return f(bf16(), v); });
+  return with_vector<f16>(a, [&](auto v) { return f(f16(), v); });
 }
 
 }  // namespace
 
 cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, int num_sms, cudaStream_t s) {
-  if (type == GBA_F32) return norm_type<float>(a, num_sms, s);
-  if (type == GBA_BF16) return norm_type<bf16>(a, num_sms, s);
-  return norm_type<f16>(a, num_sms, s);
+  return with_type(type, a, [&](auto x, auto v) { return norm_as<decltype(x), v()>(a, num_sms, s); });
 }
 
-size_t layer_norm_grad_workspace(const LayerNormArgs& a, int num_sms) {
-  const int lg = lg_of(a.d);
-  int64_t parts = std::min(a.n, WIDE_SPLIT);
-  if (lg <= MOST_LG_GRAD) {
-    const Shape sh = shape_of(a.n, lg, num_sms, GRAD_THREADS_PER_SM);
-    parts = (int64_t)sh.grid * (sh.threads >> lg);
-  }
+size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms) {
+  const int parts = with_type(type, a, [&](auto x, auto v) { return grad_shape<decltype(x), v()>(a, num_sms).parts; });
   return (size_t)parts * 2 * (size_t)a.d * sizeof(float);
 }
 
 cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, int num_sms,
                                    cudaStream_t s) {
-  if (type == GBA_F32) return grad_type<float>(a, num_sms, s);
-  if (type == GBA_BF16) return grad_type<bf16>(a, num_sms, s);
-  return grad_type<f16>(a, num_sms, s);
+  return with_type(type, a, [&](auto x, auto v) { return grad_as<decltype(x), v()>(a, num_sms, s); });
 }
 
 }  // namespace gba

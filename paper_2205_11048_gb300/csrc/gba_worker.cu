@@ -456,7 +456,7 @@ gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_ma
   a.n = x->rows;
   a.d = x->cols;
   a.param_type = param_type;
-  const gba_status st = reserve(w, layer_norm_grad_workspace(a, w->num_sms));
+  const gba_status st = reserve(w, layer_norm_grad_workspace(a, x->type, w->num_sms));
   if (st != GBA_OK) return st;
   a.parts = reinterpret_cast<float*>(w->ws);
   const cudaError_t e = launch_layer_norm_grad(a, x->type, w->num_sms, w->stream);

@@ -207,7 +207,7 @@ struct LayerNormArgs {
   float* parts;  // workspace of the gradient
 };
 cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, int num_sms, cudaStream_t s);
-size_t layer_norm_grad_workspace(const LayerNormArgs& a, int num_sms);
+size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms);
 cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, int num_sms,
                                    cudaStream_t s);
 

@@ -39,7 +39,7 @@ cudaError_t launch_layer_norm(const LayerNormArgs&, int32_t, int, cudaStream_t) 
   ++g_launches;
   return cudaSuccess;
 }
-size_t layer_norm_grad_workspace(const LayerNormArgs& a, int) { return (size_t)a.d * 8; }
+size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t, int) { return (size_t)a.d * 8; }
 cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t, int, cudaStream_t) {
   ++g_launches;
   fake_need(a.parts, (size_t)a.d * 8);
