@@ -4,9 +4,14 @@
 //
 // Bound by HBM bandwidth: a row is read once, stays in registers while its statistics are
 // formed (mean first, then the squares of the differences, so a large mean costs no digits),
-// and is written once.  A row is held by 1 << lg threads of up to 16 columns each.  Backward,
-// a block keeps its threads' shares of dgamma and dbeta in registers over all the rows it
-// takes and leaves one partial row; a second kernel adds the partial rows in order.  Rows too wide for a block's registers are read again from L2 instead.
+// and is written once.  A row is held by up to 32 lanes, or by up to 16 warps, and the loads
+// of the next row are in flight while this one is reduced.  What a thread does for a row
+// beside its columns (two sums over lanes and warps, a root) costs as many instructions as
+// ten columns or so, so a thread holds 64 bytes of a row (backward 32 of each of the two),
+// and the arithmetic is done on pairs.  Backward, a block keeps its threads' shares of
+// dgamma and dbeta in registers over all the rows it takes and leaves one partial row; a
+// second kernel adds the partial rows in order.  Rows too wide for a block's registers are
+// read again from L2 instead.
 #include <algorithm>
 
 #include "gba_worker.cuh"
@@ -16,8 +21,8 @@ namespace gba {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int EPT = 16;      // columns a thread holds, forward
-constexpr int MOST_LG = 10;  // so rows of up to 16,384 columns stay in registers
+constexpr int MOST_WARPS = 16;  // that hold a row
+constexpr int WIDE_THREADS = 1024, WIDE_GRAD_THREADS = 512;  // of the kernels for rows of any width
 constexpr uint32_t FULL = 0xffffffffu;
 
 __device__ __forceinline__ float param_at(const void* p, int32_t type, int64_t i, float missing) {
@@ -51,120 +56,244 @@ __device__ __forceinline__ void params_at(const void* p, int32_t type, int64_t c
   }
 }
 
-// Sums of N values over the 1 << lg threads of a row, in every one of them.  s: a word per
-// warp and value; the caller alternates two of them, so one barrier is enough.
+// ---- two floats in one operation ---------------------------------------------------
+struct f2 {
+  unsigned long long u;
+};
+__device__ __forceinline__ f2 pair(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(f2 a, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.u));
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+  return r;
+}
+__device__ __forceinline__ float both(f2 a) {
+  float lo, hi;
+  split(a, lo, hi);
+  return lo + hi;
+}
+
+// ---- how a block's threads share rows ----------------------------------------------
+// A row belongs to L lanes of a warp, or to W whole warps; its threads' t-th piece of V
+// columns is piece k * tpr + t, for k = 0 .. E / V - 1.
+struct Split {
+  int L, W;
+};
+struct Place {
+  int t, tpr, group, groups;
+  int warp_group;  // the first group of the thread's warp: a warp's lanes go round together
+  __device__ __forceinline__ explicit Place(const Split& s) {
+    const int lane = threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
+    if (s.W == 1) {
+      t = lane & (s.L - 1);
+      tpr = s.L;
+      group = (int)threadIdx.x / s.L;
+      groups = (int)blockDim.x / s.L;
+      warp_group = warp * (32 / s.L);
+    } else {
+      t = warp % s.W * 32 + lane;
+      tpr = s.W * 32;
+      group = warp / s.W;
+      groups = (int)blockDim.x / tpr;
+      warp_group = group;
+    }
+  }
+};
+
+// Sums of N values over the threads of a row, in every one of them.  s: N words per warp of
+// the block; the caller alternates between two of them, so one barrier a sum is enough.
 template <int N>
-__device__ __forceinline__ void row_sum(float (&x)[N], int lg, float (*s)[N]) {
-  const int in_warp = lg < 5 ? lg : 5;
+__device__ __forceinline__ void row_sum(float (&x)[N], const Split& sp, int group, float (*s)[N]) {
+  if (sp.L == 32) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    for (int o = 1; o < 1 << in_warp; o <<= 1) x[i] += __shfl_xor_sync(FULL, x[i], o);
-  if (lg <= 5) return;
-  const int warp = threadIdx.x >> 5;
+    for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+  } else {
+    for (int o = 1; o < sp.L; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+  }
+  if (sp.W == 1) return;
+  const int warp = (int)threadIdx.x >> 5;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
     for (int i = 0; i < N; ++i) s[warp][i] = x[i];
-  __syncthreads();
-  const int warps = 1 << (lg - 5), first = warp & ~(warps - 1);
+  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(sp.W * 32) : "memory");
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = 0.f;
-  for (int w = 0; w < warps; ++w)
+  for (int w = 0; w < sp.W; ++w)
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += s[first + w][i];
+    for (int i = 0; i < N; ++i) x[i] += s[group * sp.W + w][i];
 }
 
-// KEEP: a thread's parameters stay in registers over all the rows its block takes.  The next
-// row's loads are in flight while this one is reduced.
-template <typename T, int V, bool KEEP>
-__global__ void __launch_bounds__(KEEP ? 512 : 1024) k_layer_norm(LayerNormArgs a, int lg) {
-  constexpr int K = EPT / V;
-  __shared__ float s_sum[2][32][1];
+// A thread's E columns of a row, as they were loaded.  WHOLE: the row has exactly as many
+// columns as its threads hold.  Pieces past the row's end hold zeros from clear() on.
+template <typename T, int V, int E, bool WHOLE>
+struct Held {
+  static constexpr int K = E / V;
+  Pack<T, V> p[K];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < K; ++k) p[k] = Pack<T, V>{};
+  }
+  static __device__ __forceinline__ bool has(int k, const Place& at, int d) {
+    return WHOLE || (k * at.tpr + at.t) * V < d;
+  }
+  __device__ __forceinline__ void load(const T* row, const Place& at, int d) {
+    row += at.t * V;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (has(k, at, d)) p[k].load(row + k * at.tpr * V);
+  }
+  __device__ __forceinline__ void get(f2 (&x)[E / 2]) const {
+    float v[E];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float y[V];
+      p[k].get(y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[k * V + j] = y[j];
+    }
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) x[i] = pair(v[2 * i], v[2 * i + 1]);
+  }
+  static __device__ __forceinline__ void store(T* row, const f2 (&x)[E / 2], const Place& at, int d) {
+    float v[E];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) split(x[i], v[2 * i], v[2 * i + 1]);
+    row += at.t * V;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!has(k, at, d)) continue;
+      float y[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[j] = v[k * V + j];
+      Pack<T, V> o;
+      o.set(y);
+      o.store(row + k * at.tpr * V);
+    }
+  }
+};
+
+// Columns that a thread holds, forward (single elements of 16 bits take a register each).
+template <typename T, int V>
+constexpr int E_NORM = V > 1 ? 64 / (int)sizeof(T) : 16;
+
+// Where shared memory keeps the parameter of column j of piece q, of Q pieces: a lane's
+// accesses of up to 16 bytes lie next to its neighbours'.
+template <int V>
+__device__ __forceinline__ int param_slot(int q, int j, int Q) {
+  constexpr int H = V < 4 ? V : 4;
+  return ((j / H) * Q + q) * H + j % H;
+}
+
+template <typename T, int V, bool WHOLE>
+__global__ void __launch_bounds__(512) k_layer_norm(LayerNormArgs a, Split sp) {
+  constexpr int E = E_NORM<T, V>, K = E / V, P = E / 2, H = V < 4 ? V : 4;
+  extern __shared__ __align__(16) float s_param[];  // gamma, beta: [2][columns held]
+  __shared__ float s_sum[2][MOST_WARPS][1];
   follow();
-  const int tpr = 1 << lg, t = threadIdx.x & (tpr - 1);
-  const int64_t per_pass = (int64_t)gridDim.x * ((int)blockDim.x >> lg);
+  const Place at(sp);
+  const int Q = at.tpr * K;
+  const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
-  float gamma[KEEP ? K : 1][V], beta[KEEP ? K : 1][V];
-  if (KEEP)
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (c < a.d) {
-        params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[k]);
-        params_at<V>(a.beta, a.param_type, c, 0.f, beta[k]);
-      }
-    }
-  Pack<T, V> in[K];
-  auto fetch = [&](int64_t row) {
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (row < a.n && c < a.d) in[k].load(x + c);
-    }
-  };
-  int64_t row = (int64_t)blockIdx.x * ((int)blockDim.x >> lg) + (threadIdx.x >> lg);
-  // all threads of a block go round equally often: they meet in the sums
-  int64_t first = (int64_t)blockIdx.x * ((int)blockDim.x >> lg);
-  fetch(row);
+  const T* x = static_cast<const T*>(a.x);
+  int64_t row = (int64_t)blockIdx.x * at.groups + at.group;
+  int64_t first = (int64_t)blockIdx.x * at.groups + at.warp_group;
+  using Row = Held<T, V, E, WHOLE>;
+  Row in;
+  in.clear();
+  if (row < a.n) in.load(x + row * a.x_stride, at, a.d);
+  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+    const int o = param_slot<V>(c / V, c % V, Q);
+    s_param[o] = param_at(a.gamma, a.param_type, c, 1.f);
+    s_param[Q * V + o] = param_at(a.beta, a.param_type, c, 0.f);
+  }
+  __syncthreads();
   for (; first < a.n; first += per_pass, row += per_pass) {
     const bool live = row < a.n;
-    T* y = static_cast<T*>(a.y) + row * a.y_stride;
-    float v[K][V];
-    float sum[1] = {0.f};
+    f2 v[P];
+    in.get(v);
+    if (row + per_pass < a.n) in.load(x + (row + per_pass) * a.x_stride, at, a.d);
+    f2 acc = v[0];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (live && c < a.d)
-        in[k].get(v[k]);
-      else
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[k][j] = 0.f;
-#pragma unroll
-      for (int j = 0; j < V; ++j) sum[0] += v[k][j];
-    }
-    fetch(row + per_pass);
-    row_sum<1>(sum, lg, s_sum[0]);
+    for (int i = 1; i < P; ++i) acc = add2(acc, v[i]);
+    float sum[1] = {both(acc)};
+    row_sum<1>(sum, sp, at.group, s_sum[0]);
     const float mean = sum[0] * inv_d;
-    sum[0] = 0.f;
+    acc = pair(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = add2(v[i], pair(-mean, -mean));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (c < a.d)
+      if (!Row::has(k, at, a.d)) continue;
+      if constexpr (V > 1) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          v[k][j] -= mean;
-          sum[0] = fmaf(v[k][j], v[k][j], sum[0]);
-        }
+        for (int i = k * V / 2; i < (k + 1) * V / 2; ++i) acc = fma2(v[i], v[i], acc);
+      } else {
+        float lo, hi;
+        split(v[k / 2], lo, hi);
+        const float z = k % 2 ? hi : lo;
+        acc = fma2(pair(z, 0.f), pair(z, 0.f), acc);
+      }
     }
-    row_sum<1>(sum, lg, s_sum[1]);
-    const float rstd = 1.f / sqrtf(sum[0] * inv_d + a.eps);
-    if (live && t == 0) {
+    sum[0] = both(acc);
+    row_sum<1>(sum, sp, at.group, s_sum[1]);
+    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
+    if (live && at.t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
+    if (!live) continue;
+    T* y = static_cast<T*>(a.y) + row * a.y_stride + at.t * V;
+    float z[E];
+#pragma unroll
+    for (int i = 0; i < P; ++i) split(mul2(v[i], pair(rstd, rstd)), z[2 * i], z[2 * i + 1]);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (!live || c >= a.d) continue;
-      float* gk = gamma[KEEP ? k : 0];
-      float* bk = beta[KEEP ? k : 0];
-      if (!KEEP) {
-        params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[0]);
-        params_at<V>(a.beta, a.param_type, c, 0.f, beta[0]);
-      }
+      const int q = k * at.tpr + at.t;
+      if (!Row::has(k, at, a.d)) continue;
+      float o[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[k][j] = fmaf(v[k][j] * rstd, gk[j], bk[j]);
-      Pack<T, V> o;
-      o.set(v[k]);
-      o.store(y + c);
+      for (int h = 0; h < V / H; ++h) {
+        Pack<float, H> g, b;
+        float gj[H], bj[H];
+        g.load(s_param + param_slot<V>(q, h * H, Q));
+        b.load(s_param + Q * V + param_slot<V>(q, h * H, Q));
+        g.get(gj);
+        b.get(bj);
+#pragma unroll
+        for (int j = 0; j < H; ++j) o[h * H + j] = fmaf(z[k * V + h * H + j], gj[j], bj[j]);
+      }
+      Pack<T, V> w;
+      w.set(o);
+      w.store(y + k * at.tpr * V);
     }
   }
 }
 
 // Rows of any width: one block each, read three times.
 template <typename T, int V>
-__global__ void __launch_bounds__(1024) k_layer_norm_wide(LayerNormArgs a) {
+__global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs a) {
   __shared__ float s_sum[2][32][1];
+  const Split sp{32, WIDE_THREADS / 32};
   follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
@@ -179,7 +308,7 @@ __global__ void __launch_bounds__(1024) k_layer_norm_wide(LayerNormArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += v[j];
     }
-    row_sum<1>(sum, 10, s_sum[0]);
+    row_sum<1>(sum, sp, 0, s_sum[0]);
     const float mean = sum[0] * inv_d;
     sum[0] = 0.f;
     for (int64_t c = (int64_t)threadIdx.x * V; c < a.d; c += step) {
@@ -188,8 +317,8 @@ __global__ void __launch_bounds__(1024) k_layer_norm_wide(LayerNormArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] = fmaf(v[j] - mean, v[j] - mean, sum[0]);
     }
-    row_sum<1>(sum, 10, s_sum[1]);
-    const float rstd = 1.f / sqrtf(sum[0] * inv_d + a.eps);
+    row_sum<1>(sum, sp, 0, s_sum[1]);
+    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
@@ -209,138 +338,143 @@ __global__ void __launch_bounds__(1024) k_layer_norm_wide(LayerNormArgs a) {
 }
 
 // Columns that a thread of the gradient holds: as many as leave room for the weights, the two
-// sums, and the loads of this row and the next one.
+// sums, and the loads of this row and (FETCH) the next one.
 template <typename T, int V>
-constexpr int EPT_GRAD = sizeof(T) == 2 && V > 1 ? 16 : 8;
+constexpr int E_GRAD = sizeof(T) == 2 && V > 1 ? 16 : 8;
 
 // One partial row of dgamma and dbeta per block: [2][blocks][d].  What a thread keeps of a row
-// while its sums are formed is its loads; h and g are formed from them twice.  FETCH: the
-// next row's loads are in flight meanwhile.
-template <typename T, int V, bool FETCH>
-__global__ void __launch_bounds__(FETCH ? 512 : 1024) k_layer_norm_grad(LayerNormArgs a, int lg) {
-  constexpr int EPT_ = EPT_GRAD<T, V>, K = EPT_ / V;
-  __shared__ float s_sum[2][32][2];
-  __shared__ float s_part[THREADS * EPT_];
+// while its sums are formed is its loads; h and g are formed from them twice.
+template <typename T, int V, int E, bool FETCH, bool WHOLE>
+__global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split sp) {
+  constexpr int K = E / V, P = E / 2;
+  __shared__ float s_sum[2][MOST_WARPS][2];
+  __shared__ float s_part[THREADS * E];
   follow();
-  const int tpr = 1 << lg, t = threadIdx.x & (tpr - 1);
-  const int per_block = (int)blockDim.x >> lg;
-  const int64_t per_pass = (int64_t)gridDim.x * per_block;
+  const Place at(sp);
+  const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
-  float gamma[K][V], dg[K][V], db[K][V];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = (k * tpr + t) * V;
-    if (c < a.d) params_at<V>(a.gamma, a.param_type, c, 1.f, gamma[k]);
-#pragma unroll
-    for (int j = 0; j < V; ++j) dg[k][j] = db[k][j] = 0.f;
-  }
-  Pack<T, V> xin[K], din[K], xnext[FETCH ? K : 1], dnext[FETCH ? K : 1];
-  float mean = 0.f, rstd = 0.f, mnext = 0.f, rnext = 0.f;
-  auto fetch = [&](int64_t row, Pack<T, V>* xs, Pack<T, V>* ds, float& m, float& r) {
-    if (row >= a.n) return;
-    const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.dy_stride;
+  const f2 zero = pair(0.f, 0.f);
+  f2 gamma[P], dg[P], db[P];
+  {
+    float y[E];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (c < a.d) {
-        xs[k].load(x + c);
-        ds[k].load(dy + c);
-      }
+      float z[V];
+      const int c = (k * at.tpr + at.t) * V;
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = 0.f;
+      if (c < a.d) params_at<V>(a.gamma, a.param_type, c, 1.f, z);
+#pragma unroll
+      for (int j = 0; j < V; ++j) y[k * V + j] = z[j];
     }
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      gamma[i] = pair(y[2 * i], y[2 * i + 1]);
+      dg[i] = db[i] = zero;
+    }
+  }
+  using Row = Held<T, V, E, WHOLE>;
+  using Next = Held<T, V, FETCH ? E : V, WHOLE>;
+  Row xin, din;
+  Next xnext, dnext;
+  xin.clear();
+  din.clear();
+  xnext.clear();
+  dnext.clear();
+  float mean = 0.f, rstd = 0.f, mnext = 0.f, rnext = 0.f;
+  auto fetch = [&](int64_t row, auto& xs, auto& ds, float& m, float& r) {
+    if (row >= a.n) {  // adds nothing
+      xs.clear();
+      ds.clear();
+      m = r = 0.f;
+      return;
+    }
+    xs.load(static_cast<const T*>(a.x) + row * a.x_stride, at, a.d);
+    ds.load(static_cast<const T*>(a.dy) + row * a.dy_stride, at, a.d);
     m = a.mean[row];
     r = a.rstd[row];
   };
-  int64_t first = (int64_t)blockIdx.x * per_block;
-  int64_t row = first + ((int)threadIdx.x >> lg);
+  int64_t row = (int64_t)blockIdx.x * at.groups + at.group;
+  int64_t first = (int64_t)blockIdx.x * at.groups + at.warp_group;
   if (FETCH) fetch(row, xnext, dnext, mnext, rnext);
   int flip = 0;
   for (; first < a.n; first += per_pass, row += per_pass) {
-    const bool live = row < a.n;
     if constexpr (FETCH) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        xin[k] = xnext[k];
-        din[k] = dnext[k];
-      }
+      xin = xnext;
+      din = dnext;
       mean = mnext;
       rstd = rnext;
       fetch(row + per_pass, xnext, dnext, mnext, rnext);
     } else {
       fetch(row, xin, din, mean, rstd);
     }
-    float sum[2] = {0.f, 0.f};
+    const f2 m = pair(-mean, -mean), r = pair(rstd, rstd);
+    f2 s0 = zero, s1 = zero;
+    {
+      f2 x[P], g[P];
+      xin.get(x);
+      din.get(g);  // 0 past the row's end, and so are its products
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (!live || c >= a.d) continue;
-      float x[V], g[V];
-      xin[k].get(x);
-      din[k].get(g);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float h = (x[j] - mean) * rstd;
-        db[k][j] += g[j];
-        dg[k][j] = fmaf(g[j], h, dg[k][j]);
-        g[j] *= gamma[k][j];
-        sum[0] += g[j];
-        sum[1] = fmaf(g[j], h, sum[1]);
+      for (int i = 0; i < P; ++i) {
+        const f2 h = mul2(add2(x[i], m), r);
+        db[i] = add2(db[i], g[i]);
+        dg[i] = fma2(g[i], h, dg[i]);
+        g[i] = mul2(g[i], gamma[i]);
+        s0 = add2(s0, g[i]);
+        s1 = fma2(g[i], h, s1);
       }
     }
-    row_sum<2>(sum, lg, s_sum[flip]);
+    float sum[2] = {both(s0), both(s1)};
+    row_sum<2>(sum, sp, at.group, s_sum[flip]);
     flip ^= 1;
     const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
-    T* dx = static_cast<T*>(a.y) + row * a.y_stride;
+    const f2 nmg = pair(-mg, -mg), nmgh = pair(-mgh, -mgh);
+    f2 x[P], g[P];
+    if (row >= a.n) continue;
+    xin.get(x);
+    din.get(g);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
-      if (!live || c >= a.d) continue;
-      float x[V], g[V];
-      xin[k].get(x);
-      din[k].get(g);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float h = (x[j] - mean) * rstd;
-        g[j] = rstd * (g[j] * gamma[k][j] - mg - h * mgh);
-      }
-      Pack<T, V> o;
-      o.set(g);
-      o.store(dx + c);
+    for (int i = 0; i < P; ++i) {
+      const f2 h = mul2(add2(x[i], m), r);
+      g[i] = mul2(r, fma2(h, nmgh, fma2(g[i], gamma[i], nmg)));
     }
+    Row::store(static_cast<T*>(a.y) + row * a.y_stride, g, at, a.d);
   }
   // the block's groups of threads, in order: first those within a warp, then through shared memory
+  float mine[2][E];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+  for (int i = 0; i < P; ++i) {
+    split(dg[i], mine[0][2 * i], mine[0][2 * i + 1]);
+    split(db[i], mine[1][2 * i], mine[1][2 * i + 1]);
+  }
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      for (int o = tpr; o < 32; o <<= 1) {
-        dg[k][j] += __shfl_xor_sync(FULL, dg[k][j], o);
-        db[k][j] += __shfl_xor_sync(FULL, db[k][j], o);
-      }
-  const int lgw = lg < 5 ? 5 : lg;
-  const int groups = (int)blockDim.x >> lgw, group = (int)threadIdx.x >> lgw, width = tpr * EPT_;
-  const bool one_of = lg >= 5 || (threadIdx.x & 31) < tpr;
+  for (int which = 0; which < 2; ++which)
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      for (int o = sp.L; o < 32; o <<= 1) mine[which][e] += __shfl_xor_sync(FULL, mine[which][e], o);
+  const int sets = sp.W == 1 ? (int)blockDim.x >> 5 : at.groups;
+  const int set = sp.W == 1 ? (int)threadIdx.x >> 5 : at.group, width = at.tpr * E;
+  const bool one_of = (int)(threadIdx.x & 31) < sp.L;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float* out = a.parts + ((int64_t)which * gridDim.x + blockIdx.x) * a.d;
-    float(*mine)[V] = which == 0 ? dg : db;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * tpr + t) * V;
+      const int c = (k * at.tpr + at.t) * V;
       if (!one_of || c >= a.d) continue;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        if (groups == 1)
-          out[c + j] = mine[k][j];
+        if (sets == 1)
+          out[c + j] = mine[which][k * V + j];
         else
-          s_part[group * width + c + j] = mine[k][j];
+          s_part[set * width + c + j] = mine[which][k * V + j];
       }
     }
-    if (groups == 1) continue;
+    if (sets == 1) continue;
     __syncthreads();
     for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
       float x = 0.f;
-      for (int g = 0; g < groups; ++g) x += s_part[g * width + c];
+      for (int g = 0; g < sets; ++g) x += s_part[g * width + c];
       out[c] = x;
     }
     __syncthreads();
@@ -349,8 +483,9 @@ __global__ void __launch_bounds__(FETCH ? 512 : 1024) k_layer_norm_grad(LayerNor
 
 // Rows of any width: dx by one block a row, read twice.
 template <typename T, int V>
-__global__ void __launch_bounds__(512) k_layer_norm_grad_wide(LayerNormArgs a) {
-  __shared__ float s_sum[2][16][2];
+__global__ void __launch_bounds__(WIDE_GRAD_THREADS) k_layer_norm_grad_wide(LayerNormArgs a) {
+  __shared__ float s_sum[2][WIDE_GRAD_THREADS / 32][2];
+  const Split sp{32, WIDE_GRAD_THREADS / 32};
   follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
@@ -376,7 +511,7 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad_wide(LayerNormArgs a) {
         sum[1] = fmaf(gj, (h[j] - mean) * rstd, sum[1]);
       }
     }
-    row_sum<2>(sum, 9, s_sum[flip]);
+    row_sum<2>(sum, sp, 0, s_sum[flip]);
     flip ^= 1;
     const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
     for (int64_t c = (int64_t)threadIdx.x * V; c < a.d; c += step) {
@@ -452,75 +587,113 @@ __global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int
   }
 }
 
-int lg_of(int32_t d, int ept) {
-  int lg = 0;
-  while (((int64_t)ept << lg) < d) ++lg;
-  return lg;
+// ---- launches ------------------------------------------------------------------------
+
+constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns
+
+// The threads of a row of d columns, E to a thread, and of a block of such rows.
+Split split_of(int32_t d, int E, int* threads) {
+  const int need = (d + E - 1) / E;
+  Split s{1, 1};
+  while (s.L < need && s.L < 32) s.L <<= 1;
+  if (need > 32) s.W = (need + 31) / 32;
+  *threads = s.W == 1 ? THREADS : 32 * s.W * std::max(1, THREADS / (32 * s.W));
+  return s;
 }
 
-// Blocks of the register kernels, and threads of each.
-struct Shape {
-  unsigned grid, threads;
+// Blocks of a kernel that an SM holds, for each number of warps of a row (a row's warps give
+// the block's size).
+struct Residency {
+  int blocks[MOST_WARPS + 1];
+  template <typename F, typename S>
+  Residency(F* kernel, int E, S smem_of) {
+    for (int w = 1; w <= MOST_WARPS; ++w) {
+      int threads;
+      split_of(w * 32 * E, E, &threads);
+      const size_t smem = smem_of(w);
+      blocks[w] = 0;
+      if (smem > 48 * 1024)
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+      if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks[w], kernel, threads, smem) != cudaSuccess ||
+          blocks[w] < 1)
+        blocks[w] = 1;
+    }
+  }
 };
-Shape shape_of(int64_t n, int lg, int num_sms, int threads_per_sm) {
-  const unsigned threads = std::max(THREADS, 1 << lg);
-  const int64_t blocks = (n + (threads >> lg) - 1) / (threads >> lg);
-  return Shape{(unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * (threads_per_sm / (int)threads)), threads};
+
+unsigned grid_of(int64_t n, const Split& s, int threads, int num_sms, int per_sm) {
+  const int64_t rows = threads / (s.L * s.W);  // a block's
+  return (unsigned)std::min<int64_t>((n + rows - 1) / rows, (int64_t)num_sms * per_sm);
 }
-// Threads of a kernel that an SM holds, in blocks of so many.
-template <typename F>
-int threads_per_sm(F* kernel, int threads) {
-  int blocks = 0;
-  if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, threads, 0) != cudaSuccess || blocks < 1)
-    blocks = 1;
-  return blocks * threads;
+
+template <typename T, int V, bool WHOLE>
+cudaError_t norm_rows(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int E = E_NORM<T, V>;
+  auto smem_of = [](int w) { return (size_t)w * 32 * E * 2 * sizeof(float); };
+  static const Residency held(k_layer_norm<T, V, WHOLE>, E, smem_of);
+  int threads;
+  const Split sp = split_of(a.d, E, &threads);
+  return launch_following(k_layer_norm<T, V, WHOLE>,
+                          dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s,
+                          a, sp);
 }
-constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns
+
+// Does every thread that holds a row of d columns hold E of them?  (Asked where it saves
+// instructions: in rows read by vectors of 16 bytes.)
+template <typename T, int V, int E>
+bool is_whole(int32_t d) {
+  int threads;
+  const Split sp = split_of(d, E, &threads);
+  return V * sizeof(T) == 16 && sp.L * sp.W * E == d;
+}
 
 template <typename T, int V>
 cudaError_t norm_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  const int lg = lg_of(a.d, EPT);
-  if (lg > MOST_LG)
-    return launch_following(k_layer_norm_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 2)), 1024,
-                            0, s, a);
-  if (lg == MOST_LG) {
-    const Shape sh = shape_of(a.n, lg, num_sms, 1024);
-    return launch_following(k_layer_norm<T, V, false>, dim3(sh.grid), sh.threads, 0, s, a, lg);
-  }
-  static const int held[2] = {threads_per_sm(k_layer_norm<T, V, true>, THREADS),
-                              threads_per_sm(k_layer_norm<T, V, true>, 2 * THREADS)};
-  const Shape sh = shape_of(a.n, lg, num_sms, held[lg == 9]);
-  return launch_following(k_layer_norm<T, V, true>, dim3(sh.grid), sh.threads, 0, s, a, lg);
+  constexpr int E = E_NORM<T, V>;
+  if (a.d > MOST_WARPS * 32 * E)
+    return launch_following(k_layer_norm_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 2)),
+                            WIDE_THREADS, 0, s, a);
+  if constexpr (V * sizeof(T) == 16)
+    if (is_whole<T, V, E>(a.d)) return norm_rows<T, V, true>(a, num_sms, s);
+  return norm_rows<T, V, false>(a, num_sms, s);
 }
 
-// The kernel of a gradient: rows of up to 8,192 columns stay in registers.
+// How a gradient's rows are held: with the next row's loads in flight, without (float32 rows of
+// up to 8,192 columns), or not at all.
 enum class Way { FETCH, PLAIN, WIDE };
 struct GradShape {
   Way way;
-  int lg;
-  Shape shape;
-  int parts;  // partial rows
+  bool whole;
+  Split split;
+  int threads;
+  int parts;  // blocks, and partial rows
 };
 
 template <typename T, int V>
 GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
+  constexpr int E = E_GRAD<T, V>;
   GradShape g{};
-  g.lg = lg_of(a.d, EPT_GRAD<T, V>);
-  if (a.d > 8192) {
+  auto none = [](int) { return (size_t)0; };
+  if (a.d <= MOST_WARPS * 32 * E) {
+    static const Residency held(k_layer_norm_grad<T, V, E, true, false>, E, none);
+    g.way = Way::FETCH;
+    g.whole = is_whole<T, V, E>(a.d);
+    g.split = split_of(a.d, E, &g.threads);
+    g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held.blocks[g.split.W]);
+  } else if (E < 16 && a.d <= MOST_WARPS * 32 * 16) {
+    g.way = Way::PLAIN;
+    g.split = split_of(a.d, 16, &g.threads);
+    g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, 1);
+  } else {
     g.way = Way::WIDE;
     g.parts = (int)std::min(a.n, WIDE_SPLIT);
-    return g;
   }
-  g.way = g.lg <= 9 ? Way::FETCH : Way::PLAIN;
-  static const int held[2] = {threads_per_sm(k_layer_norm_grad<T, V, true>, THREADS),
-                              threads_per_sm(k_layer_norm_grad<T, V, true>, 2 * THREADS)};
-  g.shape = shape_of(a.n, g.lg, num_sms, g.way == Way::PLAIN ? 1024 : held[g.lg == 9]);
-  g.parts = (int)g.shape.grid;
   return g;
 }
 
 template <typename T, int V>
 cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
+  constexpr int E = E_GRAD<T, V>;
   const GradShape g = grad_shape<T, V>(a, num_sms);
   cudaError_t e;
   if (g.way == Way::WIDE) {
@@ -529,12 +702,14 @@ cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
                          THREADS, 0, s, a);
     if (e == cudaSuccess)
       e = launch_following(k_layer_norm_grad_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 4)),
-                           512, 0, s, a);
+                           WIDE_GRAD_THREADS, 0, s, a);
   } else {
-    auto kernel = k_layer_norm_grad<T, V, true>;
-    if constexpr (EPT_GRAD<T, V> == 8)  // the others hold 8,192 columns in 512 threads
-      if (g.way == Way::PLAIN) kernel = k_layer_norm_grad<T, V, false>;
-    e = launch_following(kernel, dim3(g.shape.grid), g.shape.threads, 0, s, a, g.lg);
+    auto kernel = k_layer_norm_grad<T, V, E, true, false>;
+    if constexpr (V * sizeof(T) == 16)
+      if (g.whole) kernel = k_layer_norm_grad<T, V, E, true, true>;
+    if constexpr (E < 16)
+      if (g.way == Way::PLAIN) kernel = k_layer_norm_grad<T, V, 16, false, false>;
+    e = launch_following(kernel, dim3(g.parts), g.threads, 0, s, a, g.split);
   }
   if (e != cudaSuccess || (!a.dgamma && !a.dbeta)) return e;
   return launch_following(k_layer_norm_params, dim3((unsigned)((a.d + 31) / 32), 2), 1024, 0, s, a, g.parts);
