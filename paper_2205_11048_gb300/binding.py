@@ -521,12 +521,17 @@ def _refuse(why):
     raise GBAError(GBA_E_ARG, why)
 
 
+_types = {}  # torch dtype -> gba_dtype
+
+
 def _type_of(t):
-    import torch
-    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    if t.dtype not in types:
+    if not _types:
+        import torch
+        _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    try:
+        return _types[t.dtype]
+    except KeyError:
         _refuse(f"tensors are float32, bfloat16 or float16, not {t.dtype}")
-    return types[t.dtype]
 
 
 def _on_gpu(*tensors):
@@ -537,11 +542,12 @@ def _on_gpu(*tensors):
 
 def _matrix(t):
     """t as a gba_matrix: two dimensions, rows of consecutive elements."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
         _refuse("a matrix has two dimensions, and rows of consecutive elements")
-    rows, cols = t.shape
-    stride = t.stride(0) if rows > 1 else max(cols, 1)
-    return gba_matrix(t.data_ptr() if rows else None, rows, stride, cols, _type_of(t))
+    rows, cols = shape
+    return gba_matrix(t.data_ptr() if rows else None, rows, strides[0] if rows > 1 else max(cols, 1), cols,
+                      _type_of(t))
 
 
 def _rows_of(t):
@@ -549,7 +555,8 @@ def _rows_of(t):
     their elements not consecutive (an expanded tensor, a transposed one)."""
     if t.dim() != 2:
         t = t.reshape(t.numel() // max(1, t.shape[-1]), t.shape[-1])
-    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    (rows, cols), strides = t.shape, t.stride()
+    if (cols > 1 and strides[1] != 1) or (rows > 1 and strides[0] < cols):
         t = t.contiguous()
     return t
 
@@ -597,8 +604,11 @@ class Worker:
         self.L = load()
         self.h = None
         self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self._raw_stream = self.stream.cuda_stream
+        self._index = torch.cuda.current_device()
+        self._device = torch.device("cuda", self._index)
         h = _P()
-        check(self.L.gba_worker_create(self.stream.cuda_stream, ctypes.byref(h)), what="gba_worker_create")
+        check(self.L.gba_worker_create(self._raw_stream, ctypes.byref(h)), what="gba_worker_create")
         self.h = h
 
     def close(self):
@@ -613,14 +623,19 @@ class Worker:
             pass
 
     def _call(self, name, *args):
-        now = self.torch.cuda.current_stream()
-        apart = now != self.stream
-        if apart:
+        call = getattr(self.L, name)
+        if self.torch._C._cuda_getCurrentRawStream(self._index) == self._raw_stream:
+            status = call(self.h, *args)
+        else:
+            now = self.torch.cuda.current_stream(self._device)
             self.stream.wait_stream(now)
-        status = getattr(self.L, name)(self.h, *args)
-        if apart:
+            status = call(self.h, *args)
             now.wait_stream(self.stream)
-        self._check(status, name)
+        if status < 0:
+            self._check(status, name)
+
+    def _new(self, *shape, dtype=None):
+        return self.torch.empty(shape, dtype=dtype or self.torch.float32, device=self._device)
 
     def _check(self, status, name):
         if status < 0:
@@ -638,7 +653,7 @@ class Worker:
 
     def _embed_out(self, ids, d, dtype, out):
         if out is None:
-            out = self.torch.empty(*ids.shape, d, dtype=dtype, device=ids.device)
+            out = self._new(*ids.shape, d, dtype=dtype)
         _on_gpu(out)
         flat = out if out.dim() == 2 else out.view(ids.numel(), d)
         return out, _matrix(flat)
@@ -670,9 +685,9 @@ class Worker:
         ids, grad = self._ids(ids), _rows_of(grad)
         _on_gpu(grad)
         n, d = ids.numel(), grad.shape[1]
-        ids_out = torch.empty(n, dtype=torch.int64, device=ids.device)
-        rows_out = torch.empty(n, d, dtype=torch.float32, device=ids.device)
-        count = torch.empty((), dtype=torch.int64, device=ids.device)
+        ids_out = self._new(n, dtype=torch.int64)
+        rows_out = self._new(n, d)
+        count = self._new(dtype=torch.int64)
         self._call("gba_embed_grad", ids.data_ptr(), n, _matrix(grad), rows, id_mode, scale,
                    NO_PAD if pad_id is None else pad_id, ids_out.data_ptr(), rows_out.data_ptr(),
                    count.data_ptr())
@@ -689,7 +704,7 @@ class Worker:
     def grad_norm(self, grads):
         """The 2-norm of all the tensors together (a list, or grad_parts of it), on the device."""
         p = grads if isinstance(grads, GradParts) else GradParts(grads)
-        norm = self.torch.empty((), dtype=self.torch.float32, device="cuda")
+        norm = self._new()
         self._call("gba_grad_norm", p.array, p.n, norm.data_ptr())
         return norm
 
@@ -697,33 +712,36 @@ class Worker:
         """Scales the tensors (a list, or grad_parts of it) by min(1, max_norm / (norm + 1e-6)),
         in place or into the parts' outputs; returns the norm."""
         p = grads if isinstance(grads, GradParts) else GradParts(grads)
-        norm = self.torch.empty((), dtype=self.torch.float32, device="cuda")
+        norm = self._new()
         self._call("gba_clip_grads", p.array, p.n, max_norm, norm.data_ptr())
         return norm
 
     def _params(self, d, *params):
-        types = {_type_of(p) for p in params if p is not None}
-        if len(types) > 1:
-            _refuse("the parameters of a layer norm have one type")
-        _on_gpu(*params)
+        at, kind = [], None
         for p in params:
-            if p is not None and (p.numel() != d or not p.is_contiguous()):
+            if p is None:
+                at.append(None)
+                continue
+            _on_gpu(p)
+            if p.numel() != d or not p.is_contiguous():
                 _refuse("a parameter has a value per column")
-        return [None if p is None else p.data_ptr() for p in params], types.pop() if types else F32
+            if kind is not None and kind != _type_of(p):
+                _refuse("the parameters of a layer norm have one type")
+            kind = _type_of(p)
+            at.append(p.data_ptr())
+        return at, F32 if kind is None else kind
 
     def layer_norm(self, x, gamma=None, beta=None, eps=1e-5):
         """(y, mean, rstd) of the rows of x (its last dimension)."""
-        torch = self.torch
         _on_gpu(x)
         rows = _rows_of(x)
         n, d = rows.shape
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean = torch.empty(n, dtype=torch.float32, device=x.device)
-        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+        y = self._new(n, d, dtype=x.dtype)
+        mean, rstd = self._new(n), self._new(n)
         (pg, pb), ptype = self._params(d, gamma, beta)
-        self._call("gba_layer_norm", _matrix(rows), pg, pb, ptype, eps, _matrix(y.view(n, d)),
-                   mean.data_ptr(), rstd.data_ptr())
-        return y, mean, rstd
+        self._call("gba_layer_norm", _matrix(rows), pg, pb, ptype, eps, _matrix(y), mean.data_ptr(),
+                   rstd.data_ptr())
+        return y if x.dim() == 2 else y.view(x.shape), mean, rstd
 
     def layer_norm_grad(self, dy, x, gamma, mean, rstd):
         """(dx, dgamma, dbeta) from the gradient of layer_norm's y and its mean and rstd."""
@@ -734,10 +752,9 @@ class Worker:
         if mean.numel() != n or rstd.numel() != n or {mean.dtype, rstd.dtype} != {torch.float32}:
             _refuse("mean and rstd are float32, one for each row")
         mean, rstd = mean.contiguous(), rstd.contiguous()
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dgamma = torch.empty(d, dtype=torch.float32, device=x.device)
-        dbeta = torch.empty(d, dtype=torch.float32, device=x.device)
+        dx = self._new(n, d, dtype=x.dtype)
+        dgamma, dbeta = self._new(d), self._new(d)
         (pg,), ptype = self._params(d, gamma)
         self._call("gba_layer_norm_grad", _matrix(dr), _matrix(xr), pg, ptype, mean.data_ptr(),
-                   rstd.data_ptr(), _matrix(dx.view(n, d)), dgamma.data_ptr(), dbeta.data_ptr())
-        return dx, dgamma, dbeta
+                   rstd.data_ptr(), _matrix(dx), dgamma.data_ptr(), dbeta.data_ptr())
+        return dx if x.dim() == 2 else dx.view(x.shape), dgamma, dbeta

@@ -20,7 +20,7 @@ namespace gba {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int NORM_BLOCKS = 8;  // per SM, at most
+constexpr int NORM_BLOCKS = 5, CLIP_BLOCKS = 4;  // that an SM holds
 
 struct Part {
   const void* grad;
@@ -148,7 +148,7 @@ __device__ __forceinline__ double block_sum(double x) {
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, NORM_BLOCKS)
     k_grad_norm(const __grid_constant__ PartList<CAP> l, NormOut o) {
   __shared__ bool s_last;
   follow();
@@ -185,9 +185,13 @@ __global__ void __launch_bounds__(THREADS)
   }
 }
 
+// A warp's vectors leave in the order of the outputs.  Where an output does not start on the
+// boundary that its vectors need (a tensor packed behind others of odd sizes), the lanes'
+// values change places through shared memory, so that neighbouring lanes still store
+// neighbouring elements.
 template <typename T, typename TO>
-__device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, float c) {
-  constexpr int V = Layout<T>::V;
+__device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, float c, float* swap) {
+  constexpr int V = Layout<T>::V, U = 4;
   const Layout<T> lay(p);
   const T* g = static_cast<const T*>(p.grad);
   TO* out = static_cast<TO*>(p.out);
@@ -197,7 +201,10 @@ __device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, 
   const bool aligned = (uintptr_t)ov % A == 0;
   const int64_t per = unit / V, lo = (int64_t)k * per;
   const int64_t hi = lo + per < lay.vecs ? lo + per : lay.vecs;
-  auto scaled = [&](const Pack<T, V>& w, int64_t i) {
+  const int lane = threadIdx.x & 31;
+  float* mine = swap + (threadIdx.x >> 5) * (32 * V);  // the warp's
+  // first: the warp's first vector, of which `count` are left
+  auto scaled = [&](const Pack<T, V>& w, int64_t first, int count) {
     float x[V];
     w.get(x);
 #pragma unroll
@@ -205,25 +212,33 @@ __device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, 
     if (aligned) {
       Pack<TO, V> y;
       y.set(x);
-      y.store(ov + i * V);
+      if (lane < count) y.store(ov + (first + lane) * V);
     } else {
+      __syncwarp();
 #pragma unroll
-      for (int j = 0; j < V; ++j) ov[i * V + j] = from_float<TO>(x[j]);
+      for (int j = 0; j < V; j += 4)
+        *reinterpret_cast<float4*>(mine + lane * V + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int e = j * 32 + lane;
+        if (e < count * V) ov[first * V + e] = from_float<TO>(mine[e]);
+      }
     }
   };
-  constexpr int U = 4;
-  int64_t i = lo + threadIdx.x;
-  for (; i + (U - 1) * THREADS < hi; i += U * THREADS) {
+  int64_t first = lo + (threadIdx.x & ~31u);  // a warp's lanes go round together
+  for (; first + (U - 1) * THREADS + 32 <= hi; first += U * THREADS) {
     Pack<T, V> w[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u].load(gv + (i + u * THREADS) * V);
+    for (int u = 0; u < U; ++u) w[u].load(gv + (first + u * THREADS + lane) * V);
 #pragma unroll
-    for (int u = 0; u < U; ++u) scaled(w[u], i + u * THREADS);
+    for (int u = 0; u < U; ++u) scaled(w[u], first + u * THREADS, 32);
   }
-  for (; i < hi; i += THREADS) {
-    Pack<T, V> w;
-    w.load(gv + i * V);
-    scaled(w, i);
+  for (; first < hi; first += THREADS) {
+    const int count = hi - first < 32 ? (int)(hi - first) : 32;
+    Pack<T, V> w{};
+    if (lane < count) w.load(gv + (first + lane) * V);
+    scaled(w, first, count);
   }
   if (k == 0 && (int)threadIdx.x < lay.singles(p.n)) {
     const int64_t e = lay.single(threadIdx.x);
@@ -232,18 +247,19 @@ __device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, 
 }
 
 template <typename T>
-__device__ __forceinline__ void clip_out(const Part& p, uint32_t k, int unit, float c) {
+__device__ __forceinline__ void clip_out(const Part& p, uint32_t k, int unit, float c, float* swap) {
   if (p.out_type == GBA_F32)
-    clip_piece<T, float>(p, k, unit, c);
+    clip_piece<T, float>(p, k, unit, c, swap);
   else if (p.out_type == GBA_BF16)
-    clip_piece<T, bf16>(p, k, unit, c);
+    clip_piece<T, bf16>(p, k, unit, c, swap);
   else
-    clip_piece<T, f16>(p, k, unit, c);
+    clip_piece<T, f16>(p, k, unit, c, swap);
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, CLIP_BLOCKS)
     k_grad_clip(const __grid_constant__ PartList<CAP> l, const float* coef) {
+  __shared__ __align__(16) float swap[THREADS * 8];
   follow();
   const float c = *(const volatile float*)coef;
   for (uint32_t b = blockIdx.x; b < l.pieces; b += gridDim.x) {
@@ -252,11 +268,11 @@ __global__ void __launch_bounds__(THREADS)
     if (p.out == p.grad && c == 1.f) continue;
     const uint32_t k = piece - p.first;
     if (p.type == GBA_F32)
-      clip_out<float>(p, k, l.unit, c);
+      clip_out<float>(p, k, l.unit, c, swap);
     else if (p.type == GBA_BF16)
-      clip_out<bf16>(p, k, l.unit, c);
+      clip_out<bf16>(p, k, l.unit, c, swap);
     else
-      clip_out<f16>(p, k, l.unit, c);
+      clip_out<f16>(p, k, l.unit, c, swap);
   }
 }
 
@@ -297,7 +313,7 @@ cudaError_t run_as(const gba_grad_part* parts, int32_t n_parts, bool clip, int u
   for (int32_t at = (n_parts - 1) / CAP * CAP; at >= 0 && n_parts > 0; at -= CAP) {
     const PartList<CAP> l = list_of<CAP>(parts + at, std::min(CAP, n_parts - at), unit);
     if (l.pieces == 0) continue;
-    const unsigned grid = std::min(l.pieces, (unsigned)(num_sms * NORM_BLOCKS));
+    const unsigned grid = std::min(l.pieces, (unsigned)(num_sms * CLIP_BLOCKS));
     const cudaError_t e = launch_following(k_grad_clip<CAP>, dim3(grid), THREADS, 0, s, l, (const float*)o.coef);
     if (e != cudaSuccess) return e;
   }
@@ -306,6 +322,8 @@ cudaError_t run_as(const gba_grad_part* parts, int32_t n_parts, bool clip, int u
 
 }  // namespace
 
+constexpr int MOST_UNIT = 8192;
+
 size_t norm_workspace(int64_t n_parts, int num_sms) {
   const size_t launches = (size_t)(n_parts / CAP_MOST + 1);
   return 256 + launches * (size_t)(num_sms * NORM_BLOCKS) * sizeof(double);
@@ -313,11 +331,11 @@ size_t norm_workspace(int64_t n_parts, int num_sms) {
 
 cudaError_t launch_norm(const gba_grad_part* parts, int32_t n_parts, bool clip, float max_norm,
                         float* norm, char* ws, uint32_t* ticket, int num_sms, cudaStream_t s) {
-  // pieces that give every SM some, of 2,048 to 32,768 elements
+  // pieces that give every block several, of 2,048 to 8,192 elements
   uint64_t total = 0;
   for (int32_t i = 0; i < n_parts; ++i) total += (uint64_t)parts[i].n;
   int unit = 2048;
-  while (unit < 32768 && total / (uint64_t)unit > (uint64_t)num_sms * 16) unit *= 2;
+  while (unit < MOST_UNIT && total / (uint64_t)unit > (uint64_t)num_sms * 16) unit *= 2;
   // and no more of them than 2^31
   const uint64_t most = (total / (uint64_t)unit) + (uint64_t)n_parts;
   if (most >= (1ull << 31)) return cudaErrorInvalidValue;
@@ -328,7 +346,7 @@ cudaError_t launch_norm(const gba_grad_part* parts, int32_t n_parts, bool clip, 
   o.coef = reinterpret_cast<float*>(ws);
   o.max_norm = max_norm;
   if (n_parts <= 16) return run_as<16>(parts, n_parts, clip, unit, o, num_sms, s);
-  if (n_parts <= 120) return run_as<120>(parts, n_parts, clip, unit, o, num_sms, s);
+  if (n_parts <= 240) return run_as<240>(parts, n_parts, clip, unit, o, num_sms, s);
   return run_as<CAP_MOST>(parts, n_parts, clip, unit, o, num_sms, s);
 }
 
