@@ -8,14 +8,20 @@
 // ids are sorted with their positions as payload (the step's onesweep passes; stable, so
 // a row's positions stay ascending and its sum has one order), and then each gradient row
 // is read once, where it lies:
-//  - items: a run of equal rows is cut at the sorted positions p = 0 mod CUT whose row
-//    stood at p - CUT too, so runs shorter than CUT stay whole and no item is longer than
-//    2 CUT - 1 positions;
+//  - items: a run of equal rows is cut at the sorted positions p = 0 mod c whose row stood
+//    at p - c too, so runs shorter than c stay whole and no item is longer than 2 c - 1
+//    positions;
 //  - sums: one lane group per item and column slab adds the item's gradient rows; a run of
 //    one item goes straight to the output, the others leave float32 sums of their items
-//    (in slots that follow from the cut's position: 2 p / CUT for the item before the first
-//    cut p, one more for the item that starts at p);
-//  - merge: one block per cut run and slab adds the items' sums in their order.
+//    (in slots that follow from the cut's position: 2 p / c for the item before the first
+//    cut p, one more for the item that starts at p).  Rows of a dense output that do not
+//    occur are cleared by the same kernel, so that every row is written once;
+//  - merge: a warp per cut run and slab, or a block where the run has many items, adds the
+//    items' sums in their order.
+// The items of a hot row follow one another through a lane group, so their length bounds
+// the time of small calls, and their sums' traffic that of large ones: c is 16 for up to
+// 65,536 positions (a message of 6,656 x 16 floats, kernel of the sums: 24.7 us with 64) and
+// 64 above.
 #include <algorithm>
 
 #include "gba_worker.cuh"
@@ -26,7 +32,10 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int CUT = 64;
+constexpr int SUM_BLOCKS = 4, MERGE_BLOCKS = 3;  // of k_token_sums and k_token_merge, that an SM holds
+constexpr uint32_t LONG_PARTS = 16;
+constexpr int MIN_CUT_LG = 4, MAX_CUT_LG = 6;
+inline int cut_lg_of(int64_t n) { return n <= 65536 ? MIN_CUT_LG : MAX_CUT_LG; }
 constexpr int ITEM_TILE = 2048;  // sorted positions per tile of the item scan
 constexpr int MAX_RADIX = 512;   // of a sort pass
 
@@ -149,9 +158,11 @@ struct Counters {
   uint32_t step;     // the call's error word
   uint32_t tickets[MAX_PASSES];
   uint32_t scan_ticket;
-  uint32_t n_items, n_runs, n_cut;
+  uint32_t n_items, n_runs;
+  uint32_t n_cut[2];  // cut runs of a few items, and of more than LONG_PARTS
   uint32_t P;        // positions that are no padding: the first P of the sorted ones
-  uint32_t pad[6];
+  uint32_t rest;     // claims of the rows that are cleared
+  uint32_t pad[4];
 };
 static_assert(sizeof(Counters) == 64, "the histograms follow it");
 
@@ -163,9 +174,10 @@ struct Item {
 // Where the parts of the workspace are; what must start at zero comes first.
 struct GradPlan {
   SortPlan sort;
-  size_t counters, hist, sort_status, scan_status, cleared;  // cleared: bytes from 0 on
+  size_t counters, hist, sort_status, scan_status, present, cleared;  // cleared: bytes from 0 on
   size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, bytes;
   int64_t tiles;
+  int cut_lg;
 };
 
 GradPlan plan_of(const EmbedGradArgs& a) {
@@ -175,6 +187,7 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   while (bits < 32 && (top >> bits) != 0) ++bits;
   p.sort = make_sort_plan(bits, 9);
   p.tiles = (a.n + ITEM_TILE - 1) / ITEM_TILE;
+  p.cut_lg = cut_lg_of(a.n);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -186,6 +199,7 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.hist = take((size_t)MAX_PASSES * MAX_RADIX * 4);
   p.sort_status = take(sort_status_words(a.n, p.sort.radix) * 8);
   p.scan_status = take((size_t)p.tiles * 8);
+  p.present = take(a.dense && !a.accumulate ? ((size_t)a.V + 31) / 32 * 4 : 0);
   p.cleared = at;
   for (int i = 0; i < 2; ++i) {
     p.keys[i] = take(n * 4);
@@ -194,8 +208,8 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.items = take(n * sizeof(Item));
   p.run_row = take(n * 4);
   p.run_start = take(n * 4);
-  p.cuts = take((n / CUT + 1) * 8);
-  p.parts = take((2 * (n / CUT) + 2) * (size_t)a.d * 4);
+  p.cuts = take(2 * ((n >> p.cut_lg) + 1) * 8);
+  p.parts = take((2 * (n >> p.cut_lg) + 2) * (size_t)a.d * 4);
   p.bytes = at;
   return p;
 }
@@ -262,8 +276,10 @@ struct ItemArgs {
   Item* items;
   uint32_t* run_row;
   uint32_t* run_start;
-  uint2* cuts;       // (run, first cut)
+  uint2* cuts;       // (run, first cut): [2][n >> cut_lg + 1]
   int64_t* ids_out;  // message form
+  uint32_t* present; // dense form, overwriting: a bit per row that occurs
+  int32_t cut_lg;
 };
 
 // Look-back word: [61:60] flag, [59:30] items, [29:0] runs.
@@ -289,23 +305,37 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
   const uint32_t tile = s_tile;
   const uint32_t base = tile * (uint32_t)ITEM_TILE + (uint32_t)(warp * PER_WARP);
 
-  uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS];
+  const uint32_t cut = 1u << a.cut_lg;
+  uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS], several[ROUNDS], firsts[ROUNDS], longs[ROUNDS];
   unsigned long long sum = 0ull;
 #pragma unroll
-  for (int j = 0; j < ROUNDS; ++j) {
+  for (int j = 0; j < ROUNDS; ++j) {  // every load of the tile before anything is written
     const uint32_t p = base + (uint32_t)(j * 32 + lane);
-    bool head = false, start = false;
+    bool head = false, start = false, more = false, first_cut = false, is_long = false;
     key[j] = a.pad_key;
     if (p < a.n) {
       key[j] = a.keys[p];
       const uint32_t before = p > 0 ? a.keys[p - 1] : ~0u;
+      const uint32_t q = ((p + cut - 1) >> a.cut_lg << a.cut_lg) + cut;  // a head's first cut, if its run is so long
+      const bool at_cut = (p & (cut - 1)) == 0 && p >= cut;
+      const uint32_t at_q = q < a.n ? a.keys[q] : ~0u;
+      const uint32_t back = at_cut ? a.keys[p - cut] : ~0u;
+      const uint32_t back2 = at_cut && p >= 2 * cut ? a.keys[p - 2 * cut] : ~0u;
+      const uint64_t far = (uint64_t)p + ((uint64_t)(LONG_PARTS - 1) << a.cut_lg);
+      const uint32_t at_far = at_cut && far < a.n ? a.keys[far] : ~0u;
       const bool real = key[j] != a.pad_key;
       head = real && key[j] != before;
-      start = head || (real && p % CUT == 0 && p >= CUT && a.keys[p - CUT] == key[j]);
+      start = head || (real && back == key[j]);
+      more = !head || at_q == key[j];
+      first_cut = !head && start && back2 != key[j];
+      is_long = at_far == key[j];  // that many cuts from here on, and the item before them
       if (real && (p + 1 == a.n || a.keys[p + 1] == a.pad_key)) a.ctr->P = p + 1;
     }
     heads[j] = __ballot_sync(FULL, head);
     starts[j] = __ballot_sync(FULL, start);
+    several[j] = __ballot_sync(FULL, more);
+    firsts[j] = __ballot_sync(FULL, first_cut);
+    longs[j] = __ballot_sync(FULL, is_long);
     sum += (unsigned long long)__popc(starts[j]) << 30 | (unsigned long long)__popc(heads[j]);
   }
   if (lane == 0) s_warp[warp] = sum;
@@ -365,19 +395,17 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
     const bool head = (heads[j] & me) != 0u;
     const uint32_t r = run + __popc(heads[j] & (lt | me)) - 1u;  // the run p belongs to
     if ((starts[j] & me) && at < a.n && r < a.n) {  // the bounds hold unless a wait gave up
-      bool several = !head;
       if (head) {
-        // the first cut of this run, if it has one
-        const uint32_t q = (p + CUT - 1) / CUT * CUT + CUT;
-        several = q < a.n && a.keys[q] == key[j];
         a.run_row[r] = key[j];
         a.run_start[r] = p;
         if (a.ids_out) a.ids_out[r] = (int64_t)key[j];
-      } else if (p < 2 * CUT || a.keys[p - 2 * CUT] != key[j]) {
-        const uint32_t c = atomicAdd(&a.ctr->n_cut, 1u);
-        if (c <= a.n / CUT) a.cuts[c] = make_uint2(r, p);
+        if (a.present) atomicOr(a.present + (key[j] >> 5), 1u << (key[j] & 31u));
+      } else if (firsts[j] & me) {
+        const uint32_t which = longs[j] & me ? 1u : 0u, room = (a.n >> a.cut_lg) + 1u;
+        const uint32_t c = atomicAdd(&a.ctr->n_cut[which], 1u);
+        if (c < room) a.cuts[which * room + c] = make_uint2(r, p);
       }
-      a.items[at] = Item{p << 1 | (head ? 1u : 0u), r << 1 | (several ? 1u : 0u)};
+      a.items[at] = Item{p << 1 | (head ? 1u : 0u), r << 1 | (several[j] & me ? 1u : 0u)};
     }
     item += __popc(starts[j]);
     run += __popc(heads[j]);
@@ -393,8 +421,9 @@ struct SumArgs {
   int32_t accumulate;
   float scale;
   uint32_t n;
+  int32_t cut_lg;
   const uint32_t* order;
-  const Counters* ctr;
+  Counters* ctr;
   const Item* items;
   const uint32_t* run_row;
   const uint32_t* run_start;
@@ -404,6 +433,8 @@ struct SumArgs {
   int64_t* n_out;
   float* out;
   int64_t out_stride;
+  const uint32_t* present;  // dense form, overwriting
+  int64_t V;
 };
 
 template <int V>
@@ -424,108 +455,171 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t run, int64_
   o.store(dst);
 }
 
-// A lane group of 1 << lg lanes per item and slab.  Adds the item's gradient rows in
-// ascending order of their positions.
+// A lane group of 1 << lg lanes per item and slab of V columns a lane, the slabs of an item
+// side by side.  A group takes every so-many-th item and adds its gradient rows in ascending
+// order of their positions, U at a time; where the next U rows lie, of this item or the next
+// one, is read while these arrive, since most rows of a table occur once or twice and their
+// loads would wait for two others each time.  Warps that are done clear the message form's
+// slots that no row needs, or the rows of the dense form that do not occur.  Of the latter
+// they claim `claim` at a time: which warp clears a row changes no value, and it evens out
+// what hot rows leave uneven (262,144 x 2048 bf16 into 131,072 rows: 427 us with equal shares).
 template <typename T, int V>
-__global__ void __launch_bounds__(THREADS) k_token_sums(SumArgs a, int lg, ErrSink err) {
+__global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, int lg, int slabs, int claim, ErrSink err) {
+  constexpr int U = 4;
   follow();
   const bool failed = *(const volatile uint32_t*)err.step != 0u;
   const uint32_t n_items = failed ? 0u : a.ctr->n_items, n_runs = failed ? 0u : a.ctr->n_runs, P = a.ctr->P;
   const int L = 1 << lg;
   const int l = threadIdx.x & (L - 1);
-  const uint32_t groups = gridDim.x * (uint32_t)(THREADS >> lg);
-  const int64_t c = ((int64_t)blockIdx.y * L + l) * V;
-  // the message form's slots that no row needs come after the items
-  const uint32_t units = a.ids_out ? n_items + (a.n - n_runs) : n_items;
-  if (a.n_out && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.n_out = n_runs;
-  const T* grad = static_cast<const T*>(a.grad);
-  for (uint64_t unit = ((uint64_t)blockIdx.x * THREADS + threadIdx.x) >> lg; unit < units; unit += groups) {
-    if (unit >= n_items) {
-      const uint32_t slot = n_runs + (uint32_t)(unit - n_items);
-      if (l == 0 && blockIdx.y == 0) a.ids_out[slot] = n_runs > 0 ? (int64_t)a.run_row[n_runs - 1] : -1;
-      if (c < a.d) {
-        float z[V];
+  const uint32_t group = (blockIdx.x * THREADS + threadIdx.x) >> lg;
+  const uint32_t streams = ((gridDim.x * THREADS) >> lg) / slabs;
+  const uint32_t stream = group / slabs, slab = group - stream * slabs;
+  if (a.n_out && blockIdx.x == 0 && threadIdx.x == 0) *a.n_out = n_runs;
+  const int64_t c = ((int64_t)slab * L + l) * V;
+  const bool in = c < a.d;
+  const T* grad = static_cast<const T*>(a.grad) + c;
+
+  // the item being added, its positions [p, e), and the places of the next U of them
+  uint32_t unit = stream < streams ? stream : n_items, p = 0, e = 0, next_e = 0;
+  Item it{}, next{};
+  auto item_at = [&](uint64_t u, Item& to, uint32_t& end) {
+    end = 0;
+    if (u >= n_items) return;
+    to = a.items[u];
+    end = u + 1 < n_items ? a.items[u + 1].start >> 1 : P;
+  };
+  item_at(unit, it, e);
+  p = it.start >> 1;
+  item_at((uint64_t)unit + streams, next, next_e);
+  uint32_t at[U];
 #pragma unroll
-        for (int j = 0; j < V; ++j) z[j] = 0.f;
-        Pack<float, V> o;
-        o.set(z);
-        o.store(a.out + (uint64_t)slot * (uint64_t)a.out_stride + c);
-      }
-      continue;
-    }
-    if (c >= a.d) continue;
-    const Item it = a.items[unit];
-    const uint32_t s = it.start >> 1;
-    const uint32_t e = unit + 1 < n_items ? a.items[unit + 1].start >> 1 : P;
-    float x[V];
+  for (int i = 0; i < U; ++i)
+    if (p + i < e) at[i] = a.order[p + i];
+  float x[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = 0.f;
-    uint32_t p = s;
-    for (; p + 4 <= e; p += 4) {
-      Pack<T, V> g[4];
+  for (int j = 0; j < V; ++j) x[j] = 0.f;
+  while (unit < n_items) {
+    Pack<T, V> g[U];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i].load(grad + (uint64_t)a.order[p + i] * (uint64_t)a.stride + c);
+    for (int i = 0; i < U; ++i)
+      if (in && p + i < e) g[i].load(grad + (uint64_t)at[i] * (uint64_t)a.stride);
+    const uint32_t left = e - p;
+    const bool more = left > (uint32_t)U;
+    const uint32_t p1 = more ? p + U : next.start >> 1, e1 = more ? e : next_e;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < U; ++i)
+      if (p1 + i < e1) at[i] = a.order[p1 + i];
+    Item after = next;
+    uint32_t after_e = next_e;
+    if (!more) item_at((uint64_t)unit + 2ull * streams, after, after_e);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if ((uint32_t)i < left) {
         float y[V];
         g[i].get(y);
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] += y[j];
       }
-    }
-    for (; p < e; ++p) {
-      Pack<T, V> g;
-      float y[V];
-      g.load(grad + (uint64_t)a.order[p] * (uint64_t)a.stride + c);
-      g.get(y);
+    if (!more) {
+      if (in) {
+        if (it.run & 1u) {
+          // the item before the first cut, or the one that starts at a cut
+          const uint32_t up = ((it.start >> 1) + (1u << a.cut_lg) - 1u) >> a.cut_lg;
+          const uint32_t slot = it.start & 1u ? 2u * (up + 1u) : 2u * up + 1u;
+          Pack<float, V> o;
+          o.set(x);
+          o.store(a.parts + (uint64_t)slot * (uint64_t)a.d + c);
+        } else {
+          write_sum<V>(a, it.run >> 1, c, x);
+        }
+      }
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[j] += y[j];
+      for (int j = 0; j < V; ++j) x[j] = 0.f;
+      it = next;
+      next = after;
+      next_e = after_e;
+      unit = (uint64_t)unit + streams < n_items ? unit + streams : n_items;
     }
-    if (it.run & 1u) {
-      // the item before the first cut, or the one that starts at a cut
-      const uint32_t slot = it.start & 1u ? 2u * ((s + CUT - 1) / CUT + 1u) : 2u * (s / CUT) + 1u;
-      Pack<float, V> o;
-      o.set(x);
-      o.store(a.parts + (uint64_t)slot * (uint64_t)a.d + c);
-    } else {
-      write_sum<V>(a, it.run >> 1, c, x);
+    p = p1;
+    e = e1;
+  }
+  const uint64_t rest = a.ids_out ? a.n - n_runs : a.present ? (uint64_t)a.V : 0u;
+  if (rest == 0) return;
+  __syncwarp();
+  const int lane = threadIdx.x & 31;
+  const Pack<float, V> zero{};
+  auto clear = [&](uint64_t row) {
+    float* dst = a.out + row * (uint64_t)a.out_stride;
+    for (int64_t q = (int64_t)l * V; q < a.d; q += L * V) zero.store(dst + q);
+  };
+  if (a.ids_out) {
+    const int64_t id = n_runs > 0 ? (int64_t)a.run_row[n_runs - 1] : -1;
+    for (uint64_t row = (uint64_t)n_runs + group; row < a.n; row += (gridDim.x * THREADS) >> lg) {
+      if (l == 0) a.ids_out[row] = id;
+      clear(row);
+    }
+    return;
+  }
+  for (;;) {
+    uint32_t mine = 0;
+    if (lane == 0) mine = atomicAdd(&a.ctr->rest, 1u);
+    const uint64_t first = (uint64_t)__shfl_sync(FULL, mine, 0) * (uint64_t)claim;
+    if (first >= rest) break;
+    const uint64_t last = first + claim < rest ? first + claim : rest;
+    for (uint64_t row = first + (lane >> lg); row < last; row += 32 >> lg)
+      if (failed || !(a.present[row >> 5] >> (row & 31u) & 1u)) clear(row);
+  }
+}
+
+// Adds the sums lo .. hi - 1 of a cut run's items to x, at columns c .. c + V - 1, in order.
+// Compensated, so that a row of a million tokens is as exact as one of a hundred.
+template <int V>
+__device__ __forceinline__ void add_parts(const SumArgs& a, uint32_t first_cut, uint32_t lo, uint32_t hi, int64_t c,
+                                          CSum (&x)[V]) {
+  constexpr int U = 8;
+  for (uint32_t k = lo; k < hi; k += U) {
+    Pack<float, V> g[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const uint64_t slot = 2ull * (first_cut >> a.cut_lg) + (k + i == 0 ? 0u : 2u * (k + i) - 1u);
+      if (k + i < hi) g[i].load(a.parts + slot * (uint64_t)a.d + c);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (k + i >= hi) continue;
+      float y[V];
+      g[i].get(y);
+#pragma unroll
+      for (int j = 0; j < V; ++j) csum_add(x[j], y[j]);
     }
   }
 }
 
-// One block per cut run and slab of 32 * V columns: each warp adds a share of the items'
-// sums in order, and the warps' sums are added in order (compensated, so that a row of
-// a million tokens is as exact as one of a hundred).
+// Cut runs, in slabs of 32 * V columns: those of many items by a block each, whose warps add a
+// share of the items' sums each and then the shares in order; then the others by a warp each.
 template <int V>
-__global__ void __launch_bounds__(THREADS) k_token_merge(SumArgs a, ErrSink err) {
+__global__ void __launch_bounds__(THREADS, MERGE_BLOCKS) k_token_merge(SumArgs a, int slabs, ErrSink err) {
   constexpr int WARPS = THREADS / 32;
   __shared__ float s_hi[WARPS][32 * V], s_lo[WARPS][32 * V];
   follow();
   if (*(const volatile uint32_t*)err.step != 0u) return;
-  const uint32_t n_cut = a.ctr->n_cut, n_runs = a.ctr->n_runs, P = a.ctr->P;
+  const uint32_t n_runs = a.ctr->n_runs, P = a.ctr->P, room = (a.n >> a.cut_lg) + 1u;
+  const uint32_t n_short = a.ctr->n_cut[0], n_long = a.ctr->n_cut[1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t c = ((int64_t)blockIdx.y * 32 + lane) * V;
-  for (uint32_t i = blockIdx.x; i < n_cut; i += gridDim.x) {
-    const uint2 cut = a.cuts[i];
+  // the items of a run: the one before the first cut, and one from each cut on
+  auto parts_of = [&](const uint2& cut) {
     const uint32_t end = cut.x + 1 < n_runs ? a.run_start[cut.x + 1] : P;
-    const uint32_t parts = 1u + (end - cut.y + CUT - 1) / CUT;  // before the first cut, and from each on
-    const uint32_t each = (parts + WARPS - 1) / WARPS;
+    return 1u + ((end - cut.y + (1u << a.cut_lg) - 1u) >> a.cut_lg);
+  };
+  for (uint64_t i = blockIdx.x; i < (uint64_t)n_long * slabs; i += gridDim.x) {
+    const uint2 cut = a.cuts[room + i / slabs];
+    const int64_t c = ((int64_t)(i % slabs) * 32 + lane) * V;
+    const uint32_t parts = parts_of(cut), each = (parts + WARPS - 1) / WARPS;
     const uint32_t lo = min(parts, warp * each), hi = min(parts, lo + each);
     CSum x[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) x[j] = CSum{0.f, 0.f};
-    if (c < a.d) {
-#pragma unroll 4
-      for (uint32_t k = lo; k < hi; ++k) {
-        const uint64_t slot = 2ull * (cut.y / CUT) + (k == 0 ? 0u : 2u * k - 1u);
-        Pack<float, V> g;
-        float y[V];
-        g.load(a.parts + slot * (uint64_t)a.d + c);
-        g.get(y);
-#pragma unroll
-        for (int j = 0; j < V; ++j) csum_add(x[j], y[j]);
-      }
-    }
+    if (c < a.d) add_parts<V>(a, cut.y, lo, hi, c, x);
     __syncthreads();  // the block is done with the run before
 #pragma unroll
     for (int j = 0; j < V; ++j) {
@@ -543,6 +637,20 @@ __global__ void __launch_bounds__(THREADS) k_token_merge(SumArgs a, ErrSink err)
       write_sum<V>(a, cut.x, c, y);
     }
   }
+  for (uint64_t i = (uint64_t)blockIdx.x * WARPS + warp; i < (uint64_t)n_short * slabs;
+       i += (uint64_t)gridDim.x * WARPS) {
+    const uint2 cut = a.cuts[i / slabs];
+    const int64_t c = ((int64_t)(i % slabs) * 32 + lane) * V;
+    if (c >= a.d) continue;
+    CSum x[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = CSum{0.f, 0.f};
+    add_parts<V>(a, cut.y, 0u, parts_of(cut), c, x);
+    float y[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[j] = csum_value(x[j]);
+    write_sum<V>(a, cut.x, c, y);
+  }
 }
 
 template <typename T, int V>
@@ -551,14 +659,20 @@ cudaError_t sums_as(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) 
   int lg = 0;
   while ((1 << lg) < pieces && lg < 5) ++lg;
   const int64_t slabs = (pieces + (1 << lg) - 1) >> lg;
-  const int64_t units = (int64_t)a.n + a.n / CUT;
+  const int64_t units = ((int64_t)a.n + (a.n >> a.cut_lg) + (a.present ? a.V : 0)) * slabs;
   const int64_t blocks = (units + (THREADS >> lg) - 1) / (THREADS >> lg);
-  const dim3 grid((unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * 16), (unsigned)slabs);
-  const cudaError_t e = launch_following(k_token_sums<T, V>, grid, THREADS, 0, s, a, lg, err);
-  if (e != cudaSuccess || a.n <= CUT) return e;  // no run can be cut
-  const dim3 mgrid((unsigned)std::min<int64_t>(a.n / CUT, (int64_t)num_sms * 4),
-                   (unsigned)((pieces + 31) / 32));
-  return launch_following(k_token_merge<V>, mgrid, THREADS, 0, s, a, err);
+  const int64_t least = (slabs + (THREADS >> lg) - 1) / (THREADS >> lg);  // that hold one item
+  const int64_t most = std::max<int64_t>(least, (int64_t)num_sms * SUM_BLOCKS);
+  const int claim = (int)std::max<int64_t>(32 >> lg, 32768 / ((int64_t)a.d * 4));  // rows of about 32 KB
+  const cudaError_t e = launch_following(k_token_sums<T, V>, dim3((unsigned)std::min(blocks, most)), THREADS, 0, s, a,
+                                         lg, (int)slabs, claim, err);
+  if (e != cudaSuccess || a.n <= 1u << a.cut_lg) return e;  // no run can be cut
+  constexpr int VM = V < 4 ? V : 4;  // the sums are float32
+  const int64_t mpieces = (a.d + VM - 1) / VM;
+  const int64_t mslabs = (mpieces + 31) / 32;
+  const int64_t mblocks = ((a.n >> a.cut_lg) * mslabs + THREADS / 32 - 1) / (THREADS / 32);
+  return launch_following(k_token_merge<VM>, dim3((unsigned)std::min<int64_t>(mblocks, num_sms * MERGE_BLOCKS)),
+                          THREADS, 0, s, a, (int)mslabs, err);
 }
 
 template <typename T>
@@ -597,14 +711,12 @@ size_t embed_grad_workspace(const EmbedGradArgs& a, size_t* step_word) {
 
 cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns, int num_sms,
                               cudaStream_t s) {
-  if (a.dense && !a.accumulate) {
-    const cudaError_t e =
-        a.dense_stride == a.d
-            ? cudaMemsetAsync(a.dense, 0, (size_t)a.V * a.d * 4, s)
-            : cudaMemset2DAsync(a.dense, (size_t)a.dense_stride * 4, 0, (size_t)a.d * 4, (size_t)a.V, s);
-    if (e != cudaSuccess) return e;
+  if (a.n == 0) {  // the dense form: nothing is added
+    if (a.accumulate) return cudaSuccess;
+    return a.dense_stride == a.d
+               ? cudaMemsetAsync(a.dense, 0, (size_t)a.V * a.d * 4, s)
+               : cudaMemset2DAsync(a.dense, (size_t)a.dense_stride * 4, 0, (size_t)a.d * 4, (size_t)a.V, s);
   }
-  if (a.n == 0) return cudaSuccess;
   const GradPlan p = plan_of(a);
   auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
   Counters* ctr = reinterpret_cast<Counters*>(ws + p.counters);
@@ -636,7 +748,8 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   const ItemArgs ia{at(p.keys[in]), (uint32_t)a.n, (uint32_t)a.V, ctr,
                     reinterpret_cast<unsigned long long*>(ws + p.scan_status),
                     reinterpret_cast<Item*>(ws + p.items), at(p.run_row), at(p.run_start),
-                    reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out};
+                    reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out,
+                    a.dense && !a.accumulate ? at(p.present) : nullptr, p.cut_lg};
   e = launch_following(k_token_items, dim3((unsigned)p.tiles), THREADS, 0, s, ia, a.err, wait_ns);
   if (e != cudaSuccess) return e;
   SumArgs sa{};
@@ -646,6 +759,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   sa.accumulate = a.accumulate;
   sa.scale = a.scale;
   sa.n = (uint32_t)a.n;
+  sa.cut_lg = p.cut_lg;
   sa.order = at(p.vals[in]);
   sa.ctr = ctr;
   sa.items = ia.items;
@@ -657,6 +771,8 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   sa.n_out = a.n_out;
   sa.out = a.dense ? a.dense : a.rows_out;
   sa.out_stride = a.dense ? a.dense_stride : a.d;
+  sa.present = ia.present;
+  sa.V = a.V;
   if (a.type == GBA_F32) return sums_type<float>(sa, a.err, num_sms, s);
   if (a.type == GBA_BF16) return sums_type<bf16>(sa, a.err, num_sms, s);
   return sums_type<f16>(sa, a.err, num_sms, s);
