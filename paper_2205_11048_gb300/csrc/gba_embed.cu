@@ -22,9 +22,13 @@
 // the time of small calls, and their sums' traffic that of large ones: c is 16 for up to
 // 65,536 positions (a message of 6,656 x 16 floats, kernel of the sums: 24.7 us with 64) and
 // 64 above.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "gba_worker.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace gba {
 
@@ -33,6 +37,7 @@ namespace {
 constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xffffffffu;
 constexpr int SUM_BLOCKS = 4, MERGE_BLOCKS = 3;  // of k_token_sums and k_token_merge, that an SM holds
+constexpr int64_t SMALL_N = 8192;  // that k_token_small takes
 constexpr uint32_t LONG_PARTS = 16;
 constexpr int MIN_CUT_LG = 4, MAX_CUT_LG = 6;
 inline int cut_lg_of(int64_t n) { return n <= 65536 ? MIN_CUT_LG : MAX_CUT_LG; }
@@ -178,6 +183,7 @@ struct GradPlan {
   size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, bytes;
   int64_t tiles;
   int cut_lg;
+  bool small;  // keys, sort and items by one cluster
 };
 
 GradPlan plan_of(const EmbedGradArgs& a) {
@@ -185,6 +191,8 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   const uint64_t top = (uint64_t)a.V;  // the key that stands for padding
   int bits = 1;
   while (bits < 32 && (top >> bits) != 0) ++bits;
+  // (a table whose bits of presence eight blocks would take long to clear is not for it)
+  p.small = a.n <= SMALL_N && (!a.dense || a.accumulate || a.V <= 1 << 22);
   p.sort = make_sort_plan(bits, 9);
   p.tiles = (a.n + ITEM_TILE - 1) / ITEM_TILE;
   p.cut_lg = cut_lg_of(a.n);
@@ -233,8 +241,16 @@ struct KeyArgs {
   uint32_t* keys;
 };
 
-// The row of every id (V at padding positions, so that they sort last) and the digit
-// counts of every pass.
+// The row of an id, or V for padding, which so sorts last.
+__device__ __forceinline__ uint32_t key_of(const KeyArgs& a, int64_t id, bool& bad) {
+  if (id == a.pad_id && a.pad_id != GBA_NO_PAD) return (uint32_t)a.V;
+  if (a.id_mode == GBA_ID_MODULO) return (uint32_t)mod_u64((uint64_t)id, (uint64_t)a.V, a.mod_magic);
+  if (id >= 0 && id < a.V) return (uint32_t)id;
+  bad = true;
+  return (uint32_t)a.V;
+}
+
+// The keys of every id and the digit counts of every pass.
 __global__ void __launch_bounds__(THREADS) k_token_keys(KeyArgs a, SortPlan plan, ErrSink err) {
   __shared__ uint32_t h[MAX_PASSES * MAX_RADIX];
   const int words = plan.passes * plan.radix;
@@ -243,19 +259,9 @@ __global__ void __launch_bounds__(THREADS) k_token_keys(KeyArgs a, SortPlan plan
   __syncthreads();
   const uint32_t stride = gridDim.x * THREADS;
   for (uint32_t i = blockIdx.x * THREADS + threadIdx.x; i < a.n; i += stride) {
-    const int64_t id = a.ids[i];
-    uint32_t key;
-    if (id == a.pad_id && a.pad_id != GBA_NO_PAD) {
-      key = (uint32_t)a.V;
-    } else if (a.id_mode == GBA_ID_MODULO) {
-      key = (uint32_t)mod_u64((uint64_t)id, (uint64_t)a.V, a.mod_magic);
-    } else {
-      key = (uint32_t)id;
-      if (id < 0 || id >= a.V) {
-        raise_error(err, ERR_ID_RANGE);
-        key = (uint32_t)a.V;
-      }
-    }
+    bool bad = false;
+    const uint32_t key = key_of(a, a.ids[i], bad);
+    if (bad) raise_error(err, ERR_ID_RANGE);
     a.keys[i] = key;
     for (int p = 0; p < plan.passes; ++p)
       atomicAdd(h + p * plan.radix + ((key >> plan.shift[p]) & plan.mask[p]), 1u);
@@ -282,6 +288,51 @@ struct ItemArgs {
   int32_t cut_lg;
 };
 
+// What stands at sorted position p < n.
+struct Marks {
+  bool head, start;        // of a run, of an item
+  bool several;            // the run has more items than this one
+  bool first_cut, is_long; // p is the run's first cut, and at least LONG_PARTS - 1 cuts follow the run's head
+  bool last;               // before the padding, or the end
+};
+__device__ __forceinline__ Marks marks_of(const ItemArgs& a, const uint32_t* keys, uint32_t p, uint32_t& key) {
+  const uint32_t cut = 1u << a.cut_lg;
+  key = keys[p];
+  const uint32_t before = p > 0 ? keys[p - 1] : ~0u;
+  const uint32_t after = p + 1 < a.n ? keys[p + 1] : a.pad_key;
+  const uint32_t q = ((p + cut - 1) >> a.cut_lg << a.cut_lg) + cut;  // a head's first cut, if its run is so long
+  const bool at_cut = (p & (cut - 1)) == 0 && p >= cut;
+  const uint64_t far = (uint64_t)p + ((uint64_t)(LONG_PARTS - 1) << a.cut_lg);
+  const uint32_t at_q = q < a.n ? keys[q] : ~0u;
+  const uint32_t back = at_cut ? keys[p - cut] : ~0u;
+  const uint32_t back2 = at_cut && p >= 2 * cut ? keys[p - 2 * cut] : ~0u;
+  const uint32_t at_far = at_cut && far < a.n ? keys[far] : ~0u;
+  const bool real = key != a.pad_key;
+  Marks m;
+  m.head = real && key != before;
+  m.start = m.head || (real && back == key);
+  m.several = !m.head || at_q == key;
+  m.first_cut = !m.head && m.start && back2 != key;
+  m.is_long = at_far == key;
+  m.last = real && after == a.pad_key;
+  return m;
+}
+
+__device__ __forceinline__ void write_item(const ItemArgs& a, uint32_t p, uint32_t key, uint32_t item, uint32_t run,
+                                           bool head, bool several, bool first_cut, bool is_long) {
+  if (head) {
+    a.run_row[run] = key;
+    a.run_start[run] = p;
+    if (a.ids_out) a.ids_out[run] = (int64_t)key;
+    if (a.present) atomicOr(a.present + (key >> 5), 1u << (key & 31u));
+  } else if (first_cut) {
+    const uint32_t which = is_long ? 1u : 0u, room = (a.n >> a.cut_lg) + 1u;
+    const uint32_t c = atomicAdd(&a.ctr->n_cut[which], 1u);
+    if (c < room) a.cuts[which * room + c] = make_uint2(run, p);
+  }
+  a.items[item] = Item{p << 1 | (head ? 1u : 0u), run << 1 | (several ? 1u : 0u)};
+}
+
 // Look-back word: [61:60] flag, [59:30] items, [29:0] runs.
 constexpr unsigned long long SCAN_AGG = 1ull << 60;
 constexpr unsigned long long SCAN_INCL = 2ull << 60;
@@ -305,37 +356,22 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
   const uint32_t tile = s_tile;
   const uint32_t base = tile * (uint32_t)ITEM_TILE + (uint32_t)(warp * PER_WARP);
 
-  const uint32_t cut = 1u << a.cut_lg;
   uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS], several[ROUNDS], firsts[ROUNDS], longs[ROUNDS];
   unsigned long long sum = 0ull;
 #pragma unroll
   for (int j = 0; j < ROUNDS; ++j) {  // every load of the tile before anything is written
     const uint32_t p = base + (uint32_t)(j * 32 + lane);
-    bool head = false, start = false, more = false, first_cut = false, is_long = false;
+    Marks m{};
     key[j] = a.pad_key;
     if (p < a.n) {
-      key[j] = a.keys[p];
-      const uint32_t before = p > 0 ? a.keys[p - 1] : ~0u;
-      const uint32_t q = ((p + cut - 1) >> a.cut_lg << a.cut_lg) + cut;  // a head's first cut, if its run is so long
-      const bool at_cut = (p & (cut - 1)) == 0 && p >= cut;
-      const uint32_t at_q = q < a.n ? a.keys[q] : ~0u;
-      const uint32_t back = at_cut ? a.keys[p - cut] : ~0u;
-      const uint32_t back2 = at_cut && p >= 2 * cut ? a.keys[p - 2 * cut] : ~0u;
-      const uint64_t far = (uint64_t)p + ((uint64_t)(LONG_PARTS - 1) << a.cut_lg);
-      const uint32_t at_far = at_cut && far < a.n ? a.keys[far] : ~0u;
-      const bool real = key[j] != a.pad_key;
-      head = real && key[j] != before;
-      start = head || (real && back == key[j]);
-      more = !head || at_q == key[j];
-      first_cut = !head && start && back2 != key[j];
-      is_long = at_far == key[j];  // that many cuts from here on, and the item before them
-      if (real && (p + 1 == a.n || a.keys[p + 1] == a.pad_key)) a.ctr->P = p + 1;
+      m = marks_of(a, a.keys, p, key[j]);
+      if (m.last) a.ctr->P = p + 1;
     }
-    heads[j] = __ballot_sync(FULL, head);
-    starts[j] = __ballot_sync(FULL, start);
-    several[j] = __ballot_sync(FULL, more);
-    firsts[j] = __ballot_sync(FULL, first_cut);
-    longs[j] = __ballot_sync(FULL, is_long);
+    heads[j] = __ballot_sync(FULL, m.head);
+    starts[j] = __ballot_sync(FULL, m.start);
+    several[j] = __ballot_sync(FULL, m.several);
+    firsts[j] = __ballot_sync(FULL, m.first_cut);
+    longs[j] = __ballot_sync(FULL, m.is_long);
     sum += (unsigned long long)__popc(starts[j]) << 30 | (unsigned long long)__popc(heads[j]);
   }
   if (lane == 0) s_warp[warp] = sum;
@@ -392,23 +428,180 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
     const uint32_t p = base + (uint32_t)(j * 32 + lane);
     const uint32_t me = 1u << lane;
     const uint32_t at = item + __popc(starts[j] & lt);
-    const bool head = (heads[j] & me) != 0u;
     const uint32_t r = run + __popc(heads[j] & (lt | me)) - 1u;  // the run p belongs to
-    if ((starts[j] & me) && at < a.n && r < a.n) {  // the bounds hold unless a wait gave up
-      if (head) {
-        a.run_row[r] = key[j];
-        a.run_start[r] = p;
-        if (a.ids_out) a.ids_out[r] = (int64_t)key[j];
-        if (a.present) atomicOr(a.present + (key[j] >> 5), 1u << (key[j] & 31u));
-      } else if (firsts[j] & me) {
-        const uint32_t which = longs[j] & me ? 1u : 0u, room = (a.n >> a.cut_lg) + 1u;
-        const uint32_t c = atomicAdd(&a.ctr->n_cut[which], 1u);
-        if (c < room) a.cuts[which * room + c] = make_uint2(r, p);
-      }
-      a.items[at] = Item{p << 1 | (head ? 1u : 0u), r << 1 | (several[j] & me ? 1u : 0u)};
-    }
+    if ((starts[j] & me) && at < a.n && r < a.n)  // the bounds hold unless a wait gave up
+      write_item(a, p, key[j], at, r, (heads[j] & me) != 0u, (several[j] & me) != 0u, (firsts[j] & me) != 0u,
+                 (longs[j] & me) != 0u);
     item += __popc(starts[j]);
     run += __popc(heads[j]);
+  }
+}
+
+// ---- gradient: keys, sort and items of a small call, by one cluster ----------------------------
+// The same passes over digits as the larger sort, with the keys in the shared memory of
+// eight blocks: a warp ranks its keys among equal digits, the blocks tell each other their
+// counts and send the keys to their places.  One launch instead of five or six whose work is a
+// few microseconds: whole calls of 1,000, 4,000, 8,000 and 16,000 tokens x 64 floats take 14.5,
+// 17.2, 22.0 and 29.9 us this way and 20.5, 25.9, 27.4 and 29.5 the other, so it is for up to
+// 8,192.  (One block alone takes 30 us for 6,656 keys: match.any gives an SM about one key every
+// two cycles.)
+constexpr int CL_BLOCKS = 8, CL_THREADS = 512, CL_WARPS = CL_THREADS / 32;
+constexpr int CL_RADIX = 512;  // a digit for each thread
+static_assert(CL_RADIX == CL_THREADS && 2 * CL_BLOCKS * CL_THREADS == SMALL_N, "");
+
+template <int I>  // keys a thread
+__global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
+    k_token_small(KeyArgs ka, SortPlan plan, ItemArgs a, uint32_t* sorted, uint32_t* order, ErrSink err) {
+  constexpr int PER = CL_THREADS * I;  // a block's
+  __shared__ uint32_t s_keys[PER];
+  __shared__ uint16_t s_vals[PER];
+  __shared__ uint16_t s_cnt[CL_WARPS][CL_RADIX];  // per warp: counts, then offsets among equal digits
+  __shared__ uint32_t s_all[CL_BLOCKS][CL_RADIX];  // every block's counts of the pass
+  __shared__ uint32_t s_place[CL_RADIX];           // where this block's keys of a digit go
+  __shared__ uint32_t s_scan[CL_RADIX / 32];
+  __shared__ unsigned long long s_warp[CL_WARPS];
+  __shared__ unsigned long long s_sums[CL_BLOCKS];
+  __shared__ uint32_t s_bad[CL_BLOCKS];
+  follow();
+  auto cluster = cg::this_cluster();
+  const int me = (int)cluster.block_rank();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t at = (uint32_t)(warp * 32 * I + lane), base = (uint32_t)(me * PER), lt = lanemask_lt();
+  uint32_t key[I], val[I];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < I; ++j) {
+    const uint32_t p = base + at + j * 32;
+    key[j] = p < ka.n ? key_of(ka, ka.ids[p], bad) : ~0u;  // the rest ranks behind every key
+    val[j] = p;
+  }
+  if (me == 0 && tid == 0) *a.ctr = Counters{};
+  if (a.present)
+    for (int64_t i = base / I + tid; i < (ka.V + 31) / 32; i += CL_BLOCKS * CL_THREADS) a.present[i] = 0u;
+  const int any_bad = __syncthreads_or(bad);
+  cluster.sync();  // every block has started: its shared memory may be written
+  if (tid < CL_BLOCKS) cluster.map_shared_rank(s_bad, tid)[me] = any_bad ? 1u : 0u;
+
+  for (int pass = 0; pass < plan.passes; ++pass) {
+    const int shift = plan.shift[pass];
+    const uint32_t mask = plan.mask[pass];
+    for (int i = tid; i < CL_WARPS * CL_RADIX / 2; i += CL_THREADS) reinterpret_cast<uint32_t*>(s_cnt)[i] = 0u;
+    __syncthreads();
+    uint32_t rank[I];
+#pragma unroll
+    for (int j = 0; j < I; ++j) {
+      const uint32_t d = (key[j] >> shift) & mask;
+      const uint32_t peers = __match_any_sync(FULL, d);
+      const uint32_t before = s_cnt[warp][d];
+      rank[j] = before + __popc(peers & lt);
+      __syncwarp();
+      if ((peers & lt) == 0u) s_cnt[warp][d] = (uint16_t)(before + __popc(peers));
+      __syncwarp();
+    }
+    __syncthreads();
+    uint32_t own = 0u;
+#pragma unroll
+    for (int w = 0; w < CL_WARPS; ++w) {
+      const uint32_t c = s_cnt[w][tid];
+      s_cnt[w][tid] = (uint16_t)own;
+      own += c;
+    }
+#pragma unroll
+    for (int b = 0; b < CL_BLOCKS; ++b) cluster.map_shared_rank(&s_all[me][tid], b)[0] = own;
+    cluster.sync();  // and every block has read the keys of the pass before
+    if (pass == 0) {  // the same answer in every block
+      uint32_t failed = 0u;
+      for (int b = 0; b < CL_BLOCKS; ++b) failed |= s_bad[b];
+      if (failed) {
+        if (me == 0 && tid == 0) raise_error(err, ERR_ID_RANGE);
+        return;
+      }
+    }
+    uint32_t total = 0u, before_me = 0u;
+#pragma unroll
+    for (int b = 0; b < CL_BLOCKS; ++b) {
+      const uint32_t c = s_all[b][tid];
+      if (b < me) before_me += c;
+      total += c;
+    }
+    uint32_t incl = total;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(FULL, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    uint32_t place = incl - total + before_me;
+#pragma unroll
+    for (int w = 0; w < CL_WARPS; ++w)
+      if (w < warp) place += s_scan[w];
+    s_place[tid] = place;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < I; ++j) {
+      const uint32_t d = (key[j] >> shift) & mask;
+      const uint32_t pos = s_place[d] + s_cnt[warp][d] + rank[j];  // a permutation of 0 .. 8 PER - 1
+      const uint32_t block = pos / PER, slot = pos % PER;
+      cluster.map_shared_rank(s_keys, block)[slot] = key[j];
+      cluster.map_shared_rank(s_vals, block)[slot] = (uint16_t)val[j];
+    }
+    cluster.sync();
+#pragma unroll
+    for (int j = 0; j < I; ++j) {
+      key[j] = s_keys[at + j * 32];
+      val[j] = s_vals[at + j * 32];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < I; ++j) {
+    const uint32_t p = base + at + j * 32;
+    if (p < a.n) {
+      sorted[p] = key[j];
+      order[p] = val[j];
+    }
+  }
+  cluster.sync();  // the marks look at other blocks' keys
+  Marks m[I];
+  unsigned long long sum = 0ull;
+#pragma unroll
+  for (int j = 0; j < I; ++j) {
+    const uint32_t p = base + at + j * 32;
+    m[j] = Marks{};
+    if (p < a.n) m[j] = marks_of(a, sorted, p, key[j]);
+    if (m[j].last) a.ctr->P = p + 1;
+    sum += (unsigned long long)__popc(__ballot_sync(FULL, m[j].start)) << 30 |
+           (unsigned long long)__popc(__ballot_sync(FULL, m[j].head));
+  }
+  if (lane == 0) s_warp[warp] = sum;
+  __syncthreads();
+  unsigned long long before = 0ull, mine = 0ull;
+#pragma unroll
+  for (int w = 0; w < CL_WARPS; ++w) {
+    if (w < warp) before += s_warp[w];
+    mine += s_warp[w];
+  }
+  if (tid < CL_BLOCKS) cluster.map_shared_rank(s_sums, tid)[me] = mine;
+  cluster.sync();
+  unsigned long long all = 0ull;
+#pragma unroll
+  for (int b = 0; b < CL_BLOCKS; ++b) {
+    if (b < me) before += s_sums[b];
+    all += s_sums[b];
+  }
+  if (me == 0 && tid == 0) {
+    a.ctr->n_items = (uint32_t)(all >> 30);
+    a.ctr->n_runs = (uint32_t)all & 0x3FFFFFFFu;
+  }
+  uint32_t item = (uint32_t)(before >> 30), run = (uint32_t)before & 0x3FFFFFFFu;
+#pragma unroll
+  for (int j = 0; j < I; ++j) {
+    const uint32_t starts = __ballot_sync(FULL, m[j].start), heads = __ballot_sync(FULL, m[j].head);
+    if (m[j].start)
+      write_item(a, base + at + j * 32, key[j], item + __popc(starts & lt),
+                 run + __popc(heads & (lt | 1u << lane)) - 1u, m[j].head, m[j].several, m[j].first_cut, m[j].is_long);
+    item += __popc(starts);
+    run += __popc(heads);
   }
 }
 
@@ -720,38 +913,50 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   const GradPlan p = plan_of(a);
   auto at = [&](size_t o) { return reinterpret_cast<uint32_t*>(ws + o); };
   Counters* ctr = reinterpret_cast<Counters*>(ws + p.counters);
-  const int64_t words = (int64_t)p.cleared / 16;
-  cudaError_t e = launch_following(
-      k_token_clear, dim3((unsigned)std::min<int64_t>((words + THREADS - 1) / THREADS, num_sms * 4)),
-      THREADS, 0, s, reinterpret_cast<uint4*>(ws), words);
-  if (e != cudaSuccess) return e;
   const KeyArgs ka{a.ids, (uint32_t)a.n, a.id_mode, a.pad_id, a.V, a.mod_magic, at(p.hist), at(p.keys[0])};
-  e = launch_following(k_token_keys, dim3((unsigned)std::min<int64_t>((a.n + 1023) / 1024, num_sms * 6)),
-                       THREADS, 0, s, ka, p.sort, a.err);
-  if (e != cudaSuccess) return e;
-  int in = 0;
-  for (int i = 0; i < p.sort.passes; ++i, in ^= 1) {
-    SortPass sp{};
-    sp.N = (uint32_t)a.n;
-    sp.hist = at(p.hist) + i * p.sort.radix;
-    sp.ticket = &ctr->tickets[i];
-    sp.keys_in = at(p.keys[in]);
-    sp.vals_in = at(p.vals[in]);
-    sp.keys_out = at(p.keys[in ^ 1]);
-    sp.vals_out = at(p.vals[in ^ 1]);
-    sp.status = reinterpret_cast<unsigned long long*>(ws + p.sort_status);
-    sp.epoch = (uint32_t)i + 1u;
-    launch_onesweep(p.sort, i, sp, a.err, wait_ns, s);
+  ItemArgs ia{nullptr, (uint32_t)a.n, (uint32_t)a.V, ctr, reinterpret_cast<unsigned long long*>(ws + p.scan_status),
+              reinterpret_cast<Item*>(ws + p.items), at(p.run_row), at(p.run_start),
+              reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out,
+              a.dense && !a.accumulate ? at(p.present) : nullptr, p.cut_lg};
+  const uint32_t* order = nullptr;
+  cudaError_t e;
+  if (p.small) {
+    order = at(p.vals[0]);
+    ia.keys = at(p.keys[0]);
+    auto kernel = a.n <= CL_BLOCKS * CL_THREADS ? k_token_small<1> : k_token_small<2>;
+    e = launch_following(kernel, dim3(CL_BLOCKS), CL_THREADS, 0, s, ka, p.sort, ia, at(p.keys[0]), at(p.vals[0]),
+                         a.err);
+    if (e != cudaSuccess) return e;
+  } else {
+    const int64_t words = (int64_t)p.cleared / 16;
+    e = launch_following(k_token_clear,
+                         dim3((unsigned)std::min<int64_t>((words + THREADS - 1) / THREADS, num_sms * 4)), THREADS, 0,
+                         s, reinterpret_cast<uint4*>(ws), words);
+    if (e != cudaSuccess) return e;
+    e = launch_following(k_token_keys, dim3((unsigned)std::min<int64_t>((a.n + 1023) / 1024, num_sms * 6)), THREADS,
+                         0, s, ka, p.sort, a.err);
+    if (e != cudaSuccess) return e;
+    int in = 0;
+    for (int i = 0; i < p.sort.passes; ++i, in ^= 1) {
+      SortPass sp{};
+      sp.N = (uint32_t)a.n;
+      sp.hist = at(p.hist) + i * p.sort.radix;
+      sp.ticket = &ctr->tickets[i];
+      sp.keys_in = at(p.keys[in]);
+      sp.vals_in = at(p.vals[in]);
+      sp.keys_out = at(p.keys[in ^ 1]);
+      sp.vals_out = at(p.vals[in ^ 1]);
+      sp.status = reinterpret_cast<unsigned long long*>(ws + p.sort_status);
+      sp.epoch = (uint32_t)i + 1u;
+      launch_onesweep(p.sort, i, sp, a.err, wait_ns, s);
+    }
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    order = at(p.vals[in]);
+    ia.keys = at(p.keys[in]);
+    e = launch_following(k_token_items, dim3((unsigned)p.tiles), THREADS, 0, s, ia, a.err, wait_ns);
+    if (e != cudaSuccess) return e;
   }
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  const ItemArgs ia{at(p.keys[in]), (uint32_t)a.n, (uint32_t)a.V, ctr,
-                    reinterpret_cast<unsigned long long*>(ws + p.scan_status),
-                    reinterpret_cast<Item*>(ws + p.items), at(p.run_row), at(p.run_start),
-                    reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out,
-                    a.dense && !a.accumulate ? at(p.present) : nullptr, p.cut_lg};
-  e = launch_following(k_token_items, dim3((unsigned)p.tiles), THREADS, 0, s, ia, a.err, wait_ns);
-  if (e != cudaSuccess) return e;
   SumArgs sa{};
   sa.grad = a.grad;
   sa.stride = a.stride;
@@ -760,7 +965,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   sa.scale = a.scale;
   sa.n = (uint32_t)a.n;
   sa.cut_lg = p.cut_lg;
-  sa.order = at(p.vals[in]);
+  sa.order = order;
   sa.ctr = ctr;
   sa.items = ia.items;
   sa.run_row = ia.run_row;
