@@ -4,11 +4,13 @@
 //
 // Bound by HBM bandwidth: a row is read once, stays in registers while its statistics are
 // formed (mean first, then the squares of the differences, so a large mean costs no digits),
-// and is written once.  A row is held by up to 32 lanes, or by up to 16 warps, and the loads
-// of the next row are in flight while this one is reduced.  What a thread does for a row
-// beside its columns (two sums over lanes and warps, a root) costs as many instructions as
-// ten columns or so, so a thread holds 64 bytes of a row (backward 32 of each of the two),
-// and the arithmetic is done on pairs.  Backward, a block keeps its threads' shares of
+// and is written once.  A narrow row is held by up to 32 lanes, one vector each; a wider one
+// by up to 16 warps, each of which holds consecutive columns, and the loads of the next row
+// are in flight while this one is reduced.  What a thread does for a row beside its columns
+// (two sums over lanes and warps, a root, addresses) costs as many instructions as ten
+// columns or so, so a thread of a wide row holds 64 bytes of it (backward 32 of each of the
+// two), the arithmetic is done on pairs, and a warp whose columns all exist checks none of
+// them.  Backward, a block keeps its threads' shares of
 // dgamma and dbeta in registers over all the rows it takes and leaves one partial row; a
 // second kernel adds the partial rows in order.  Rows too wide for a block's registers are
 // read again from L2 instead.
@@ -90,61 +92,71 @@ __device__ __forceinline__ float both(f2 a) {
 }
 
 // ---- how a block's threads share rows ----------------------------------------------
-// A row belongs to L lanes of a warp, or to W whole warps; its threads' t-th piece of V
-// columns is piece k * tpr + t, for k = 0 .. E / V - 1.
+// LANES: a row belongs to L lanes of a warp, and a lane's piece k of V columns is the row's
+// piece k L + lane.  Otherwise it belongs to W warps, warp w holds the 32 E columns from
+// 32 E w on, and a lane's piece k is the warp's piece 32 k + lane.
 struct Split {
   int L, W;
 };
+template <int V, int E, bool LANES>
 struct Place {
-  int t, tpr, group, groups;
-  int warp_group;  // the first group of the thread's warp: a warp's lanes go round together
-  __device__ __forceinline__ explicit Place(const Split& s) {
+  int group, groups;  // of threads that hold a row: this thread's, and how many the block has
+  int warp_group;     // the first group of the thread's warp: a warp's lanes go round together
+  int t;              // this thread in its group
+  int first;          // its first column
+  int step;           // columns from one piece to the next
+  bool whole;         // every column that the warp's threads hold exists
+  __device__ __forceinline__ Place(const Split& s, int d) {
     const int lane = threadIdx.x & 31, warp = (int)threadIdx.x >> 5;
-    if (s.W == 1) {
+    if (LANES) {
       t = lane & (s.L - 1);
-      tpr = s.L;
       group = (int)threadIdx.x / s.L;
       groups = (int)blockDim.x / s.L;
       warp_group = warp * (32 / s.L);
+      first = t * V;
+      step = s.L * V;
+      whole = d == s.L * E;
     } else {
-      t = warp % s.W * 32 + lane;
-      tpr = s.W * 32;
-      group = warp / s.W;
-      groups = (int)blockDim.x / tpr;
-      warp_group = group;
+      const int w = warp % s.W;
+      t = w * 32 + lane;
+      group = warp_group = warp / s.W;
+      groups = (int)blockDim.x / (32 * s.W);
+      first = w * 32 * E + lane * V;
+      step = 32 * V;
+      whole = (w + 1) * 32 * E <= d;
     }
   }
 };
 
 // Sums of N values over the threads of a row, in every one of them.  s: N words per warp of
 // the block; the caller alternates between two of them, so one barrier a sum is enough.
-template <int N>
+template <int N, bool LANES>
 __device__ __forceinline__ void row_sum(float (&x)[N], const Split& sp, int group, float (*s)[N]) {
-  if (sp.L == 32) {
+  if constexpr (LANES) {
+    for (int o = 1; o < sp.L; o <<= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+  } else {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
-  } else {
-    for (int o = 1; o < sp.L; o <<= 1)
+    if (sp.W == 1) return;
+    const int warp = (int)threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(FULL, x[i], o);
+      for (int i = 0; i < N; ++i) s[warp][i] = x[i];
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(sp.W * 32) : "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = 0.f;
+    for (int w = 0; w < sp.W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += s[group * sp.W + w][i];
   }
-  if (sp.W == 1) return;
-  const int warp = (int)threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0)
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[warp][i] = x[i];
-  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(sp.W * 32) : "memory");
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = 0.f;
-  for (int w = 0; w < sp.W; ++w)
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += s[group * sp.W + w][i];
 }
 
-// A thread's E columns of a row, as they were loaded.  WHOLE: the row has exactly as many
-// columns as its threads hold.  Pieces past the row's end hold zeros from clear() on.
+// A thread's E columns of a row, as they were loaded.  Pieces past the row's end hold zeros
+// from clear() on.  left: columns from the thread's first one to the row's end.
 template <typename T, int V, int E, bool WHOLE>
 struct Held {
   static constexpr int K = E / V;
@@ -153,14 +165,11 @@ struct Held {
 #pragma unroll
     for (int k = 0; k < K; ++k) p[k] = Pack<T, V>{};
   }
-  static __device__ __forceinline__ bool has(int k, const Place& at, int d) {
-    return WHOLE || (k * at.tpr + at.t) * V < d;
-  }
-  __device__ __forceinline__ void load(const T* row, const Place& at, int d) {
-    row += at.t * V;
+  static __device__ __forceinline__ bool has(int k, int step, int left) { return WHOLE || k * step < left; }
+  __device__ __forceinline__ void load(const T* from, int step, int left) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (has(k, at, d)) p[k].load(row + k * at.tpr * V);
+      if (has(k, step, left)) p[k].load(from + k * step);
   }
   __device__ __forceinline__ void get(f2 (&x)[E / 2]) const {
     float v[E];
@@ -174,109 +183,101 @@ struct Held {
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) x[i] = pair(v[2 * i], v[2 * i + 1]);
   }
-  static __device__ __forceinline__ void store(T* row, const f2 (&x)[E / 2], const Place& at, int d) {
+  static __device__ __forceinline__ void store(T* to, const f2 (&x)[E / 2], int step, int left) {
     float v[E];
 #pragma unroll
     for (int i = 0; i < E / 2; ++i) split(x[i], v[2 * i], v[2 * i + 1]);
-    row += at.t * V;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (!has(k, at, d)) continue;
+      if (!has(k, step, left)) continue;
       float y[V];
 #pragma unroll
       for (int j = 0; j < V; ++j) y[j] = v[k * V + j];
       Pack<T, V> o;
       o.set(y);
-      o.store(row + k * at.tpr * V);
+      o.store(to + k * step);
     }
   }
 };
 
-// Columns that a thread holds, forward (single elements of 16 bits take a register each).
+// Columns that a thread holds: of a narrow row one vector; of a wide one, forward, 64 bytes
+// (single elements of 16 bits take a register each, so 16 of those).
+template <int V>
+constexpr int E_LANES = V > 1 ? V : 2;
 template <typename T, int V>
 constexpr int E_NORM = V > 1 ? 64 / (int)sizeof(T) : 16;
 
-// Where shared memory keeps the parameter of column j of piece q, of Q pieces: a lane's
-// accesses of up to 16 bytes lie next to its neighbours'.
+// Shared memory keeps a parameter of column j of piece q, of Q pieces, where a lane's accesses
+// of up to 16 bytes lie next to its neighbours'.
 template <int V>
 __device__ __forceinline__ int param_slot(int q, int j, int Q) {
   constexpr int H = V < 4 ? V : 4;
   return ((j / H) * Q + q) * H + j % H;
 }
 
-template <typename T, int V, bool WHOLE>
-__global__ void __launch_bounds__(512) k_layer_norm(LayerNormArgs a, Split sp) {
-  constexpr int E = E_NORM<T, V>, K = E / V, P = E / 2, H = V < 4 ? V : 4;
-  extern __shared__ __align__(16) float s_param[];  // gamma, beta: [2][columns held]
-  __shared__ float s_sum[2][MOST_WARPS][1];
-  follow();
-  const Place at(sp);
-  const int Q = at.tpr * K;
+template <typename T, int V, int E, bool LANES, bool WHOLE>
+__device__ __forceinline__ void norm_rows(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
+                                          float* s_param, int Q, float (*s_sum)[MOST_WARPS][1]) {
+  constexpr int K = E / V, P = E / 2, H = V < 4 ? V : 4;
+  using Row = Held<T, V, E, WHOLE>;
+  const int step = LANES ? at.step : 32 * V, left = a.d - at.first;
   const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
-  const T* x = static_cast<const T*>(a.x);
-  int64_t row = (int64_t)blockIdx.x * at.groups + at.group;
   int64_t first = (int64_t)blockIdx.x * at.groups + at.warp_group;
-  using Row = Held<T, V, E, WHOLE>;
+  int64_t row = (int64_t)blockIdx.x * at.groups + at.group;
+  const T* x = static_cast<const T*>(a.x) + at.first;
+  const float* gamma = s_param + at.first / V * H;  // piece k of them is step / V pieces further
   Row in;
   in.clear();
-  if (row < a.n) in.load(x + row * a.x_stride, at, a.d);
-  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
-    const int o = param_slot<V>(c / V, c % V, Q);
-    s_param[o] = param_at(a.gamma, a.param_type, c, 1.f);
-    s_param[Q * V + o] = param_at(a.beta, a.param_type, c, 0.f);
-  }
-  __syncthreads();
+  if (row < a.n) in.load(x + row * a.x_stride, step, left);
+  asm volatile("bar.sync 0;" ::: "memory");  // the parameters are there, for warps of either kind
   for (; first < a.n; first += per_pass, row += per_pass) {
     const bool live = row < a.n;
     f2 v[P];
     in.get(v);
-    if (row + per_pass < a.n) in.load(x + (row + per_pass) * a.x_stride, at, a.d);
+    if (row + per_pass < a.n) in.load(x + (row + per_pass) * a.x_stride, step, left);
     f2 acc = v[0];
 #pragma unroll
     for (int i = 1; i < P; ++i) acc = add2(acc, v[i]);
     float sum[1] = {both(acc)};
-    row_sum<1>(sum, sp, at.group, s_sum[0]);
+    row_sum<1, LANES>(sum, sp, at.group, s_sum[0]);
     const float mean = sum[0] * inv_d;
-    acc = pair(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < P; ++i) v[i] = add2(v[i], pair(-mean, -mean));
+    if (!WHOLE) {
+      float z[E];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (!Row::has(k, at, a.d)) continue;
-      if constexpr (V > 1) {
+      for (int i = 0; i < P; ++i) split(v[i], z[2 * i], z[2 * i + 1]);
 #pragma unroll
-        for (int i = k * V / 2; i < (k + 1) * V / 2; ++i) acc = fma2(v[i], v[i], acc);
-      } else {
-        float lo, hi;
-        split(v[k / 2], lo, hi);
-        const float z = k % 2 ? hi : lo;
-        acc = fma2(pair(z, 0.f), pair(z, 0.f), acc);
-      }
+      for (int e = 0; e < E; ++e) z[e] = Row::has(e / V, step, left) ? z[e] : 0.f;
+#pragma unroll
+      for (int i = 0; i < P; ++i) v[i] = pair(z[2 * i], z[2 * i + 1]);
     }
+    acc = mul2(v[0], v[0]);
+#pragma unroll
+    for (int i = 1; i < P; ++i) acc = fma2(v[i], v[i], acc);
     sum[0] = both(acc);
-    row_sum<1>(sum, sp, at.group, s_sum[1]);
+    row_sum<1, LANES>(sum, sp, at.group, s_sum[1]);
     const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
     if (live && at.t == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
     if (!live) continue;
-    T* y = static_cast<T*>(a.y) + row * a.y_stride + at.t * V;
+    T* y = static_cast<T*>(a.y) + row * a.y_stride + at.first;
     float z[E];
 #pragma unroll
     for (int i = 0; i < P; ++i) split(mul2(v[i], pair(rstd, rstd)), z[2 * i], z[2 * i + 1]);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int q = k * at.tpr + at.t;
-      if (!Row::has(k, at, a.d)) continue;
+      if (!Row::has(k, step, left)) continue;
       float o[V];
 #pragma unroll
       for (int h = 0; h < V / H; ++h) {
         Pack<float, H> g, b;
         float gj[H], bj[H];
-        g.load(s_param + param_slot<V>(q, h * H, Q));
-        b.load(s_param + Q * V + param_slot<V>(q, h * H, Q));
+        g.load(gamma + h * Q * H + k * (step / V) * H);
+        b.load(gamma + Q * V + h * Q * H + k * (step / V) * H);
         g.get(gj);
         b.get(bj);
 #pragma unroll
@@ -284,17 +285,34 @@ __global__ void __launch_bounds__(512) k_layer_norm(LayerNormArgs a, Split sp) {
       }
       Pack<T, V> w;
       w.set(o);
-      w.store(y + k * at.tpr * V);
+      w.store(y + k * step);
     }
   }
+}
+
+template <typename T, int V, int E, bool LANES>
+__global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm(LayerNormArgs a, Split sp) {
+  extern __shared__ __align__(16) float s_param[];  // gamma, beta: [2][columns held]
+  __shared__ float s_sum[2][MOST_WARPS][1];
+  follow();
+  const Place<V, E, LANES> at(sp, a.d);
+  const int Q = sp.L * sp.W * (E / V);
+  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+    const int o = param_slot<V>(c / V, c % V, Q);
+    s_param[o] = param_at(a.gamma, a.param_type, c, 1.f);
+    s_param[Q * V + o] = param_at(a.beta, a.param_type, c, 0.f);
+  }
+  if (at.whole)
+    norm_rows<T, V, E, LANES, true>(a, sp, at, s_param, Q, s_sum);
+  else
+    norm_rows<T, V, E, LANES, false>(a, sp, at, s_param, Q, s_sum);
 }
 
 // Rows of any width: one block each, read three times.
 template <typename T, int V>
 __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs a) {
   __shared__ float s_sum[2][32][1];
-  const Split sp{32, WIDE_THREADS / 32};
-  follow();
+    follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -308,7 +326,7 @@ __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs 
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] += v[j];
     }
-    row_sum<1>(sum, sp, 0, s_sum[0]);
+    row_sum<1, false>(sum, Split{32, WIDE_THREADS / 32}, 0, s_sum[0]);
     const float mean = sum[0] * inv_d;
     sum[0] = 0.f;
     for (int64_t c = (int64_t)threadIdx.x * V; c < a.d; c += step) {
@@ -317,7 +335,7 @@ __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs 
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[0] = fmaf(v[j] - mean, v[j] - mean, sum[0]);
     }
-    row_sum<1>(sum, sp, 0, s_sum[1]);
+    row_sum<1, false>(sum, Split{32, WIDE_THREADS / 32}, 0, s_sum[1]);
     const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -337,44 +355,39 @@ __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs 
   }
 }
 
-// Columns that a thread of the gradient holds: as many as leave room for the weights, the two
-// sums, and the loads of this row and (FETCH) the next one.
+// Columns that a thread of the gradient holds of a wide row: as many as leave room for the
+// weights, the two sums, and the loads of this row and (FETCH) the next one.
 template <typename T, int V>
 constexpr int E_GRAD = sizeof(T) == 2 && V > 1 ? 16 : 8;
 
-// One partial row of dgamma and dbeta per block: [2][blocks][d].  What a thread keeps of a row
-// while its sums are formed is its loads; h and g are formed from them twice.
-template <typename T, int V, int E, bool FETCH, bool WHOLE>
-__global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split sp) {
+// dx of the rows that this thread's group takes, and its shares of dgamma and dbeta.  What a
+// thread keeps of a row while its sums are formed is its loads; h and g are formed from them
+// twice.
+template <typename T, int V, int E, bool LANES, bool FETCH, bool WHOLE>
+__device__ __forceinline__ void grad_rows(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
+                                          float (*s_sum)[MOST_WARPS][2], f2 (&dg)[E / 2], f2 (&db)[E / 2]) {
   constexpr int K = E / V, P = E / 2;
-  __shared__ float s_sum[2][MOST_WARPS][2];
-  __shared__ float s_part[THREADS * E];
-  follow();
-  const Place at(sp);
+  using Row = Held<T, V, E, WHOLE>;
+  using Next = Held<T, V, FETCH ? E : V, WHOLE>;
+  const int step = LANES ? at.step : 32 * V, left = a.d - at.first;
   const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
   const f2 zero = pair(0.f, 0.f);
-  f2 gamma[P], dg[P], db[P];
+  f2 gamma[P];
   {
     float y[E];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       float z[V];
-      const int c = (k * at.tpr + at.t) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j) z[j] = 0.f;
-      if (c < a.d) params_at<V>(a.gamma, a.param_type, c, 1.f, z);
+      if (Row::has(k, step, left)) params_at<V>(a.gamma, a.param_type, at.first + k * step, 1.f, z);
 #pragma unroll
       for (int j = 0; j < V; ++j) y[k * V + j] = z[j];
     }
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      gamma[i] = pair(y[2 * i], y[2 * i + 1]);
-      dg[i] = db[i] = zero;
-    }
+    for (int i = 0; i < P; ++i) gamma[i] = pair(y[2 * i], y[2 * i + 1]);
   }
-  using Row = Held<T, V, E, WHOLE>;
-  using Next = Held<T, V, FETCH ? E : V, WHOLE>;
   Row xin, din;
   Next xnext, dnext;
   xin.clear();
@@ -389,8 +402,8 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split 
       m = r = 0.f;
       return;
     }
-    xs.load(static_cast<const T*>(a.x) + row * a.x_stride, at, a.d);
-    ds.load(static_cast<const T*>(a.dy) + row * a.dy_stride, at, a.d);
+    xs.load(static_cast<const T*>(a.x) + row * a.x_stride + at.first, step, left);
+    ds.load(static_cast<const T*>(a.dy) + row * a.dy_stride + at.first, step, left);
     m = a.mean[row];
     r = a.rstd[row];
   };
@@ -425,12 +438,12 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split 
       }
     }
     float sum[2] = {both(s0), both(s1)};
-    row_sum<2>(sum, sp, at.group, s_sum[flip]);
+    row_sum<2, LANES>(sum, sp, at.group, s_sum[flip]);
     flip ^= 1;
+    if (row >= a.n) continue;
     const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
     const f2 nmg = pair(-mg, -mg), nmgh = pair(-mgh, -mgh);
     f2 x[P], g[P];
-    if (row >= a.n) continue;
     xin.get(x);
     din.get(g);
 #pragma unroll
@@ -438,29 +451,48 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split 
       const f2 h = mul2(add2(x[i], m), r);
       g[i] = mul2(r, fma2(h, nmgh, fma2(g[i], gamma[i], nmg)));
     }
-    Row::store(static_cast<T*>(a.y) + row * a.y_stride, g, at, a.d);
+    Row::store(static_cast<T*>(a.y) + row * a.y_stride + at.first, g, step, left);
   }
+}
+
+// One partial row of dgamma and dbeta per block: [2][blocks][d].
+template <typename T, int V, int E, bool LANES, bool FETCH>
+__global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm_grad(LayerNormArgs a, Split sp) {
+  constexpr int K = E / V, P = E / 2;
+  __shared__ float s_sum[2][MOST_WARPS][2];
+  __shared__ float s_part[THREADS * E];
+  follow();
+  const Place<V, E, LANES> at(sp, a.d);
+  f2 dg[P], db[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) dg[i] = db[i] = pair(0.f, 0.f);
+  if (at.whole)
+    grad_rows<T, V, E, LANES, FETCH, true>(a, sp, at, s_sum, dg, db);
+  else
+    grad_rows<T, V, E, LANES, FETCH, false>(a, sp, at, s_sum, dg, db);
   // the block's groups of threads, in order: first those within a warp, then through shared memory
+  __syncwarp();
   float mine[2][E];
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     split(dg[i], mine[0][2 * i], mine[0][2 * i + 1]);
     split(db[i], mine[1][2 * i], mine[1][2 * i + 1]);
   }
+  if (LANES)
 #pragma unroll
-  for (int which = 0; which < 2; ++which)
+    for (int which = 0; which < 2; ++which)
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      for (int o = sp.L; o < 32; o <<= 1) mine[which][e] += __shfl_xor_sync(FULL, mine[which][e], o);
-  const int sets = sp.W == 1 ? (int)blockDim.x >> 5 : at.groups;
-  const int set = sp.W == 1 ? (int)threadIdx.x >> 5 : at.group, width = at.tpr * E;
-  const bool one_of = (int)(threadIdx.x & 31) < sp.L;
+      for (int e = 0; e < E; ++e)
+        for (int o = sp.L; o < 32; o <<= 1) mine[which][e] += __shfl_xor_sync(FULL, mine[which][e], o);
+  const int sets = LANES ? (int)blockDim.x >> 5 : at.groups;
+  const int set = LANES ? (int)threadIdx.x >> 5 : at.group, width = sp.L * sp.W * E;
+  const bool one_of = !LANES || (int)(threadIdx.x & 31) < sp.L;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float* out = a.parts + ((int64_t)which * gridDim.x + blockIdx.x) * a.d;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = (k * at.tpr + at.t) * V;
+      const int c = at.first + k * at.step;
       if (!one_of || c >= a.d) continue;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -485,8 +517,7 @@ __global__ void __launch_bounds__(512) k_layer_norm_grad(LayerNormArgs a, Split 
 template <typename T, int V>
 __global__ void __launch_bounds__(WIDE_GRAD_THREADS) k_layer_norm_grad_wide(LayerNormArgs a) {
   __shared__ float s_sum[2][WIDE_GRAD_THREADS / 32][2];
-  const Split sp{32, WIDE_GRAD_THREADS / 32};
-  follow();
+    follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
   int flip = 0;
@@ -511,7 +542,7 @@ __global__ void __launch_bounds__(WIDE_GRAD_THREADS) k_layer_norm_grad_wide(Laye
         sum[1] = fmaf(gj, (h[j] - mean) * rstd, sum[1]);
       }
     }
-    row_sum<2>(sum, sp, 0, s_sum[flip]);
+    row_sum<2, false>(sum, Split{32, WIDE_GRAD_THREADS / 32}, 0, s_sum[flip]);
     flip ^= 1;
     const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
     for (int64_t c = (int64_t)threadIdx.x * V; c < a.d; c += step) {
@@ -591,25 +622,28 @@ __global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int
 
 constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns
 
-// The threads of a row of d columns, E to a thread, and of a block of such rows.
-Split split_of(int32_t d, int E, int* threads) {
-  const int need = (d + E - 1) / E;
+// The lanes of a narrow row of d columns, E to a lane.
+Split lanes_of(int32_t d, int E) {
   Split s{1, 1};
-  while (s.L < need && s.L < 32) s.L <<= 1;
-  if (need > 32) s.W = (need + 31) / 32;
-  *threads = s.W == 1 ? THREADS : 32 * s.W * std::max(1, THREADS / (32 * s.W));
+  while (s.L * E < d) s.L <<= 1;
   return s;
 }
 
-// Blocks of a kernel that an SM holds, for each number of warps of a row (a row's warps give
-// the block's size).
+// The warps of a wide row, E columns to a lane, and the threads of a block of such rows.
+Split warps_of(int32_t d, int E, int* threads) {
+  const Split s{32, (d + 32 * E - 1) / (32 * E)};
+  *threads = 32 * s.W * std::max(1, THREADS / (32 * s.W));
+  return s;
+}
+
+// Blocks of a kernel for wide rows that an SM holds, for each number of warps of a row.
 struct Residency {
   int blocks[MOST_WARPS + 1];
   template <typename F, typename S>
   Residency(F* kernel, int E, S smem_of) {
     for (int w = 1; w <= MOST_WARPS; ++w) {
       int threads;
-      split_of(w * 32 * E, E, &threads);
+      warps_of(w * 32 * E, E, &threads);
       const size_t smem = smem_of(w);
       blocks[w] = 0;
       if (smem > 48 * 1024)
@@ -620,50 +654,47 @@ struct Residency {
     }
   }
 };
+// And of one for narrow rows.
+template <typename F>
+int resident(F* kernel, size_t smem) {
+  int blocks = 0;
+  return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, THREADS, smem) == cudaSuccess && blocks > 0
+             ? blocks
+             : 1;
+}
 
 unsigned grid_of(int64_t n, const Split& s, int threads, int num_sms, int per_sm) {
   const int64_t rows = threads / (s.L * s.W);  // a block's
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows, (int64_t)num_sms * per_sm);
 }
 
-template <typename T, int V, bool WHOLE>
-cudaError_t norm_rows(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int E = E_NORM<T, V>;
-  auto smem_of = [](int w) { return (size_t)w * 32 * E * 2 * sizeof(float); };
-  static const Residency held(k_layer_norm<T, V, WHOLE>, E, smem_of);
-  int threads;
-  const Split sp = split_of(a.d, E, &threads);
-  return launch_following(k_layer_norm<T, V, WHOLE>,
-                          dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s,
-                          a, sp);
-}
-
-// Does every thread that holds a row of d columns hold E of them?  (Asked where it saves
-// instructions: in rows read by vectors of 16 bytes.)
-template <typename T, int V, int E>
-bool is_whole(int32_t d) {
-  int threads;
-  const Split sp = split_of(d, E, &threads);
-  return V * sizeof(T) == 16 && sp.L * sp.W * E == d;
-}
-
 template <typename T, int V>
 cudaError_t norm_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int E = E_NORM<T, V>;
+  constexpr int EL = E_LANES<V>, E = E_NORM<T, V>;
+  if (a.d <= 32 * EL) {
+    constexpr size_t smem = (size_t)32 * EL * 2 * sizeof(float);
+    static const int held = resident(k_layer_norm<T, V, EL, true>, smem);
+    const Split sp = lanes_of(a.d, EL);
+    return launch_following(k_layer_norm<T, V, EL, true>, dim3(grid_of(a.n, sp, THREADS, num_sms, held)), THREADS,
+                            smem, s, a, sp);
+  }
   if (a.d > MOST_WARPS * 32 * E)
     return launch_following(k_layer_norm_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 2)),
                             WIDE_THREADS, 0, s, a);
-  if constexpr (V * sizeof(T) == 16)
-    if (is_whole<T, V, E>(a.d)) return norm_rows<T, V, true>(a, num_sms, s);
-  return norm_rows<T, V, false>(a, num_sms, s);
+  auto smem_of = [](int w) { return (size_t)w * 32 * E * 2 * sizeof(float); };
+  static const Residency held(k_layer_norm<T, V, E, false>, E, smem_of);
+  int threads;
+  const Split sp = warps_of(a.d, E, &threads);
+  return launch_following(k_layer_norm<T, V, E, false>,
+                          dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s, a,
+                          sp);
 }
 
-// How a gradient's rows are held: with the next row's loads in flight, without (float32 rows of
-// up to 8,192 columns), or not at all.
-enum class Way { FETCH, PLAIN, WIDE };
+// How a gradient's rows are held: a vector a lane, with the next row's loads in flight, without
+// (rows of up to 8,192 columns that are read by 8 columns a thread), or not at all.
+enum class Way { LANES, FETCH, PLAIN, WIDE };
 struct GradShape {
   Way way;
-  bool whole;
   Split split;
   int threads;
   int parts;  // blocks, and partial rows
@@ -671,18 +702,22 @@ struct GradShape {
 
 template <typename T, int V>
 GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
-  constexpr int E = E_GRAD<T, V>;
+  constexpr int EL = E_LANES<V>, E = E_GRAD<T, V>;
   GradShape g{};
-  auto none = [](int) { return (size_t)0; };
-  if (a.d <= MOST_WARPS * 32 * E) {
-    static const Residency held(k_layer_norm_grad<T, V, E, true, false>, E, none);
+  if (a.d <= 32 * EL) {
+    static const int held = resident(k_layer_norm_grad<T, V, EL, true, true>, 0);
+    g.way = Way::LANES;
+    g.split = lanes_of(a.d, EL);
+    g.threads = THREADS;
+    g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held);
+  } else if (a.d <= MOST_WARPS * 32 * E) {
+    static const Residency held(k_layer_norm_grad<T, V, E, false, true>, E, [](int) { return (size_t)0; });
     g.way = Way::FETCH;
-    g.whole = is_whole<T, V, E>(a.d);
-    g.split = split_of(a.d, E, &g.threads);
+    g.split = warps_of(a.d, E, &g.threads);
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held.blocks[g.split.W]);
   } else if (E < 16 && a.d <= MOST_WARPS * 32 * 16) {
     g.way = Way::PLAIN;
-    g.split = split_of(a.d, 16, &g.threads);
+    g.split = warps_of(a.d, 16, &g.threads);
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, 1);
   } else {
     g.way = Way::WIDE;
@@ -693,7 +728,7 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
 
 template <typename T, int V>
 cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int E = E_GRAD<T, V>;
+  constexpr int EL = E_LANES<V>, E = E_GRAD<T, V>;
   const GradShape g = grad_shape<T, V>(a, num_sms);
   cudaError_t e;
   if (g.way == Way::WIDE) {
@@ -704,9 +739,7 @@ cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
       e = launch_following(k_layer_norm_grad_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 4)),
                            WIDE_GRAD_THREADS, 0, s, a);
   } else {
-    auto kernel = k_layer_norm_grad<T, V, E, true, false>;
-    if constexpr (V * sizeof(T) == 16)
-      if (g.whole) kernel = k_layer_norm_grad<T, V, E, true, true>;
+    auto kernel = g.way == Way::LANES ? k_layer_norm_grad<T, V, EL, true, true> : k_layer_norm_grad<T, V, E, false, true>;
     if constexpr (E < 16)
       if (g.way == Way::PLAIN) kernel = k_layer_norm_grad<T, V, 16, false, false>;
     e = launch_following(kernel, dim3(g.parts), g.threads, 0, s, a, g.split);
