@@ -18,10 +18,10 @@
 //    occur are cleared by the same kernel, so that every row is written once;
 //  - merge: a warp per cut run and slab, or a block where the run has many items, adds the
 //    items' sums in their order.
-// The items of a hot row follow one another through a lane group, so their length bounds
-// the time of small calls, and their sums' traffic that of large ones: c is 16 for up to
-// 65,536 positions (a message of 6,656 x 16 floats, kernel of the sums: 24.7 us with 64) and
-// 64 above.
+// The rows of an item follow one another through a lane group, so the length of a hot row's
+// items bounds the time of small calls, and their sums' traffic that of large ones: c is 16
+// for gradients of up to 2^26 elements (a message of 6,656 x 16 floats, kernel of the sums:
+// 7.8 us, and 24.7 with 64), 64 above.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -36,11 +36,11 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int SUM_BLOCKS = 4, MERGE_BLOCKS = 3;  // of k_token_sums and k_token_merge, that an SM holds
+constexpr int MERGE_THREADS = 512, MERGE_BLOCKS = 1;
 constexpr int64_t SMALL_N = 8192;  // that k_token_small takes
 constexpr uint32_t LONG_PARTS = 16;
 constexpr int MIN_CUT_LG = 4, MAX_CUT_LG = 6;
-inline int cut_lg_of(int64_t n) { return n <= 65536 ? MIN_CUT_LG : MAX_CUT_LG; }
+inline int cut_lg_of(int64_t n, int64_t d) { return n * d <= 1ll << 26 ? MIN_CUT_LG : MAX_CUT_LG; }
 constexpr int ITEM_TILE = 2048;  // sorted positions per tile of the item scan
 constexpr int MAX_RADIX = 512;   // of a sort pass
 
@@ -60,17 +60,79 @@ __device__ __forceinline__ uint32_t lanemask_lt() {
 
 // ---- lookup -----------------------------------------------------------------------
 
+// The lanes of the group of 1 << lg that this lane is in.
+__device__ __forceinline__ uint32_t group_mask(int lg) {
+  const uint32_t first = (threadIdx.x & 31) >> lg << lg;
+  return lg == 5 ? FULL : ((1u << (1 << lg)) - 1u) << first;
+}
+
+// Writes a lane group's values x, V consecutive ones a lane, to the n elements that exist from
+// `to` on (ADD: adds them), neighbouring lanes to neighbouring elements: the lanes' values
+// change places through shared memory.  For outputs whose rows do not start on the boundary
+// that vectors need.
+template <typename T, int V, bool ADD>
+__device__ __forceinline__ void write_in_order(float* swap, const float (&x)[V], int lg, int64_t n, T* to) {
+  const uint32_t mask = group_mask(lg);
+  const int L = 1 << lg, l = threadIdx.x & (L - 1);
+  float* mine = swap + (threadIdx.x >> lg << lg) * V;  // the group's
+  __syncwarp(mask);
+#pragma unroll
+  for (int j = 0; j < V; j += 4)
+    *reinterpret_cast<float4*>(mine + l * V + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+  __syncwarp(mask);
+  const int count = n < L * V ? (int)n : L * V;
+  if constexpr (sizeof(T) == 4) {
+    mine += l;
+    to += l;
+    if (count == 32 * V) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) to[i * 32] = ADD ? to[i * 32] + mine[i * 32] : mine[i * 32];
+    } else {
+      for (int e = 0; e + l < count; e += L) to[e] = ADD ? to[e] + mine[e] : mine[e];
+    }
+  } else {  // in pairs from the first 4-byte boundary on
+    static_assert(!ADD, "");
+    const int odd = (int)((uintptr_t)to >> 1 & 1), pairs = (count - odd) >> 1;
+    if (odd && l == 0) to[0] = from_float<T>(mine[0]);
+    if (odd + 2 * pairs < count && l == L - 1) to[count - 1] = from_float<T>(mine[count - 1]);
+    mine += odd + 2 * l;
+    to += odd + 2 * l;
+    auto put = [&](int e) {
+      const float y[2] = {mine[e], mine[e + 1]};
+      Pack<T, 2> o;
+      o.set(y);
+      o.store(to + e);
+    };
+    if (pairs >= 16 * V - 1 && lg == 5) {  // all of them, but for the last where the first is odd
+#pragma unroll
+      for (int i = 0; i < V / 2 - 1; ++i) put(i * 64);
+      if ((V / 2 - 1) * 32 + l < pairs) put((V / 2 - 1) * 64);
+    } else {
+      for (int q = l; q < pairs; q += L) put(2 * (q - l));
+    }
+  }
+}
+
+// Which rows may start anywhere, or not be whole numbers of vectors: none, the input's, or the
+// output's as well.
+enum Rows { EVEN, LOOSE_IN, LOOSE };
+
 // A lane group of 1 << lg lanes per token and slab of K * V columns a lane.
-template <typename TI, typename TO, int V, int K>
+template <typename TI, typename TO, int V, int K, Rows R>
 __global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
+  __shared__ __align__(16) float swap[R == LOOSE ? THREADS * V : 4];
   follow();
   const int L = 1 << lg;
   const int l = threadIdx.x & (L - 1);
   const int64_t groups = (int64_t)gridDim.x * (THREADS >> lg);
   const int64_t g0 = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> lg;
   const int64_t c0 = ((int64_t)blockIdx.y * K * L + l) * V;
+  const char* lo = static_cast<const char*>(a.w);
+  const char* hi = lo + ((uint64_t)(a.V - 1) * (uint64_t)a.w_stride + (uint64_t)a.d) * sizeof(TI);
+  int64_t next = g0 < a.n ? a.ids[g0] : 0;
   for (int64_t i = g0; i < a.n; i += groups) {
-    const int64_t id = a.ids[i];
+    const int64_t id = next;
+    if (i + groups < a.n) next = a.ids[i + groups];
     bool zero = id == a.pad_id && a.pad_id != GBA_NO_PAD;
     bool fresh = false;  // HASH: an id never seen has its initial values
     uint64_t row = 0;
@@ -95,23 +157,24 @@ __global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
     }
     const TI* src = static_cast<const TI*>(a.w) + row * (uint64_t)a.w_stride;
     TO* dst = static_cast<TO*>(a.out) + (uint64_t)i * (uint64_t)a.out_stride;
-    Pack<TI, V> in[K];
+    std::conditional_t<R != EVEN, Loose<TI>, Pack<TI, V>> in[K];
     if (!zero && !fresh) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int64_t c = c0 + (int64_t)k * L * V;
-        if (c < a.d) in[k].load(src + c);
+        if (c >= a.d) continue;
+        if constexpr (R != EVEN)
+          in[k].load(src + c, a.d - c, lo, hi);
+        else
+          in[k].load(src + c);
       }
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int64_t c = c0 + (int64_t)k * L * V;
-      if (c >= a.d) continue;
-      float x[V];
-      if (zero) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) x[j] = 0.f;
-      } else {
+      if (c - l * V >= a.d || (R != LOOSE && c >= a.d)) continue;  // of the group, or of the lane
+      float x[V] = {};
+      if (!zero && c < a.d) {
         if (fresh) {
 #pragma unroll
           for (int j = 0; j < V; ++j)
@@ -122,39 +185,45 @@ __global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] *= a.scale;
       }
-      Pack<TO, V> o;
-      o.set(x);
-      o.store(dst + c);
+      if constexpr (R == LOOSE) {
+        write_in_order<TO, V, false>(swap, x, lg, a.d - (c - l * V), dst + (c - l * V));
+      } else {
+        Pack<TO, V> o;
+        o.set(x);
+        o.store(dst + c);
+      }
     }
   }
 }
 
-template <typename TI, typename TO, int V>
+template <typename TI, typename TO, int V, Rows R>
 cudaError_t embed_as(const EmbedArgs& a, int num_sms, cudaStream_t s) {
   const int64_t pieces = (a.d + V - 1) / V;
   int lg = 0;
   while ((1 << lg) < pieces && lg < 5) ++lg;
-  constexpr int K = 4;
-  // four pieces a lane in flight, unless that leaves SMs without work
-  const bool wide = a.n * pieces / (32 * K) >= (int64_t)num_sms * 16;
-  const int64_t slab = (int64_t)(wide ? K : 1) << lg;
-  const int64_t slabs = (pieces + slab - 1) / slab;
+  const int64_t each = (pieces + (1 << lg) - 1) >> lg;  // of a lane
+  // up to four pieces a lane in flight, unless that leaves SMs without work
+  const bool wide = a.n * pieces / 128 >= (int64_t)num_sms * 16;
+  const int64_t slabs = wide ? (each + 3) / 4 : each;
   const int64_t blocks = (a.n + (THREADS >> lg) - 1) / (THREADS >> lg);
   const dim3 grid((unsigned)std::min<int64_t>(blocks, (int64_t)num_sms * 32), (unsigned)slabs);
-  return wide ? launch_following(k_embed<TI, TO, V, K>, grid, THREADS, 0, s, a, lg)
-              : launch_following(k_embed<TI, TO, V, 1>, grid, THREADS, 0, s, a, lg);
+  auto kernel = k_embed<TI, TO, V, 1, R>;
+  switch ((each + slabs - 1) / slabs) {
+    case 2: kernel = k_embed<TI, TO, V, 2, R>; break;
+    case 3: kernel = k_embed<TI, TO, V, 3, R>; break;
+    case 4: kernel = k_embed<TI, TO, V, 4, R>; break;
+  }
+  return launch_following(kernel, grid, THREADS, 0, s, a, lg);
 }
 
+// Vectors of 8 elements, or of 4 float32; loose rows by 16 bytes of the input.
 template <typename TI, typename TO>
 cudaError_t embed_types(const EmbedArgs& a, int num_sms, cudaStream_t s) {
-  constexpr int most = 16 / (int)std::min(sizeof(TI), sizeof(TO));
-  const int v = std::min(vector_of(most, a.w, a.w_stride, a.d, sizeof(TI)),
-                         vector_of(most, a.out, a.out_stride, a.d, sizeof(TO)));
-  if constexpr (most == 8)
-    if (v == 8) return embed_as<TI, TO, 8>(a, num_sms, s);
-  if (v == 4) return embed_as<TI, TO, 4>(a, num_sms, s);
-  if (v == 2) return embed_as<TI, TO, 2>(a, num_sms, s);
-  return embed_as<TI, TO, 1>(a, num_sms, s);
+  constexpr int V = 16 / (int)std::min(sizeof(TI), sizeof(TO)), VL = Loose<TI>::V;
+  if (vector_of(V, a.w, a.w_stride, a.d, sizeof(TI)) == V && vector_of(V, a.out, a.out_stride, a.d, sizeof(TO)) == V)
+    return embed_as<TI, TO, V, EVEN>(a, num_sms, s);
+  if (vector_of(VL, a.out, a.out_stride, a.d, sizeof(TO)) == VL) return embed_as<TI, TO, VL, LOOSE_IN>(a, num_sms, s);
+  return embed_as<TI, TO, VL, LOOSE>(a, num_sms, s);
 }
 
 // ---- gradient: workspace -------------------------------------------------------------
@@ -186,6 +255,9 @@ struct GradPlan {
   bool small;  // keys, sort and items by one cluster
 };
 
+// Floats from one item's sum to the next: vectors of them are aligned, whatever the width.
+__host__ __device__ __forceinline__ uint64_t part_stride(int64_t d) { return ((uint64_t)d + 7) / 8 * 8; }
+
 GradPlan plan_of(const EmbedGradArgs& a) {
   GradPlan p{};
   const uint64_t top = (uint64_t)a.V;  // the key that stands for padding
@@ -195,7 +267,7 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.small = a.n <= SMALL_N && (!a.dense || a.accumulate || a.V <= 1 << 22);
   p.sort = make_sort_plan(bits, 9);
   p.tiles = (a.n + ITEM_TILE - 1) / ITEM_TILE;
-  p.cut_lg = cut_lg_of(a.n);
+  p.cut_lg = cut_lg_of(a.n, a.d);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -217,7 +289,7 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.run_row = take(n * 4);
   p.run_start = take(n * 4);
   p.cuts = take(2 * ((n >> p.cut_lg) + 1) * 8);
-  p.parts = take((2 * (n >> p.cut_lg) + 2) * (size_t)a.d * 4);
+  p.parts = take((2 * (n >> p.cut_lg) + 2) * part_stride(a.d) * 4);
   p.bytes = at;
   return p;
 }
@@ -630,23 +702,27 @@ struct SumArgs {
   int64_t V;
 };
 
+// Where run's sum goes, from column c on.
+__device__ __forceinline__ float* sum_at(const SumArgs& a, uint32_t run, int64_t c) {
+  return a.out + (uint64_t)(a.ids_out ? run : a.run_row[run]) * (uint64_t)a.out_stride + c;
+}
+
 template <int V>
-__device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t run, int64_t c, float (&x)[V]) {
-  const uint64_t row = a.ids_out ? run : a.run_row[run];
-  float* dst = a.out + row * (uint64_t)a.out_stride + c;
-#pragma unroll
-  for (int j = 0; j < V; ++j) x[j] *= a.scale;
+__device__ __forceinline__ void write_sum(const SumArgs& a, float* dst, const float (&x)[V]) {
+  float y[V] = {};
   Pack<float, V> o;
   if (a.accumulate) {
-    float y[V];
     o.load(dst);
     o.get(y);
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] += y[j];
   }
-  o.set(x);
+#pragma unroll
+  for (int j = 0; j < V; ++j) y[j] = a.accumulate ? y[j] + x[j] * a.scale : x[j] * a.scale;
+  o.set(y);
   o.store(dst);
 }
+
+template <Rows R>
+constexpr int SUM_BLOCKS = R == EVEN ? 4 : 3;  // of k_token_sums, that an SM holds
 
 // A lane group of 1 << lg lanes per item and slab of V columns a lane, the slabs of an item
 // side by side.  A group takes every so-many-th item and adds its gradient rows in ascending
@@ -656,9 +732,11 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t run, int64_
 // slots that no row needs, or the rows of the dense form that do not occur.  Of the latter
 // they claim `claim` at a time: which warp clears a row changes no value, and it evens out
 // what hot rows leave uneven (262,144 x 2048 bf16 into 131,072 rows: 427 us with equal shares).
-template <typename T, int V>
-__global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, int lg, int slabs, int claim, ErrSink err) {
-  constexpr int U = 4;
+template <typename T, Rows R>
+__global__ void __launch_bounds__(THREADS, SUM_BLOCKS<R>)
+    k_token_sums(SumArgs a, int lg, int slabs, int claim, ErrSink err) {
+  constexpr int U = 4, V = 16 / (int)sizeof(T);
+  __shared__ __align__(16) float swap[R == LOOSE ? THREADS * V : 4];
   follow();
   const bool failed = *(const volatile uint32_t*)err.step != 0u;
   const uint32_t n_items = failed ? 0u : a.ctr->n_items, n_runs = failed ? 0u : a.ctr->n_runs, P = a.ctr->P;
@@ -671,6 +749,8 @@ __global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, i
   const int64_t c = ((int64_t)slab * L + l) * V;
   const bool in = c < a.d;
   const T* grad = static_cast<const T*>(a.grad) + c;
+  const char* lo = static_cast<const char*>(a.grad);
+  const char* hi = lo + ((uint64_t)(a.n - 1) * (uint64_t)a.stride + (uint64_t)a.d) * sizeof(T);
 
   // the item being added, its positions [p, e), and the places of the next U of them
   uint32_t unit = stream < streams ? stream : n_items, p = 0, e = 0, next_e = 0;
@@ -688,16 +768,20 @@ __global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, i
 #pragma unroll
   for (int i = 0; i < U; ++i)
     if (p + i < e) at[i] = a.order[p + i];
-  float x[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) x[j] = 0.f;
+  float x[V] = {};
   while (unit < n_items) {
-    Pack<T, V> g[U];
+    std::conditional_t<R != EVEN, Loose<T>, Pack<T, V>> g[U];
 #pragma unroll
-    for (int i = 0; i < U; ++i)
-      if (in && p + i < e) g[i].load(grad + (uint64_t)at[i] * (uint64_t)a.stride);
-    const uint32_t left = e - p;
-    const bool more = left > (uint32_t)U;
+    for (int i = 0; i < U; ++i) {
+      if (!in || p + i >= e) continue;
+      const T* from = grad + (uint64_t)at[i] * (uint64_t)a.stride;
+      if constexpr (R != EVEN)
+        g[i].load(from, a.d - c, lo, hi);
+      else
+        g[i].load(from);
+    }
+    const uint32_t here = e - p;
+    const bool more = here > (uint32_t)U;
     const uint32_t p1 = more ? p + U : next.start >> 1, e1 = more ? e : next_e;
 #pragma unroll
     for (int i = 0; i < U; ++i)
@@ -707,24 +791,30 @@ __global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, i
     if (!more) item_at((uint64_t)unit + 2ull * streams, after, after_e);
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if ((uint32_t)i < left) {
+      if (in && (uint32_t)i < here) {
         float y[V];
         g[i].get(y);
 #pragma unroll
         for (int j = 0; j < V; ++j) x[j] += y[j];
       }
     if (!more) {
-      if (in) {
-        if (it.run & 1u) {
-          // the item before the first cut, or the one that starts at a cut
-          const uint32_t up = ((it.start >> 1) + (1u << a.cut_lg) - 1u) >> a.cut_lg;
-          const uint32_t slot = it.start & 1u ? 2u * (up + 1u) : 2u * up + 1u;
-          Pack<float, V> o;
-          o.set(x);
-          o.store(a.parts + (uint64_t)slot * (uint64_t)a.d + c);
-        } else {
-          write_sum<V>(a, it.run >> 1, c, x);
-        }
+      if (it.run & 1u) {
+        // the item before the first cut, or the one that starts at a cut
+        const uint32_t up = ((it.start >> 1) + (1u << a.cut_lg) - 1u) >> a.cut_lg;
+        const uint32_t slot = it.start & 1u ? 2u * (up + 1u) : 2u * up + 1u;
+        Pack<float, V> o;
+        o.set(x);
+        if (in) o.store(a.parts + (uint64_t)slot * part_stride(a.d) + c);
+      } else if constexpr (R == LOOSE) {
+        const int64_t group_column = c - l * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j) x[j] *= a.scale;
+        if (a.accumulate)
+          write_in_order<float, V, true>(swap, x, lg, a.d - group_column, sum_at(a, it.run >> 1, group_column));
+        else
+          write_in_order<float, V, false>(swap, x, lg, a.d - group_column, sum_at(a, it.run >> 1, group_column));
+      } else if (in) {
+        write_sum<V>(a, sum_at(a, it.run >> 1, c), x);
       }
 #pragma unroll
       for (int j = 0; j < V; ++j) x[j] = 0.f;
@@ -740,10 +830,11 @@ __global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, i
   if (rest == 0) return;
   __syncwarp();
   const int lane = threadIdx.x & 31;
-  const Pack<float, V> zero{};
+  constexpr int VZ = R == LOOSE ? 1 : V;
+  const Pack<float, VZ> zero{};
   auto clear = [&](uint64_t row) {
     float* dst = a.out + row * (uint64_t)a.out_stride;
-    for (int64_t q = (int64_t)l * V; q < a.d; q += L * V) zero.store(dst + q);
+    for (int64_t q = (int64_t)l * VZ; q < a.d; q += L * VZ) zero.store(dst + q);
   };
   if (a.ids_out) {
     const int64_t id = n_runs > 0 ? (int64_t)a.run_row[n_runs - 1] : -1;
@@ -759,41 +850,61 @@ __global__ void __launch_bounds__(THREADS, SUM_BLOCKS) k_token_sums(SumArgs a, i
     const uint64_t first = (uint64_t)__shfl_sync(FULL, mine, 0) * (uint64_t)claim;
     if (first >= rest) break;
     const uint64_t last = first + claim < rest ? first + claim : rest;
-    for (uint64_t row = first + (lane >> lg); row < last; row += 32 >> lg)
-      if (failed || !(a.present[row >> 5] >> (row & 31u) & 1u)) clear(row);
+    for (uint64_t row = first; row < last; row = (row | 31u) + 1u) {  // those of one word of presence
+      const uint32_t there = failed ? 0u : a.present[row >> 5] >> (row & 31u);
+      const uint32_t rows = (uint32_t)min((uint64_t)(32u - (uint32_t)(row & 31u)), last - row);
+      for (uint32_t i = lane >> lg; i < rows; i += 32u >> lg)
+        if (!(there >> i & 1u)) clear(row + i);
+    }
   }
 }
 
-// Adds the sums lo .. hi - 1 of a cut run's items to x, at columns c .. c + V - 1, in order.
+// Adds the sums lo .. hi - 1 of a cut run's items to x, at columns c .. c + 3, in order.
 // Compensated, so that a row of a million tokens is as exact as one of a hundred.
-template <int V>
 __device__ __forceinline__ void add_parts(const SumArgs& a, uint32_t first_cut, uint32_t lo, uint32_t hi, int64_t c,
-                                          CSum (&x)[V]) {
+                                          CSum (&x)[4]) {
   constexpr int U = 8;
+  if (c >= a.d) return;
   for (uint32_t k = lo; k < hi; k += U) {
-    Pack<float, V> g[U];
+    Pack<float, 4> g[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const uint64_t slot = 2ull * (first_cut >> a.cut_lg) + (k + i == 0 ? 0u : 2u * (k + i) - 1u);
-      if (k + i < hi) g[i].load(a.parts + slot * (uint64_t)a.d + c);
+      if (k + i < hi) g[i].load(a.parts + slot * part_stride(a.d) + c);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       if (k + i >= hi) continue;
-      float y[V];
+      float y[4];
       g[i].get(y);
 #pragma unroll
-      for (int j = 0; j < V; ++j) csum_add(x[j], y[j]);
+      for (int j = 0; j < 4; ++j) csum_add(x[j], y[j]);
     }
   }
 }
 
-// Cut runs, in slabs of 32 * V columns: those of many items by a block each, whose warps add a
+// aligned: rows of the output start on 16 bytes and are whole numbers of them.
+__device__ __forceinline__ void write_parts(const SumArgs& a, uint32_t run, int64_t c, const CSum (&x)[4],
+                                            bool aligned) {
+  if (c >= a.d) return;
+  float* dst = sum_at(a, run, c);
+  float y[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) y[j] = csum_value(x[j]);
+  if (aligned) {
+    write_sum<4>(a, dst, y);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < a.d) dst[j] = a.accumulate ? dst[j] + y[j] * a.scale : y[j] * a.scale;
+}
+
+// Cut runs, in slabs of 128 columns: those of many items by a block each, whose warps add a
 // share of the items' sums each and then the shares in order; then the others by a warp each.
-template <int V>
-__global__ void __launch_bounds__(THREADS, MERGE_BLOCKS) k_token_merge(SumArgs a, int slabs, ErrSink err) {
-  constexpr int WARPS = THREADS / 32;
-  __shared__ float s_hi[WARPS][32 * V], s_lo[WARPS][32 * V];
+__global__ void __launch_bounds__(MERGE_THREADS) k_token_merge(SumArgs a, int slabs, int aligned, ErrSink err) {
+  constexpr int WARPS = MERGE_THREADS / 32;
+  __shared__ float s_hi[WARPS][128], s_lo[WARPS][128];
   follow();
   if (*(const volatile uint32_t*)err.step != 0u) return;
   const uint32_t n_runs = a.ctr->n_runs, P = a.ctr->P, room = (a.n >> a.cut_lg) + 1u;
@@ -806,48 +917,38 @@ __global__ void __launch_bounds__(THREADS, MERGE_BLOCKS) k_token_merge(SumArgs a
   };
   for (uint64_t i = blockIdx.x; i < (uint64_t)n_long * slabs; i += gridDim.x) {
     const uint2 cut = a.cuts[room + i / slabs];
-    const int64_t c = ((int64_t)(i % slabs) * 32 + lane) * V;
+    const int64_t c = (int64_t)(i % slabs) * 128 + lane * 4;
     const uint32_t parts = parts_of(cut), each = (parts + WARPS - 1) / WARPS;
     const uint32_t lo = min(parts, warp * each), hi = min(parts, lo + each);
-    CSum x[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = CSum{0.f, 0.f};
-    if (c < a.d) add_parts<V>(a, cut.y, lo, hi, c, x);
+    CSum x[4] = {};
+    add_parts(a, cut.y, lo, hi, c, x);
     __syncthreads();  // the block is done with the run before
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      s_hi[warp][lane * V + j] = x[j].hi;
-      s_lo[warp][lane * V + j] = x[j].lo;
+    for (int j = 0; j < 4; ++j) {
+      s_hi[warp][lane * 4 + j] = x[j].hi;
+      s_lo[warp][lane * 4 + j] = x[j].lo;
     }
     __syncthreads();
-    if (warp == 0 && c < a.d) {
+    if (warp == 0) {
       for (int w = 1; w < WARPS; ++w)
 #pragma unroll
-        for (int j = 0; j < V; ++j) csum_merge(x[j], s_hi[w][lane * V + j], s_lo[w][lane * V + j]);
-      float y[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) y[j] = csum_value(x[j]);
-      write_sum<V>(a, cut.x, c, y);
+        for (int j = 0; j < 4; ++j) csum_merge(x[j], s_hi[w][lane * 4 + j], s_lo[w][lane * 4 + j]);
+      write_parts(a, cut.x, c, x, aligned);
     }
   }
   for (uint64_t i = (uint64_t)blockIdx.x * WARPS + warp; i < (uint64_t)n_short * slabs;
        i += (uint64_t)gridDim.x * WARPS) {
     const uint2 cut = a.cuts[i / slabs];
-    const int64_t c = ((int64_t)(i % slabs) * 32 + lane) * V;
-    if (c >= a.d) continue;
-    CSum x[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = CSum{0.f, 0.f};
-    add_parts<V>(a, cut.y, 0u, parts_of(cut), c, x);
-    float y[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = csum_value(x[j]);
-    write_sum<V>(a, cut.x, c, y);
+    const int64_t c = (int64_t)(i % slabs) * 128 + lane * 4;
+    CSum x[4] = {};
+    add_parts(a, cut.y, 0u, parts_of(cut), c, x);
+    write_parts(a, cut.x, c, x, aligned);
   }
 }
 
-template <typename T, int V>
+template <typename T, Rows R>
 cudaError_t sums_as(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) {
+  constexpr int V = 16 / (int)sizeof(T);
   const int64_t pieces = (a.d + V - 1) / V;
   int lg = 0;
   while ((1 << lg) < pieces && lg < 5) ++lg;
@@ -855,29 +956,26 @@ cudaError_t sums_as(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) 
   const int64_t units = ((int64_t)a.n + (a.n >> a.cut_lg) + (a.present ? a.V : 0)) * slabs;
   const int64_t blocks = (units + (THREADS >> lg) - 1) / (THREADS >> lg);
   const int64_t least = (slabs + (THREADS >> lg) - 1) / (THREADS >> lg);  // that hold one item
-  const int64_t most = std::max<int64_t>(least, (int64_t)num_sms * SUM_BLOCKS);
-  const int claim = (int)std::max<int64_t>(32 >> lg, 32768 / ((int64_t)a.d * 4));  // rows of about 32 KB
-  const cudaError_t e = launch_following(k_token_sums<T, V>, dim3((unsigned)std::min(blocks, most)), THREADS, 0, s, a,
-                                         lg, (int)slabs, claim, err);
+  const int64_t grid = std::min(blocks, std::max<int64_t>(least, (int64_t)num_sms * SUM_BLOCKS<R>));
+  // claims of up to 16 KB, of which every warp finds several
+  int claim = 32 >> lg;
+  while ((int64_t)claim * 2 * a.d * 4 <= 16384 && (int64_t)claim * 2 * 4 * grid * (THREADS / 32) <= a.V) claim *= 2;
+  const cudaError_t e = launch_following(k_token_sums<T, R>, dim3((unsigned)grid), THREADS, 0, s, a, lg,
+                                         (int)slabs, claim, err);
   if (e != cudaSuccess || a.n <= 1u << a.cut_lg) return e;  // no run can be cut
-  constexpr int VM = V < 4 ? V : 4;  // the sums are float32
-  const int64_t mpieces = (a.d + VM - 1) / VM;
-  const int64_t mslabs = (mpieces + 31) / 32;
-  const int64_t mblocks = ((a.n >> a.cut_lg) * mslabs + THREADS / 32 - 1) / (THREADS / 32);
-  return launch_following(k_token_merge<VM>, dim3((unsigned)std::min<int64_t>(mblocks, num_sms * MERGE_BLOCKS)),
-                          THREADS, 0, s, a, (int)mslabs, err);
+  const int64_t mslabs = (a.d + 127) / 128;
+  const int64_t mblocks = ((a.n >> a.cut_lg) * mslabs + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
+  const int aligned = vector_of(4, a.out, a.out_stride, a.d, 4) == 4;
+  return launch_following(k_token_merge, dim3((unsigned)std::min<int64_t>(mblocks, num_sms * MERGE_BLOCKS)),
+                          MERGE_THREADS, 0, s, a, (int)mslabs, aligned, err);
 }
 
 template <typename T>
 cudaError_t sums_type(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) {
-  constexpr int most = 16 / (int)sizeof(T);
-  const int v = std::min(vector_of(most, a.grad, a.stride, a.d, sizeof(T)),
-                         vector_of(most, a.out, a.out_stride, a.d, 4));
-  if constexpr (most == 8)
-    if (v == 8) return sums_as<T, 8>(a, err, num_sms, s);
-  if (v == 4) return sums_as<T, 4>(a, err, num_sms, s);
-  if (v == 2) return sums_as<T, 2>(a, err, num_sms, s);
-  return sums_as<T, 1>(a, err, num_sms, s);
+  constexpr int V = 16 / (int)sizeof(T);
+  if (vector_of(V, a.out, a.out_stride, a.d, 4) != V) return sums_as<T, LOOSE>(a, err, num_sms, s);
+  return vector_of(V, a.grad, a.stride, a.d, sizeof(T)) == V ? sums_as<T, EVEN>(a, err, num_sms, s)
+                                                            : sums_as<T, LOOSE_IN>(a, err, num_sms, s);
 }
 
 }  // namespace

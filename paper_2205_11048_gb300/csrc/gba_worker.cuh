@@ -80,6 +80,48 @@ struct Pack {
   }
 };
 
+// 16 bytes of a matrix from an address that is only aligned to its type, by the two aligned
+// words that hold them, brought into place when they are used.  Rows of odd widths are read
+// so: by single elements a warp would fetch 64 bytes at a time.
+template <typename T>
+struct Loose {
+  static constexpr int V = 16 / (int)sizeof(T);
+  uint4 w[2];
+  uint32_t shift;  // bytes
+  // n of the elements exist, at least one; words outside the matrix's bytes [lo, hi) are not touched.
+  __device__ __forceinline__ void load(const T* p, int64_t n, const char* lo, const char* hi) {
+    const uintptr_t at = (uintptr_t)p, base = at & ~(uintptr_t)15;
+    if (base >= (uintptr_t)lo && base + 32 <= (uintptr_t)hi) {
+      shift = (uint32_t)(at & 15);
+      w[0] = reinterpret_cast<const uint4*>(base)[0];
+      w[1] = reinterpret_cast<const uint4*>(base)[1];
+    } else {
+      T t[V] = {};
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < n) t[j] = p[j];
+      shift = 0;
+      memcpy(w, t, sizeof t);
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[V]) const {
+    uint32_t v[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+    if (shift & 8)
+#pragma unroll
+      for (int k = 0; k < 6; ++k) v[k] = v[k + 2];
+    if (shift & 4)
+#pragma unroll
+      for (int k = 0; k < 5; ++k) v[k] = v[k + 1];
+    if constexpr (sizeof(T) == 2)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = __funnelshift_r(v[k], v[k + 1], (shift & 2) * 8);
+    T t[V];
+    memcpy(t, v, sizeof t);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = to_float(t[j]);
+  }
+};
+
 // The most elements (a power of two, at most `most`) that an access may take of rows of
 // `cols` elements of `bytes` each, `stride` apart from `p` on.
 inline int vector_of(int most, const void* p, int64_t stride, int64_t cols, size_t bytes) {
