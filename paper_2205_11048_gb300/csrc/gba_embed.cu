@@ -16,8 +16,8 @@
 //    (in slots that follow from the cut's position: 2 p / c for the item before the first
 //    cut p, one more for the item that starts at p).  Rows of a dense output that do not
 //    occur are cleared by the same kernel, so that every row is written once;
-//  - merge: a warp per cut run and slab, or a block where the run has many items, adds the
-//    items' sums in their order.
+//  - merge: a warp per cut run and slab, or one or several blocks where the run has many
+//    items, adds the items' sums in their order.
 // The rows of an item follow one another through a lane group, so the length of a hot row's
 // items bounds the time of small calls, and their sums' traffic that of large ones: c is 16
 // for gradients of up to 2^26 elements (a message of 6,656 x 16 floats, kernel of the sums:
@@ -36,9 +36,9 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr uint32_t FULL = 0xffffffffu;
-constexpr int MERGE_THREADS = 512, MERGE_BLOCKS = 1;
+constexpr int MERGE_THREADS = 512, HUGE_SPLIT = 8;
 constexpr int64_t SMALL_N = 8192;  // that k_token_small takes
-constexpr uint32_t LONG_PARTS = 16;
+constexpr uint32_t LONG_PARTS = 16, HUGE_PARTS = 256;
 constexpr int MIN_CUT_LG = 4, MAX_CUT_LG = 6;
 inline int cut_lg_of(int64_t n, int64_t d) { return n * d <= 1ll << 26 ? MIN_CUT_LG : MAX_CUT_LG; }
 constexpr int ITEM_TILE = 2048;  // sorted positions per tile of the item scan
@@ -233,10 +233,10 @@ struct Counters {
   uint32_t tickets[MAX_PASSES];
   uint32_t scan_ticket;
   uint32_t n_items, n_runs;
-  uint32_t n_cut[2];  // cut runs of a few items, and of more than LONG_PARTS
+  uint32_t n_cut[3];  // cut runs of a few items, of LONG_PARTS and more, of HUGE_PARTS and more
   uint32_t P;        // positions that are no padding: the first P of the sorted ones
   uint32_t rest;     // claims of the rows that are cleared
-  uint32_t pad[4];
+  uint32_t pad[3];
 };
 static_assert(sizeof(Counters) == 64, "the histograms follow it");
 
@@ -248,9 +248,9 @@ struct Item {
 // Where the parts of the workspace are; what must start at zero comes first.
 struct GradPlan {
   SortPlan sort;
-  size_t counters, hist, sort_status, scan_status, present, cleared;  // cleared: bytes from 0 on
-  size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, bytes;
-  int64_t tiles;
+  size_t counters, hist, sort_status, scan_status, present, huge_done, cleared;  // cleared: bytes from 0 on
+  size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, huge, bytes;
+  int64_t tiles, n_huge_done;
   int cut_lg;
   bool small;  // keys, sort and items by one cluster
 };
@@ -280,6 +280,8 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.sort_status = take(sort_status_words(a.n, p.sort.radix) * 8);
   p.scan_status = take((size_t)p.tiles * 8);
   p.present = take(a.dense && !a.accumulate ? ((size_t)a.V + 31) / 32 * 4 : 0);
+  const size_t huge_units = ((size_t)(a.n >> p.cut_lg) / HUGE_PARTS + 1) * (((size_t)a.d + 127) / 128);
+  p.huge_done = take(huge_units * 4);
   p.cleared = at;
   for (int i = 0; i < 2; ++i) {
     p.keys[i] = take(n * 4);
@@ -288,8 +290,10 @@ GradPlan plan_of(const EmbedGradArgs& a) {
   p.items = take(n * sizeof(Item));
   p.run_row = take(n * 4);
   p.run_start = take(n * 4);
-  p.cuts = take(2 * ((n >> p.cut_lg) + 1) * 8);
+  p.cuts = take(3 * ((n >> p.cut_lg) + 1) * 8);
   p.parts = take((2 * (n >> p.cut_lg) + 2) * part_stride(a.d) * 4);
+  p.huge = take(huge_units * HUGE_SPLIT * 64 * sizeof(float4));
+  p.n_huge_done = (int64_t)huge_units;
   p.bytes = at;
   return p;
 }
@@ -354,17 +358,20 @@ struct ItemArgs {
   Item* items;
   uint32_t* run_row;
   uint32_t* run_start;
-  uint2* cuts;       // (run, first cut): [2][n >> cut_lg + 1]
+  uint2* cuts;       // (run, first cut): [3][n >> cut_lg + 1]
   int64_t* ids_out;  // message form
   uint32_t* present; // dense form, overwriting: a bit per row that occurs
   int32_t cut_lg;
+  uint32_t* huge_done;
+  int64_t n_huge_done;
 };
 
 // What stands at sorted position p < n.
 struct Marks {
   bool head, start;        // of a run, of an item
   bool several;            // the run has more items than this one
-  bool first_cut, is_long; // p is the run's first cut, and at least LONG_PARTS - 1 cuts follow the run's head
+  bool first_cut;          // p is the run's first cut
+  bool is_long, is_huge;   // and the run has LONG_PARTS items at least, HUGE_PARTS at least
   bool last;               // before the padding, or the end
 };
 __device__ __forceinline__ Marks marks_of(const ItemArgs& a, const uint32_t* keys, uint32_t p, uint32_t& key) {
@@ -378,7 +385,9 @@ __device__ __forceinline__ Marks marks_of(const ItemArgs& a, const uint32_t* key
   const uint32_t at_q = q < a.n ? keys[q] : ~0u;
   const uint32_t back = at_cut ? keys[p - cut] : ~0u;
   const uint32_t back2 = at_cut && p >= 2 * cut ? keys[p - 2 * cut] : ~0u;
+  const uint64_t farther = (uint64_t)p + ((uint64_t)(HUGE_PARTS - 1) << a.cut_lg);
   const uint32_t at_far = at_cut && far < a.n ? keys[far] : ~0u;
+  const uint32_t at_farther = at_cut && farther < a.n ? keys[farther] : ~0u;
   const bool real = key != a.pad_key;
   Marks m;
   m.head = real && key != before;
@@ -386,19 +395,20 @@ __device__ __forceinline__ Marks marks_of(const ItemArgs& a, const uint32_t* key
   m.several = !m.head || at_q == key;
   m.first_cut = !m.head && m.start && back2 != key;
   m.is_long = at_far == key;
+  m.is_huge = at_farther == key;
   m.last = real && after == a.pad_key;
   return m;
 }
 
 __device__ __forceinline__ void write_item(const ItemArgs& a, uint32_t p, uint32_t key, uint32_t item, uint32_t run,
-                                           bool head, bool several, bool first_cut, bool is_long) {
+                                           bool head, bool several, bool first_cut, bool is_long, bool is_huge) {
   if (head) {
     a.run_row[run] = key;
     a.run_start[run] = p;
     if (a.ids_out) a.ids_out[run] = (int64_t)key;
     if (a.present) atomicOr(a.present + (key >> 5), 1u << (key & 31u));
   } else if (first_cut) {
-    const uint32_t which = is_long ? 1u : 0u, room = (a.n >> a.cut_lg) + 1u;
+    const uint32_t which = is_huge ? 2u : is_long ? 1u : 0u, room = (a.n >> a.cut_lg) + 1u;
     const uint32_t c = atomicAdd(&a.ctr->n_cut[which], 1u);
     if (c < room) a.cuts[which * room + c] = make_uint2(run, p);
   }
@@ -428,7 +438,7 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
   const uint32_t tile = s_tile;
   const uint32_t base = tile * (uint32_t)ITEM_TILE + (uint32_t)(warp * PER_WARP);
 
-  uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS], several[ROUNDS], firsts[ROUNDS], longs[ROUNDS];
+  uint32_t key[ROUNDS], heads[ROUNDS], starts[ROUNDS], several[ROUNDS], firsts[ROUNDS], longs[ROUNDS], huges[ROUNDS];
   unsigned long long sum = 0ull;
 #pragma unroll
   for (int j = 0; j < ROUNDS; ++j) {  // every load of the tile before anything is written
@@ -444,6 +454,7 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
     several[j] = __ballot_sync(FULL, m.several);
     firsts[j] = __ballot_sync(FULL, m.first_cut);
     longs[j] = __ballot_sync(FULL, m.is_long);
+    huges[j] = __ballot_sync(FULL, m.is_huge);
     sum += (unsigned long long)__popc(starts[j]) << 30 | (unsigned long long)__popc(heads[j]);
   }
   if (lane == 0) s_warp[warp] = sum;
@@ -503,7 +514,7 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
     const uint32_t r = run + __popc(heads[j] & (lt | me)) - 1u;  // the run p belongs to
     if ((starts[j] & me) && at < a.n && r < a.n)  // the bounds hold unless a wait gave up
       write_item(a, p, key[j], at, r, (heads[j] & me) != 0u, (several[j] & me) != 0u, (firsts[j] & me) != 0u,
-                 (longs[j] & me) != 0u);
+                 (longs[j] & me) != 0u, (huges[j] & me) != 0u);
     item += __popc(starts[j]);
     run += __popc(heads[j]);
   }
@@ -550,6 +561,7 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
   if (me == 0 && tid == 0) *a.ctr = Counters{};
   if (a.present)
     for (int64_t i = base / I + tid; i < (ka.V + 31) / 32; i += CL_BLOCKS * CL_THREADS) a.present[i] = 0u;
+  for (int64_t i = base / I + tid; i < a.n_huge_done; i += CL_BLOCKS * CL_THREADS) a.huge_done[i] = 0u;
   const int any_bad = __syncthreads_or(bad);
   cluster.sync();  // every block has started: its shared memory may be written
   if (tid < CL_BLOCKS) cluster.map_shared_rank(s_bad, tid)[me] = any_bad ? 1u : 0u;
@@ -671,7 +683,8 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
     const uint32_t starts = __ballot_sync(FULL, m[j].start), heads = __ballot_sync(FULL, m[j].head);
     if (m[j].start)
       write_item(a, base + at + j * 32, key[j], item + __popc(starts & lt),
-                 run + __popc(heads & (lt | 1u << lane)) - 1u, m[j].head, m[j].several, m[j].first_cut, m[j].is_long);
+                 run + __popc(heads & (lt | 1u << lane)) - 1u, m[j].head, m[j].several, m[j].first_cut, m[j].is_long,
+                 m[j].is_huge);
     item += __popc(starts);
     run += __popc(heads);
   }
@@ -694,6 +707,8 @@ struct SumArgs {
   const uint32_t* run_start;
   const uint2* cuts;
   float* parts;
+  float4* huge;         // sums of the blocks that share a run
+  uint32_t* huge_done;  // how many of them are there
   int64_t* ids_out;  // message form: rows_out, n rows of d
   int64_t* n_out;
   float* out;
@@ -900,41 +915,80 @@ __device__ __forceinline__ void write_parts(const SumArgs& a, uint32_t run, int6
     if (c + j < a.d) dst[j] = a.accumulate ? dst[j] + y[j] * a.scale : y[j] * a.scale;
 }
 
-// Cut runs, in slabs of 128 columns: those of many items by a block each, whose warps add a
-// share of the items' sums each and then the shares in order; then the others by a warp each.
+// Cut runs, in slabs of 128 columns: those of very many items by HUGE_SPLIT blocks each, whose
+// warps add a share of the items' sums each and then the shares in order, and the last of
+// which to finish adds the blocks' sums in order (58,000 tokens of one row in 3,600 items: 43 us
+// by one block); those of many by a block each; then the others by a warp each.
 __global__ void __launch_bounds__(MERGE_THREADS) k_token_merge(SumArgs a, int slabs, int aligned, ErrSink err) {
   constexpr int WARPS = MERGE_THREADS / 32;
   __shared__ float s_hi[WARPS][128], s_lo[WARPS][128];
   follow();
   if (*(const volatile uint32_t*)err.step != 0u) return;
   const uint32_t n_runs = a.ctr->n_runs, P = a.ctr->P, room = (a.n >> a.cut_lg) + 1u;
-  const uint32_t n_short = a.ctr->n_cut[0], n_long = a.ctr->n_cut[1];
+  const uint32_t n_short = a.ctr->n_cut[0], n_long = a.ctr->n_cut[1], n_huge = a.ctr->n_cut[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   // the items of a run: the one before the first cut, and one from each cut on
   auto parts_of = [&](const uint2& cut) {
     const uint32_t end = cut.x + 1 < n_runs ? a.run_start[cut.x + 1] : P;
     return 1u + ((end - cut.y + (1u << a.cut_lg) - 1u) >> a.cut_lg);
   };
-  for (uint64_t i = blockIdx.x; i < (uint64_t)n_long * slabs; i += gridDim.x) {
-    const uint2 cut = a.cuts[room + i / slabs];
-    const int64_t c = (int64_t)(i % slabs) * 128 + lane * 4;
-    const uint32_t parts = parts_of(cut), each = (parts + WARPS - 1) / WARPS;
-    const uint32_t lo = min(parts, warp * each), hi = min(parts, lo + each);
-    CSum x[4] = {};
+  // this warp's share, the w-th of so many, of the sums of cut's run
+  auto share = [&](const uint2& cut, int64_t c, int w, int warps, CSum (&x)[4]) {
+    const uint32_t parts = parts_of(cut), each = (parts + warps - 1) / warps;
+    const uint32_t lo = min(parts, w * each), hi = min(parts, lo + each);
     add_parts(a, cut.y, lo, hi, c, x);
-    __syncthreads();  // the block is done with the run before
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       s_hi[warp][lane * 4 + j] = x[j].hi;
       s_lo[warp][lane * 4 + j] = x[j].lo;
     }
+  };
+  auto merge = [&](const float* hi, const float* lo, CSum (&x)[4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) csum_merge(x[j], hi[lane * 4 + j], lo[lane * 4 + j]);
+  };
+  for (uint64_t i = blockIdx.x; i < (uint64_t)n_huge * slabs * HUGE_SPLIT; i += gridDim.x) {
+    const uint64_t unit = i / HUGE_SPLIT, part = i % HUGE_SPLIT;
+    const uint2 cut = a.cuts[2 * room + unit / slabs];
+    const int64_t c = (int64_t)(unit % slabs) * 128 + lane * 4;
+    CSum x[4] = {};
+    share(cut, c, (int)part * WARPS + warp, HUGE_SPLIT * WARPS, x);
     __syncthreads();
     if (warp == 0) {
-      for (int w = 1; w < WARPS; ++w)
+      for (int w = 1; w < WARPS; ++w) merge(s_hi[w], s_lo[w], x);
+      float4* out = a.huge + (unit * HUGE_SPLIT + part) * 64 + lane;  // of 32 lanes: hi, then lo
+      out[0] = make_float4(x[0].hi, x[1].hi, x[2].hi, x[3].hi);
+      out[32] = make_float4(x[0].lo, x[1].lo, x[2].lo, x[3].lo);
+      __threadfence();
+      __syncwarp();
+      uint32_t before = 0;
+      if (lane == 0) before = atomicAdd(a.huge_done + unit, 1u);
+      if (__shfl_sync(FULL, before, 0) + 1u == (uint32_t)HUGE_SPLIT) {
+        __threadfence();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) csum_merge(x[j], s_hi[w][lane * 4 + j], s_lo[w][lane * 4 + j]);
+        for (int j = 0; j < 4; ++j) x[j] = CSum{0.f, 0.f};
+        for (int q = 0; q < HUGE_SPLIT; ++q) {
+          const float* in = reinterpret_cast<const float*>(a.huge + (unit * HUGE_SPLIT + q) * 64 + lane);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            csum_merge(x[j], *(const volatile float*)(in + j), *(const volatile float*)(in + 128 + j));
+        }
+        write_parts(a, cut.x, c, x, aligned);
+      }
+    }
+    __syncthreads();
+  }
+  for (uint64_t i = blockIdx.x; i < (uint64_t)n_long * slabs; i += gridDim.x) {
+    const uint2 cut = a.cuts[room + i / slabs];
+    const int64_t c = (int64_t)(i % slabs) * 128 + lane * 4;
+    CSum x[4] = {};
+    share(cut, c, warp, WARPS, x);
+    __syncthreads();
+    if (warp == 0) {
+      for (int w = 1; w < WARPS; ++w) merge(s_hi[w], s_lo[w], x);
       write_parts(a, cut.x, c, x, aligned);
     }
+    __syncthreads();
   }
   for (uint64_t i = (uint64_t)blockIdx.x * WARPS + warp; i < (uint64_t)n_short * slabs;
        i += (uint64_t)gridDim.x * WARPS) {
@@ -966,7 +1020,7 @@ cudaError_t sums_as(const SumArgs& a, ErrSink err, int num_sms, cudaStream_t s) 
   const int64_t mslabs = (a.d + 127) / 128;
   const int64_t mblocks = ((a.n >> a.cut_lg) * mslabs + MERGE_THREADS / 32 - 1) / (MERGE_THREADS / 32);
   const int aligned = vector_of(4, a.out, a.out_stride, a.d, 4) == 4;
-  return launch_following(k_token_merge, dim3((unsigned)std::min<int64_t>(mblocks, num_sms * MERGE_BLOCKS)),
+  return launch_following(k_token_merge, dim3((unsigned)std::min<int64_t>(mblocks, num_sms)),
                           MERGE_THREADS, 0, s, a, (int)mslabs, aligned, err);
 }
 
@@ -1015,7 +1069,7 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   ItemArgs ia{nullptr, (uint32_t)a.n, (uint32_t)a.V, ctr, reinterpret_cast<unsigned long long*>(ws + p.scan_status),
               reinterpret_cast<Item*>(ws + p.items), at(p.run_row), at(p.run_start),
               reinterpret_cast<uint2*>(ws + p.cuts), a.ids_out,
-              a.dense && !a.accumulate ? at(p.present) : nullptr, p.cut_lg};
+              a.dense && !a.accumulate ? at(p.present) : nullptr, p.cut_lg, at(p.huge_done), p.n_huge_done};
   const uint32_t* order = nullptr;
   cudaError_t e;
   if (p.small) {
@@ -1070,6 +1124,8 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   sa.run_start = ia.run_start;
   sa.cuts = ia.cuts;
   sa.parts = reinterpret_cast<float*>(ws + p.parts);
+  sa.huge = reinterpret_cast<float4*>(ws + p.huge);
+  sa.huge_done = at(p.huge_done);
   sa.ids_out = a.ids_out;
   sa.n_out = a.n_out;
   sa.out = a.dense ? a.dense : a.rows_out;
