@@ -215,78 +215,100 @@ __device__ __forceinline__ int param_slot(int q, int j, int Q) {
   return ((j / H) * Q + q) * H + j % H;
 }
 
-template <typename T, int V, int E, bool LANES, bool WHOLE>
-__device__ __forceinline__ void norm_rows(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
-                                          float* s_param, int Q, float (*s_sum)[MOST_WARPS][1]) {
+// One row, whose columns v holds: its statistics and output.  s_param: gamma at the thread's first
+// piece; taken: called when every thread of the row has what it needs of its input.
+template <typename T, int V, int E, bool LANES, bool WHOLE, int WARPS, typename F>
+__device__ __forceinline__ void norm_row(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
+                                         int64_t row, f2 (&v)[E / 2], const float* gamma, int Q,
+                                         float (*s_sum)[WARPS][1], F taken) {
   constexpr int K = E / V, P = E / 2, H = V < 4 ? V : 4;
   using Row = Held<T, V, E, WHOLE>;
   const int step = LANES ? at.step : 32 * V, left = a.d - at.first;
-  const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
+  const bool live = row < a.n;
+  f2 acc = v[0];
+#pragma unroll
+  for (int i = 1; i < P; ++i) acc = add2(acc, v[i]);
+  float sum[1] = {both(acc)};
+  row_sum<1, LANES>(sum, sp, at.group, s_sum[0]);
+  taken();
+  const float mean = sum[0] * inv_d;
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i] = add2(v[i], pair(-mean, -mean));
+  if (!WHOLE) {
+    float z[E];
+#pragma unroll
+    for (int i = 0; i < P; ++i) split(v[i], z[2 * i], z[2 * i + 1]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = Row::has(e / V, step, left) ? z[e] : 0.f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = pair(z[2 * i], z[2 * i + 1]);
+  }
+  acc = mul2(v[0], v[0]);
+#pragma unroll
+  for (int i = 1; i < P; ++i) acc = fma2(v[i], v[i], acc);
+  sum[0] = both(acc);
+  row_sum<1, LANES>(sum, sp, at.group, s_sum[1]);
+  const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
+  if (live && at.t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  if (!live) return;
+  T* y = static_cast<T*>(a.y) + row * a.y_stride + at.first;
+  float z[E];
+#pragma unroll
+  for (int i = 0; i < P; ++i) split(mul2(v[i], pair(rstd, rstd)), z[2 * i], z[2 * i + 1]);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    if (!Row::has(k, step, left)) continue;
+    float o[V];
+#pragma unroll
+    for (int h = 0; h < V / H; ++h) {
+      Pack<float, H> g, b;
+      float gj[H], bj[H];
+      g.load(gamma + h * Q * H + k * (step / V) * H);
+      b.load(gamma + Q * V + h * Q * H + k * (step / V) * H);
+      g.get(gj);
+      b.get(bj);
+#pragma unroll
+      for (int j = 0; j < H; ++j) o[h * H + j] = fmaf(z[k * V + h * H + j], gj[j], bj[j]);
+    }
+    Pack<T, V> w;
+    w.set(o);
+    w.store(y + k * step);
+  }
+}
+
+template <typename T, int V, int E, bool LANES, bool WHOLE>
+__device__ __forceinline__ void norm_rows(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
+                                          float* s_param, int Q, float (*s_sum)[MOST_WARPS][1]) {
+  constexpr int H = V < 4 ? V : 4;
+  const int step = LANES ? at.step : 32 * V, left = a.d - at.first;
+  const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   int64_t first = (int64_t)blockIdx.x * at.groups + at.warp_group;
   int64_t row = (int64_t)blockIdx.x * at.groups + at.group;
   const T* x = static_cast<const T*>(a.x) + at.first;
   const float* gamma = s_param + at.first / V * H;  // piece k of them is step / V pieces further
-  Row in;
+  Held<T, V, E, WHOLE> in;
   in.clear();
   if (row < a.n) in.load(x + row * a.x_stride, step, left);
   asm volatile("bar.sync 0;" ::: "memory");  // the parameters are there, for warps of either kind
   for (; first < a.n; first += per_pass, row += per_pass) {
-    const bool live = row < a.n;
-    f2 v[P];
+    f2 v[E / 2];
     in.get(v);
     if (row + per_pass < a.n) in.load(x + (row + per_pass) * a.x_stride, step, left);
-    f2 acc = v[0];
-#pragma unroll
-    for (int i = 1; i < P; ++i) acc = add2(acc, v[i]);
-    float sum[1] = {both(acc)};
-    row_sum<1, LANES>(sum, sp, at.group, s_sum[0]);
-    const float mean = sum[0] * inv_d;
-#pragma unroll
-    for (int i = 0; i < P; ++i) v[i] = add2(v[i], pair(-mean, -mean));
-    if (!WHOLE) {
-      float z[E];
-#pragma unroll
-      for (int i = 0; i < P; ++i) split(v[i], z[2 * i], z[2 * i + 1]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) z[e] = Row::has(e / V, step, left) ? z[e] : 0.f;
-#pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = pair(z[2 * i], z[2 * i + 1]);
-    }
-    acc = mul2(v[0], v[0]);
-#pragma unroll
-    for (int i = 1; i < P; ++i) acc = fma2(v[i], v[i], acc);
-    sum[0] = both(acc);
-    row_sum<1, LANES>(sum, sp, at.group, s_sum[1]);
-    const float rstd = rsqrtf(sum[0] * inv_d + a.eps);
-    if (live && at.t == 0) {
-      if (a.mean) a.mean[row] = mean;
-      if (a.rstd) a.rstd[row] = rstd;
-    }
-    if (!live) continue;
-    T* y = static_cast<T*>(a.y) + row * a.y_stride + at.first;
-    float z[E];
-#pragma unroll
-    for (int i = 0; i < P; ++i) split(mul2(v[i], pair(rstd, rstd)), z[2 * i], z[2 * i + 1]);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (!Row::has(k, step, left)) continue;
-      float o[V];
-#pragma unroll
-      for (int h = 0; h < V / H; ++h) {
-        Pack<float, H> g, b;
-        float gj[H], bj[H];
-        g.load(gamma + h * Q * H + k * (step / V) * H);
-        b.load(gamma + Q * V + h * Q * H + k * (step / V) * H);
-        g.get(gj);
-        b.get(bj);
-#pragma unroll
-        for (int j = 0; j < H; ++j) o[h * H + j] = fmaf(z[k * V + h * H + j], gj[j], bj[j]);
-      }
-      Pack<T, V> w;
-      w.set(o);
-      w.store(y + k * step);
-    }
+    norm_row<T, V, E, LANES, WHOLE>(a, sp, at, row, v, gamma, Q, s_sum, [] {});
+  }
+}
+
+// gamma and beta (or 1 and 0) into shared memory, by the whole block.
+template <int V>
+__device__ __forceinline__ void fetch_params(const LayerNormArgs& a, float* s_param, int Q) {
+  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
+    const int o = param_slot<V>(c / V, c % V, Q);
+    s_param[o] = param_at(a.gamma, a.param_type, c, 1.f);
+    s_param[Q * V + o] = param_at(a.beta, a.param_type, c, 0.f);
   }
 }
 
@@ -297,15 +319,111 @@ __global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm(LayerNormA
   follow();
   const Place<V, E, LANES> at(sp, a.d);
   const int Q = sp.L * sp.W * (E / V);
-  for (int c = threadIdx.x; c < a.d; c += blockDim.x) {
-    const int o = param_slot<V>(c / V, c % V, Q);
-    s_param[o] = param_at(a.gamma, a.param_type, c, 1.f);
-    s_param[Q * V + o] = param_at(a.beta, a.param_type, c, 0.f);
-  }
+  fetch_params<V>(a, s_param, Q);
   if (at.whole)
     norm_rows<T, V, E, LANES, true>(a, sp, at, s_param, Q, s_sum);
   else
     norm_rows<T, V, E, LANES, false>(a, sp, at, s_param, Q, s_sum);
+}
+
+constexpr int RING_WARPS = 24, RING_WARPS_GRAD = 16;  // of a block
+constexpr int RING_ROWS = 4;                          // a group takes at least
+constexpr int E_GRAD_RING = 16;                       // columns of a thread, backward
+
+// ---- rows through a ring in shared memory ------------------------------------------------
+// Many wide rows that start on 16 bytes come by bulk copies: a group of warps has `stages` rows
+// on their way, which no register waits for.  One thread of the group issues the copies, every
+// thread waits for them on the stage's barrier; a wait has a limit, after which the call's
+// results are undefined, GBA_E_DEVICE_TIMEOUT is latched, and later waits are short.  Forward:
+// bf16 8,192 x 8,192 73.6 -> 55 us, 32,768 x 4,096 105 -> 90, float32 3,531 x 3,664 29.5 -> 23.
+struct Ring {
+  uint64_t* full;  // [stages] of the group
+  char* data;      // [stages][bytes] of the group
+  int stages;
+  uint32_t bytes;  // of a stage
+  int64_t limit_ns;
+  bool failed;
+
+  __device__ __forceinline__ char* stage(int64_t i) const { return data + (size_t)(i % stages) * bytes; }
+  __device__ __forceinline__ void wait(int64_t i, const ErrSink& err) {
+    if (!mbar_wait(full + i % stages, (uint32_t)(i / stages) & 1u, failed ? 1000000ll : limit_ns) && !failed) {
+      failed = true;
+      raise_error(err, ERR_TIMEOUT);
+    }
+  }
+};
+
+// The block's rings, one for each group of threads, in dynamic shared memory.
+__device__ __forceinline__ Ring make_ring(char* smem, int group, int groups, int stages, uint32_t bytes,
+                                          int64_t limit_ns) {
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem);
+  const size_t head = ((size_t)groups * stages * 8 + 127) / 128 * 128;
+  Ring r;
+  r.full = full + group * stages;
+  r.data = smem + head + (size_t)group * stages * bytes;
+  r.stages = stages;
+  r.bytes = bytes;
+  r.limit_ns = limit_ns;
+  r.failed = false;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < groups * stages; ++i) mbar_init(full + i, 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  return r;
+}
+
+// A thread's pieces of a row in shared memory.
+template <typename T, int V, int E, bool WHOLE>
+__device__ __forceinline__ void from_stage(const char* stage, int first, int left, f2 (&x)[E / 2]) {
+  Held<T, V, E, WHOLE> in;
+  if (!WHOLE) in.clear();
+  in.load(reinterpret_cast<const T*>(stage) + first, 32 * V, left);
+  in.get(x);
+}
+
+template <typename T, int V, int E, bool WHOLE>
+__device__ __forceinline__ void norm_ring(const LayerNormArgs& a, const Split& sp, const Place<V, E, false>& at,
+                                          const float* s_param, int Q, float (*s_sum)[RING_WARPS][1], Ring ring,
+                                          const ErrSink& err) {
+  constexpr int H = V < 4 ? V : 4;
+  const int64_t per_pass = (int64_t)gridDim.x * at.groups, row0 = (int64_t)blockIdx.x * at.groups + at.group;
+  auto issue = [&](int64_t i) {
+    const int64_t row = row0 + i * per_pass;
+    if (at.t != 0 || row >= a.n) return;
+    uint64_t* bar = ring.full + i % ring.stages;
+    mbar_arrive_expect_tx(bar, ring.bytes);
+    bulk_g2s(ring.stage(i), static_cast<const T*>(a.x) + row * a.x_stride, ring.bytes, bar);
+  };
+  for (int i = 0; i < ring.stages; ++i) issue(i);
+  const float* gamma = s_param + at.first / V * H;
+  int64_t i = 0;
+  for (int64_t row = row0; row < a.n; row += per_pass, ++i) {
+    ring.wait(i, err);
+    f2 v[E / 2];
+    from_stage<T, V, E, WHOLE>(ring.stage(i), at.first, a.d - at.first, v);
+    // past the row's first sum every thread has read the stage
+    norm_row<T, V, E, false, WHOLE>(a, sp, at, row, v, gamma, Q, s_sum, [&] { issue(i + ring.stages); });
+  }
+}
+
+template <typename T, int V, int E>
+__global__ void __launch_bounds__(RING_WARPS * 32, 1)
+    k_layer_norm_ring(LayerNormArgs a, Split sp, int stages, ErrSink err, int64_t limit_ns) {
+  extern __shared__ __align__(128) char s_ring[];  // parameters, barriers, rows
+  __shared__ float s_sum[2][RING_WARPS][1];
+  const Place<V, E, false> at(sp, a.d);
+  const int Q = 32 * sp.W * (E / V);
+  float* s_param = reinterpret_cast<float*>(s_ring);
+  const Ring ring = make_ring(s_ring + (size_t)2 * Q * V * sizeof(float), at.group, at.groups, stages,
+                              (uint32_t)(a.d * sizeof(T)), limit_ns);
+  follow();
+  fetch_params<V>(a, s_param, Q);
+  __syncthreads();
+  if (at.whole)
+    norm_ring<T, V, E, true>(a, sp, at, s_param, Q, s_sum, ring, err);
+  else
+    norm_ring<T, V, E, false>(a, sp, at, s_param, Q, s_sum, ring, err);
 }
 
 // Rows of any width: one block each, read three times.
@@ -360,34 +478,68 @@ __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs 
 template <typename T, int V>
 constexpr int E_GRAD = sizeof(T) == 2 && V > 1 ? 16 : 8;
 
+// A thread's columns of gamma, 0 past the row's end.
+template <int V, int E, bool WHOLE>
+__device__ __forceinline__ void params_of(const LayerNormArgs& a, int first, int step, f2 (&gamma)[E / 2]) {
+  float y[E];
+#pragma unroll
+  for (int k = 0; k < E / V; ++k) {
+    float z[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) z[j] = 0.f;
+    if (WHOLE || first + k * step < a.d) params_at<V>(a.gamma, a.param_type, first + k * step, 1.f, z);
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[k * V + j] = z[j];
+  }
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) gamma[i] = pair(y[2 * i], y[2 * i + 1]);
+}
+
+// Adds a row's share to dg and db, and gives the thread's share of the row's sums of g and g h.
+// (m: the negative mean; g: dy, which is 0 past the row's end, and so are its products.)
+template <int P>
+__device__ __forceinline__ void grad_sums(const f2 (&x)[P], const f2 (&g)[P], f2 m, f2 r, const f2 (&gamma)[P],
+                                          f2 (&dg)[P], f2 (&db)[P], float (&sum)[2]) {
+  f2 s0 = pair(0.f, 0.f), s1 = s0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const f2 h = mul2(add2(x[i], m), r);
+    db[i] = add2(db[i], g[i]);
+    dg[i] = fma2(g[i], h, dg[i]);
+    const f2 gg = mul2(g[i], gamma[i]);
+    s0 = add2(s0, gg);
+    s1 = fma2(gg, h, s1);
+  }
+  sum[0] = both(s0);
+  sum[1] = both(s1);
+}
+
+// dx of a row, in the place of dy.
+template <int P>
+__device__ __forceinline__ void grad_out(const f2 (&x)[P], f2 (&g)[P], f2 m, f2 r, const f2 (&gamma)[P], float mg,
+                                         float mgh) {
+  const f2 nmg = pair(-mg, -mg), nmgh = pair(-mgh, -mgh);
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const f2 h = mul2(add2(x[i], m), r);
+    g[i] = mul2(r, fma2(h, nmgh, fma2(g[i], gamma[i], nmg)));
+  }
+}
+
 // dx of the rows that this thread's group takes, and its shares of dgamma and dbeta.  What a
 // thread keeps of a row while its sums are formed is its loads; h and g are formed from them
 // twice.
 template <typename T, int V, int E, bool LANES, bool FETCH, bool WHOLE>
 __device__ __forceinline__ void grad_rows(const LayerNormArgs& a, const Split& sp, const Place<V, E, LANES>& at,
                                           float (*s_sum)[MOST_WARPS][2], f2 (&dg)[E / 2], f2 (&db)[E / 2]) {
-  constexpr int K = E / V, P = E / 2;
+  constexpr int P = E / 2;
   using Row = Held<T, V, E, WHOLE>;
   using Next = Held<T, V, FETCH ? E : V, WHOLE>;
   const int step = LANES ? at.step : 32 * V, left = a.d - at.first;
   const int64_t per_pass = (int64_t)gridDim.x * at.groups;
   const float inv_d = 1.f / (float)a.d;
-  const f2 zero = pair(0.f, 0.f);
   f2 gamma[P];
-  {
-    float y[E];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float z[V];
-#pragma unroll
-      for (int j = 0; j < V; ++j) z[j] = 0.f;
-      if (Row::has(k, step, left)) params_at<V>(a.gamma, a.param_type, at.first + k * step, 1.f, z);
-#pragma unroll
-      for (int j = 0; j < V; ++j) y[k * V + j] = z[j];
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i) gamma[i] = pair(y[2 * i], y[2 * i + 1]);
-  }
+  params_of<V, E, WHOLE>(a, at.first, step, gamma);
   Row xin, din;
   Next xnext, dnext;
   xin.clear();
@@ -422,55 +574,32 @@ __device__ __forceinline__ void grad_rows(const LayerNormArgs& a, const Split& s
       fetch(row, xin, din, mean, rstd);
     }
     const f2 m = pair(-mean, -mean), r = pair(rstd, rstd);
-    f2 s0 = zero, s1 = zero;
+    float sum[2];
     {
       f2 x[P], g[P];
       xin.get(x);
-      din.get(g);  // 0 past the row's end, and so are its products
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const f2 h = mul2(add2(x[i], m), r);
-        db[i] = add2(db[i], g[i]);
-        dg[i] = fma2(g[i], h, dg[i]);
-        g[i] = mul2(g[i], gamma[i]);
-        s0 = add2(s0, g[i]);
-        s1 = fma2(g[i], h, s1);
-      }
+      din.get(g);
+      grad_sums<P>(x, g, m, r, gamma, dg, db, sum);
     }
-    float sum[2] = {both(s0), both(s1)};
     row_sum<2, LANES>(sum, sp, at.group, s_sum[flip]);
     flip ^= 1;
     if (row >= a.n) continue;
-    const float mg = sum[0] * inv_d, mgh = sum[1] * inv_d;
-    const f2 nmg = pair(-mg, -mg), nmgh = pair(-mgh, -mgh);
     f2 x[P], g[P];
     xin.get(x);
     din.get(g);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const f2 h = mul2(add2(x[i], m), r);
-      g[i] = mul2(r, fma2(h, nmgh, fma2(g[i], gamma[i], nmg)));
-    }
+    grad_out<P>(x, g, m, r, gamma, sum[0] * inv_d, sum[1] * inv_d);
     Row::store(static_cast<T*>(a.y) + row * a.y_stride + at.first, g, step, left);
   }
 }
 
-// One partial row of dgamma and dbeta per block: [2][blocks][d].
-template <typename T, int V, int E, bool LANES, bool FETCH>
-__global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm_grad(LayerNormArgs a, Split sp) {
+// One partial row of dgamma and dbeta per block, [2][blocks][d]: the block's groups of threads
+// are added in order, first those within a warp, then through shared memory (s_part: a value for
+// each column that the block's threads hold).
+template <int V, int E, bool LANES>
+__device__ __forceinline__ void write_partial(const LayerNormArgs& a, const Split& sp,
+                                              const Place<V, E, LANES>& at, const f2 (&dg)[E / 2],
+                                              const f2 (&db)[E / 2], float* s_part) {
   constexpr int K = E / V, P = E / 2;
-  __shared__ float s_sum[2][MOST_WARPS][2];
-  __shared__ float s_part[THREADS * E];
-  follow();
-  const Place<V, E, LANES> at(sp, a.d);
-  f2 dg[P], db[P];
-#pragma unroll
-  for (int i = 0; i < P; ++i) dg[i] = db[i] = pair(0.f, 0.f);
-  if (at.whole)
-    grad_rows<T, V, E, LANES, FETCH, true>(a, sp, at, s_sum, dg, db);
-  else
-    grad_rows<T, V, E, LANES, FETCH, false>(a, sp, at, s_sum, dg, db);
-  // the block's groups of threads, in order: first those within a warp, then through shared memory
   __syncwarp();
   float mine[2][E];
 #pragma unroll
@@ -511,6 +640,92 @@ __global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm_grad(Layer
     }
     __syncthreads();
   }
+}
+
+template <typename T, int V, int E, bool LANES, bool FETCH>
+__global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm_grad(LayerNormArgs a, Split sp) {
+  constexpr int P = E / 2;
+  __shared__ float s_sum[2][MOST_WARPS][2];
+  __shared__ float s_part[THREADS * E];
+  follow();
+  const Place<V, E, LANES> at(sp, a.d);
+  f2 dg[P], db[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) dg[i] = db[i] = pair(0.f, 0.f);
+  if (at.whole)
+    grad_rows<T, V, E, LANES, FETCH, true>(a, sp, at, s_sum, dg, db);
+  else
+    grad_rows<T, V, E, LANES, FETCH, false>(a, sp, at, s_sum, dg, db);
+  write_partial<V, E, LANES>(a, sp, at, dg, db, s_part);
+}
+
+// The gradient's rows through the ring, x and dy of a row in one stage.  A row's stage is read
+// twice, so it is free when every thread has come to the next row's sums.
+template <typename T, int V, int E, bool WHOLE>
+__device__ __forceinline__ void grad_ring(const LayerNormArgs& a, const Split& sp, const Place<V, E, false>& at,
+                                          float (*s_sum)[RING_WARPS_GRAD][2], Ring ring, const ErrSink& err,
+                                          f2 (&dg)[E / 2], f2 (&db)[E / 2]) {
+  constexpr int P = E / 2;
+  using Row = Held<T, V, E, WHOLE>;
+  const int left = a.d - at.first;
+  const int64_t per_pass = (int64_t)gridDim.x * at.groups, row0 = (int64_t)blockIdx.x * at.groups + at.group;
+  const float inv_d = 1.f / (float)a.d;
+  const uint32_t half = ring.bytes / 2;
+  auto issue = [&](int64_t i) {
+    const int64_t row = row0 + i * per_pass;
+    if (at.t != 0 || row >= a.n) return;
+    uint64_t* bar = ring.full + i % ring.stages;
+    mbar_arrive_expect_tx(bar, ring.bytes);
+    bulk_g2s(ring.stage(i), static_cast<const T*>(a.x) + row * a.x_stride, half, bar);
+    bulk_g2s(ring.stage(i) + half, static_cast<const T*>(a.dy) + row * a.dy_stride, half, bar);
+  };
+  for (int i = 0; i < ring.stages; ++i) issue(i);
+  f2 gamma[P];
+  params_of<V, E, WHOLE>(a, at.first, 32 * V, gamma);
+  float mean = row0 < a.n ? a.mean[row0] : 0.f, rstd = row0 < a.n ? a.rstd[row0] : 0.f;
+  int64_t i = 0;
+  for (int64_t row = row0; row < a.n; row += per_pass, ++i) {
+    ring.wait(i, err);
+    const char* stage = ring.stage(i);
+    const f2 m = pair(-mean, -mean), r = pair(rstd, rstd);
+    if (row + per_pass < a.n) {
+      mean = a.mean[row + per_pass];
+      rstd = a.rstd[row + per_pass];
+    }
+    float sum[2];
+    f2 x[P], g[P];
+    from_stage<T, V, E, WHOLE>(stage, at.first, left, x);
+    from_stage<T, V, E, WHOLE>(stage + half, at.first, left, g);
+    grad_sums<P>(x, g, m, r, gamma, dg, db, sum);
+    row_sum<2, false>(sum, sp, at.group, s_sum[i & 1]);
+    if (i > 0) issue(i - 1 + ring.stages);
+    from_stage<T, V, E, WHOLE>(stage, at.first, left, x);
+    from_stage<T, V, E, WHOLE>(stage + half, at.first, left, g);
+    grad_out<P>(x, g, m, r, gamma, sum[0] * inv_d, sum[1] * inv_d);
+    Row::store(static_cast<T*>(a.y) + row * a.y_stride + at.first, g, 32 * V, left);
+  }
+}
+
+template <typename T, int V, int E>
+__global__ void __launch_bounds__(RING_WARPS_GRAD * 32, 1)
+    k_layer_norm_grad_ring(LayerNormArgs a, Split sp, int stages, ErrSink err, int64_t limit_ns) {
+  constexpr int P = E / 2;
+  extern __shared__ __align__(128) char s_ring[];  // barriers, rows; in the end the partial rows
+  __shared__ float s_sum[2][RING_WARPS_GRAD][2];
+  const Place<V, E, false> at(sp, a.d);
+  const Ring ring = make_ring(s_ring, at.group, at.groups, stages, (uint32_t)(2 * a.d * sizeof(T)), limit_ns);
+  follow();
+  __syncthreads();
+  f2 dg[P], db[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) dg[i] = db[i] = pair(0.f, 0.f);
+  if (at.whole)
+    grad_ring<T, V, E, true>(a, sp, at, s_sum, ring, err, dg, db);
+  else
+    grad_ring<T, V, E, false>(a, sp, at, s_sum, ring, err, dg, db);
+  __syncthreads();  // no row is read any more
+  write_partial<V, E, false>(a, sp, at, dg, db,
+                             reinterpret_cast<float*>(s_ring + ((size_t)at.groups * stages * 8 + 127) / 128 * 128));
 }
 
 // Rows of any width: dx by one block a row, read twice.
@@ -668,9 +883,51 @@ unsigned grid_of(int64_t n, const Split& s, int threads, int num_sms, int per_sm
   return (unsigned)std::min<int64_t>((n + rows - 1) / rows, (int64_t)num_sms * per_sm);
 }
 
+// A block of a ring kernel: one per SM, of up to `most` warps, with as many stages (up to
+// four) as 200 KB of shared memory leave room for beside `fixed` bytes.
+struct RingShape {
+  Split split;
+  int groups, stages;
+  size_t smem;
+};
+RingShape ring_of(int32_t d, int E, int most, size_t stage_bytes, size_t fixed) {
+  RingShape r;
+  int threads;
+  r.split = warps_of(d, E, &threads);
+  r.groups = std::max(1, most / r.split.W);
+  const size_t room = 200 * 1024 - fixed;
+  r.stages = (int)std::min<size_t>(4, room / ((size_t)r.groups * stage_bytes));
+  while (r.stages < 2 && r.groups > 1) {
+    --r.groups;
+    r.stages = (int)std::min<size_t>(4, room / ((size_t)r.groups * stage_bytes));
+  }
+  r.smem = fixed + ((size_t)r.groups * r.stages * 8 + 127) / 128 * 128 + (size_t)r.groups * r.stages * stage_bytes;
+  return r;
+}
+// Does a ring serve n rows?  With a few rows a group its setting up costs more than it saves.
+bool ring_serves(const RingShape& r, int64_t n, int num_sms) {
+  return r.split.W >= 2 && r.stages >= 2 && n >= (int64_t)RING_ROWS * r.groups * num_sms;
+}
+template <typename F>
+cudaError_t launch_ring(F* kernel, const RingShape& r, const LayerNormArgs& a, const RingWait& w, unsigned grid,
+                        cudaStream_t s) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+  if (e != cudaSuccess) return e;
+  return launch_following(kernel, dim3(grid), 32 * r.split.W * r.groups, r.smem, s, a, r.split, r.stages, w.err, w.limit_ns);
+}
+
 template <typename T, int V>
-cudaError_t norm_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
+cudaError_t norm_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cudaStream_t s) {
   constexpr int EL = E_LANES<V>, E = E_NORM<T, V>;
+  if constexpr (V * sizeof(T) == 16)
+    if (a.d > 32 * E && a.d <= MOST_WARPS * 32 * E) {
+      int threads;
+      const size_t params = (size_t)warps_of(a.d, E, &threads).W * 32 * E * 2 * sizeof(float);
+      const RingShape r = ring_of(a.d, E, RING_WARPS, (size_t)a.d * sizeof(T), params);
+      if (ring_serves(r, a.n, num_sms))
+        return launch_ring(k_layer_norm_ring<T, V, E>, r, a, w,
+                           (unsigned)std::min<int64_t>(num_sms, (a.n + r.groups - 1) / r.groups), s);
+    }
   if (a.d <= 32 * EL) {
     constexpr size_t smem = (size_t)32 * EL * 2 * sizeof(float);
     static const int held = resident(k_layer_norm<T, V, EL, true>, smem);
@@ -692,13 +949,21 @@ cudaError_t norm_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
 
 // How a gradient's rows are held: a vector a lane, with the next row's loads in flight, without
 // (rows of up to 8,192 columns that are read by 8 columns a thread), or not at all.
-enum class Way { LANES, FETCH, PLAIN, WIDE };
+enum class Way { LANES, FETCH, PLAIN, WIDE, RING };
 struct GradShape {
   Way way;
+  RingShape ring;
   Split split;
   int threads;
   int parts;  // blocks, and partial rows
 };
+
+// float32 rows come through the ring (4,096 x 8,192: 82 us from registers, 69 this way).  16-bit ones
+// do not: what bounds them is the instructions that widen them, twice in either way, and
+// reading shared memory adds to those (32,768 x 2,048: 75 us from registers, 87 this way, 82
+// with the loads kept in registers between the two).
+template <typename T, int V>
+constexpr bool GRAD_RING = sizeof(T) == 4 && V == 4;
 
 template <typename T, int V>
 GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
@@ -710,7 +975,19 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
     g.split = lanes_of(a.d, EL);
     g.threads = THREADS;
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held);
-  } else if (a.d <= MOST_WARPS * 32 * E) {
+    return g;
+  }
+  if constexpr (GRAD_RING<T, V>)
+    if (a.d <= RING_WARPS_GRAD * 32 * E_GRAD_RING) {
+      // (the partial rows take the stages' place in the end)
+      g.ring = ring_of(a.d, E_GRAD_RING, RING_WARPS_GRAD, (size_t)2 * a.d * sizeof(T), 0);
+      if (ring_serves(g.ring, a.n, num_sms)) {
+        g.way = Way::RING;
+        g.parts = (int)std::min<int64_t>(num_sms, (a.n + g.ring.groups - 1) / g.ring.groups);
+        return g;
+      }
+    }
+  if (a.d <= MOST_WARPS * 32 * E) {
     static const Residency held(k_layer_norm_grad<T, V, E, false, true>, E, [](int) { return (size_t)0; });
     g.way = Way::FETCH;
     g.split = warps_of(a.d, E, &g.threads);
@@ -727,7 +1004,7 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
 }
 
 template <typename T, int V>
-cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
+cudaError_t grad_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cudaStream_t s) {
   constexpr int EL = E_LANES<V>, E = E_GRAD<T, V>;
   const GradShape g = grad_shape<T, V>(a, num_sms);
   cudaError_t e;
@@ -738,6 +1015,10 @@ cudaError_t grad_as(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
     if (e == cudaSuccess)
       e = launch_following(k_layer_norm_grad_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 4)),
                            WIDE_GRAD_THREADS, 0, s, a);
+  } else if (g.way == Way::RING) {
+    e = cudaErrorInvalidValue;
+    if constexpr (GRAD_RING<T, V>)
+      e = launch_ring(k_layer_norm_grad_ring<T, V, E_GRAD_RING>, g.ring, a, w, (unsigned)g.parts, s);
   } else {
     auto kernel = g.way == Way::LANES ? k_layer_norm_grad<T, V, EL, true, true> : k_layer_norm_grad<T, V, E, false, true>;
     if constexpr (E < 16)
@@ -771,8 +1052,9 @@ auto with_type(int32_t type, const LayerNormArgs& a, F f) {
 
 }  // namespace
 
-cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, int num_sms, cudaStream_t s) {
-  return with_type(type, a, [&](auto x, auto v) { return norm_as<decltype(x), v()>(a, num_sms, s); });
+cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
+                              cudaStream_t s) {
+  return with_type(type, a, [&](auto x, auto v) { return norm_as<decltype(x), v()>(a, w, num_sms, s); });
 }
 
 size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms) {
@@ -780,9 +1062,9 @@ size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_s
   return (size_t)parts * 2 * (size_t)a.d * sizeof(float);
 }
 
-cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, int num_sms,
+cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
                                    cudaStream_t s) {
-  return with_type(type, a, [&](auto x, auto v) { return grad_as<decltype(x), v()>(a, num_sms, s); });
+  return with_type(type, a, [&](auto x, auto v) { return grad_as<decltype(x), v()>(a, w, num_sms, s); });
 }
 
 }  // namespace gba

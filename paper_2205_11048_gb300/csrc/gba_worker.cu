@@ -29,7 +29,7 @@ struct gba_worker {
 
 namespace {
 
-constexpr int64_t WAIT_NS = 2000000000ll;  // bound of the look-back waits
+constexpr int64_t WAIT_NS = 2000000000ll;  // bound of the kernels' waits
 constexpr int32_t MAX_COLS = 1 << 20;
 constexpr int64_t MAX_TOKENS = (1ll << 30) - 1;
 constexpr int64_t MAX_TABLE_ROWS = 0xFFFFFFFEll;  // keys are 32-bit; one more stands for padding
@@ -413,7 +413,7 @@ gba_status gba_layer_norm(gba_worker* w, const gba_matrix* x, const void* gamma,
   a.d = x->cols;
   a.param_type = param_type;
   a.eps = eps;
-  const cudaError_t e = launch_layer_norm(a, x->type, w->num_sms, w->stream);
+  const cudaError_t e = launch_layer_norm(a, x->type, RingWait{w->sink, WAIT_NS}, w->num_sms, w->stream);
   return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "launch the layer norm");
 }
 
@@ -459,7 +459,8 @@ gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_ma
   const gba_status st = reserve(w, layer_norm_grad_workspace(a, x->type, w->num_sms));
   if (st != GBA_OK) return st;
   a.parts = reinterpret_cast<float*>(w->ws);
-  const cudaError_t e = launch_layer_norm_grad(a, x->type, w->num_sms, w->stream);
+  const cudaError_t e = launch_layer_norm_grad(a, x->type, RingWait{w->sink, WAIT_NS}, w->num_sms,
+                                               w->stream);
   return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "launch the layer norm's gradient");
 }
 

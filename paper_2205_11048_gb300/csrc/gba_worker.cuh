@@ -248,9 +248,15 @@ struct LayerNormArgs {
   float eps;
   float* parts;  // workspace of the gradient
 };
-cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, int num_sms, cudaStream_t s);
+// Where a wait for a copy that runs out reports it, and its limit.
+struct RingWait {
+  ErrSink err;
+  int64_t limit_ns;
+};
+cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
+                              cudaStream_t s);
 size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms);
-cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, int num_sms,
+cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
                                    cudaStream_t s);
 
 }  // namespace gba

@@ -35,12 +35,12 @@ cudaError_t launch_norm(const gba_grad_part*, int32_t n_parts, bool, float, floa
   fake_need(ticket, 4);
   return cudaSuccess;
 }
-cudaError_t launch_layer_norm(const LayerNormArgs&, int32_t, int, cudaStream_t) {
+cudaError_t launch_layer_norm(const LayerNormArgs&, int32_t, const RingWait&, int, cudaStream_t) {
   ++g_launches;
   return cudaSuccess;
 }
 size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t, int) { return (size_t)a.d * 8; }
-cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t, int, cudaStream_t) {
+cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t, const RingWait&, int, cudaStream_t) {
   ++g_launches;
   fake_need(a.parts, (size_t)a.d * 8);
   return cudaSuccess;

@@ -487,6 +487,18 @@ WIDTHS = [(1, 1), (5, 2), (3, 16), (9, 17), (300, 64), (130, 100), (7, 1001), (3
 @pytest.mark.parametrize("n,d", WIDTHS)
 @pytest.mark.parametrize("extra,offset,own_params", [(0, 0, False), (8, 8, True), (3, 1, False)])
 def test_layer_norm_and_its_gradient(w, dtype, n, d, extra, offset, own_params):
+    check_layer_norm(w, dtype, n, d, extra, offset, own_params)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS.get)
+@pytest.mark.parametrize("n,d,extra", [(7400, 1040, 0), (8001, 1536, 8), (5003, 2056, 0), (3700, 4096, 16), (1300, 8192, 0),
+                                       (700, 16384, 0)])
+def test_layer_norm_of_many_wide_rows(w, dtype, n, d, extra):
+    """Rows enough for every SM to take several: they come through shared memory."""
+    check_layer_norm(w, dtype, n, d, extra, extra, False)
+
+
+def check_layer_norm(w, dtype, n, d, extra, offset, own_params):
     g = gen(n + d)
     eps = 1e-5
     x = rand(g, n, d, dtype=dtype, extra=extra, offset=offset, mean=0.5)
