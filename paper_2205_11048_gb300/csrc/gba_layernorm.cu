@@ -326,16 +326,19 @@ __global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm(LayerNormA
     norm_rows<T, V, E, LANES, false>(a, sp, at, s_param, Q, s_sum);
 }
 
-constexpr int RING_WARPS = 24, RING_WARPS_GRAD = 16;  // of a block
-constexpr int RING_ROWS = 4;                          // a group takes at least
-constexpr int E_GRAD_RING = 16;                       // columns of a thread, backward
+// Warps of a block.  Forward 20, or 24 for 16-bit rows of six warps and more: of eight, 24 warps
+// hold three groups and 20 only two (8,192 x 8,192: 57 us against 65); others gain more from
+// the registers that 20 leave a thread (16,384 x 5,120: 69 against 72.5; float32 16,384 x 4,096,
+// in two groups of eight, 88 against 100.5).
+constexpr int RING_WARPS = 20, RING_WARPS_MORE = 24, RING_WARPS_GRAD = 16;
+constexpr int RING_ROWS = 4;     // a group takes at least
+constexpr int E_GRAD_RING = 16;  // columns of a thread, backward
 
 // ---- rows through a ring in shared memory ------------------------------------------------
 // Many wide rows that start on 16 bytes come by bulk copies: a group of warps has `stages` rows
 // on their way, which no register waits for.  One thread of the group issues the copies, every
 // thread waits for them on the stage's barrier; a wait has a limit, after which the call's
-// results are undefined, GBA_E_DEVICE_TIMEOUT is latched, and later waits are short.  Forward:
-// bf16 8,192 x 8,192 73.6 -> 55 us, 32,768 x 4,096 105 -> 90, float32 3,531 x 3,664 29.5 -> 23.
+// results are undefined, GBA_E_DEVICE_TIMEOUT is latched, and later waits are short.
 struct Ring {
   uint64_t* full;  // [stages] of the group
   char* data;      // [stages][bytes] of the group
@@ -382,15 +385,15 @@ __device__ __forceinline__ void from_stage(const char* stage, int first, int lef
   in.get(x);
 }
 
-template <typename T, int V, int E, bool WHOLE>
+template <typename T, int V, int E, bool WHOLE, int WARPS>
 __device__ __forceinline__ void norm_ring(const LayerNormArgs& a, const Split& sp, const Place<V, E, false>& at,
-                                          const float* s_param, int Q, float (*s_sum)[RING_WARPS][1], Ring ring,
+                                          const float* s_param, int Q, float (*s_sum)[WARPS][1], Ring ring,
                                           const ErrSink& err) {
   constexpr int H = V < 4 ? V : 4;
   const int64_t per_pass = (int64_t)gridDim.x * at.groups, row0 = (int64_t)blockIdx.x * at.groups + at.group;
   auto issue = [&](int64_t i) {
     const int64_t row = row0 + i * per_pass;
-    if (at.t != 0 || row >= a.n) return;
+    if (at.t != 0 || row >= a.n || ring.failed) return;  // after a failure no barrier is armed twice
     uint64_t* bar = ring.full + i % ring.stages;
     mbar_arrive_expect_tx(bar, ring.bytes);
     bulk_g2s(ring.stage(i), static_cast<const T*>(a.x) + row * a.x_stride, ring.bytes, bar);
@@ -407,11 +410,11 @@ __device__ __forceinline__ void norm_ring(const LayerNormArgs& a, const Split& s
   }
 }
 
-template <typename T, int V, int E>
-__global__ void __launch_bounds__(RING_WARPS * 32, 1)
+template <typename T, int V, int E, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1)
     k_layer_norm_ring(LayerNormArgs a, Split sp, int stages, ErrSink err, int64_t limit_ns) {
   extern __shared__ __align__(128) char s_ring[];  // parameters, barriers, rows
-  __shared__ float s_sum[2][RING_WARPS][1];
+  __shared__ float s_sum[2][WARPS][1];
   const Place<V, E, false> at(sp, a.d);
   const int Q = 32 * sp.W * (E / V);
   float* s_param = reinterpret_cast<float*>(s_ring);
@@ -421,9 +424,9 @@ __global__ void __launch_bounds__(RING_WARPS * 32, 1)
   fetch_params<V>(a, s_param, Q);
   __syncthreads();
   if (at.whole)
-    norm_ring<T, V, E, true>(a, sp, at, s_param, Q, s_sum, ring, err);
+    norm_ring<T, V, E, true, WARPS>(a, sp, at, s_param, Q, s_sum, ring, err);
   else
-    norm_ring<T, V, E, false>(a, sp, at, s_param, Q, s_sum, ring, err);
+    norm_ring<T, V, E, false, WARPS>(a, sp, at, s_param, Q, s_sum, ring, err);
 }
 
 // Rows of any width: one block each, read three times.
@@ -673,7 +676,7 @@ __device__ __forceinline__ void grad_ring(const LayerNormArgs& a, const Split& s
   const uint32_t half = ring.bytes / 2;
   auto issue = [&](int64_t i) {
     const int64_t row = row0 + i * per_pass;
-    if (at.t != 0 || row >= a.n) return;
+    if (at.t != 0 || row >= a.n || ring.failed) return;  // after a failure no barrier is armed twice
     uint64_t* bar = ring.full + i % ring.stages;
     mbar_arrive_expect_tx(bar, ring.bytes);
     bulk_g2s(ring.stage(i), static_cast<const T*>(a.x) + row * a.x_stride, half, bar);
@@ -923,10 +926,14 @@ cudaError_t norm_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cuda
     if (a.d > 32 * E && a.d <= MOST_WARPS * 32 * E) {
       int threads;
       const size_t params = (size_t)warps_of(a.d, E, &threads).W * 32 * E * 2 * sizeof(float);
-      const RingShape r = ring_of(a.d, E, RING_WARPS, (size_t)a.d * sizeof(T), params);
-      if (ring_serves(r, a.n, num_sms))
-        return launch_ring(k_layer_norm_ring<T, V, E>, r, a, w,
-                           (unsigned)std::min<int64_t>(num_sms, (a.n + r.groups - 1) / r.groups), s);
+      const bool more = sizeof(T) == 2 && warps_of(a.d, E, &threads).W >= 6;
+      const RingShape r = ring_of(a.d, E, more ? RING_WARPS_MORE : RING_WARPS, (size_t)a.d * sizeof(T), params);
+      if (ring_serves(r, a.n, num_sms)) {
+        auto kernel = k_layer_norm_ring<T, V, E, RING_WARPS>;
+        if constexpr (sizeof(T) == 2)
+          if (more) kernel = k_layer_norm_ring<T, V, E, RING_WARPS_MORE>;
+        return launch_ring(kernel, r, a, w, (unsigned)std::min<int64_t>(num_sms, (a.n + r.groups - 1) / r.groups), s);
+      }
     }
   if (a.d <= 32 * EL) {
     constexpr size_t smem = (size_t)32 * EL * 2 * sizeof(float);
