@@ -251,6 +251,20 @@ def tokens(g, n, V, kind, pad):
     (4097, 130, 300_000, "distinct", 0, 0, 0), (20_000, 3, 1, "one", 0.5, 0, 0),
     (100_000, 20, 1000, "skew", 0, 0, 0), (300, 4104, 37, "skew", 0.2, 8, 0), (500, 16, 10, "one", 1.1, 0, 0)])
 def test_embed_grad(w, dtype, n, d, V, kind, pad, extra, offset):
+    check_embed_grad(w, dtype, n, d, V, kind, pad, extra, offset)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS.get)
+@pytest.mark.parametrize("n,d,V,kind,pad,extra", [
+    (16_000, 1024, 500, "skew", 0.1, 0), (15_001, 2056, 3000, "runs", 0, 8), (14_600, 4096, 9, "one", 0.3, 0),
+    (20_000, 1536, 40_000, "distinct", 0.9, 0), (14_592, 8192, 300, "skew", 0, 0), (30_000, 528, 200, "skew", 0, 0),
+    (16_000, 1024, 10, "one", 1.1, 0)])
+def test_embed_grad_of_many_wide_rows(w, dtype, n, d, V, kind, pad, extra):
+    """Tokens enough for every SM to take many, of rows of several slabs."""
+    check_embed_grad(w, dtype, n, d, V, kind, pad, extra, 0)
+
+
+def check_embed_grad(w, dtype, n, d, V, kind, pad, extra, offset):
     g = gen(n + 3 * d)
     ids = tokens(g, n, V, kind, pad)
     grad = rand(g, n, d, dtype=dtype, extra=extra, offset=offset)
