@@ -371,10 +371,11 @@ void gba_worker_destroy(gba_worker* w);
  * gba_embed - scaled embedding rows: out[i] = scale * weights[row(ids[i])].
  *
  * weights    the table, of any type; its rows are the rows of id_mode DIRECT or
- *            MODULO (a worker's own weights, or a copy).
+ *            MODULO (a worker's own weights, or a copy).  1 .. 2^32 - 3 rows.
  * ids        n device int64.  pad_id: positions holding it become rows of zeros
  *            and read nothing (GBA_NO_PAD: none).
- * out        n x weights->cols, of any type; must not overlap the weights.
+ * out        n x weights->cols, of float32, of the weights' type, or of any type if
+ *            the weights are float32; must not overlap the weights.  n < 2^30.
  * A DIRECT id outside [0, rows) gets a row of zeros and latches GBA_E_ID_RANGE.
  */
 gba_status gba_embed(gba_worker* w, const gba_matrix* weights, int32_t id_mode,
@@ -400,7 +401,7 @@ gba_status gba_embed_table(gba_worker* w, gba_handle* h, int32_t t, const int64_
  *
  * grad       n x cols, the gradient of gba_embed's output.  Rows at padding
  *            positions are not read.
- * rows, id_mode  of the table: DIRECT or MODULO, rows < 2^32 - 2.
+ * rows, id_mode  of the table: DIRECT or MODULO, 1 .. 2^32 - 3 rows.
  * ids_out    n device int64: the rows that occur, ascending, then the last of
  *            them repeated up to n.
  * rows_out   n x cols device float32, 16-byte aligned, contiguous: scale * (sum of

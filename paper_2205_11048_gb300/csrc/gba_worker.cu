@@ -32,7 +32,7 @@ namespace {
 constexpr int64_t WAIT_NS = 2000000000ll;  // bound of the kernels' waits
 constexpr int32_t MAX_COLS = 1 << 20;
 constexpr int64_t MAX_TOKENS = (1ll << 30) - 1;
-constexpr int64_t MAX_TABLE_ROWS = 0xFFFFFFFEll;  // keys are 32-bit; one more stands for padding
+constexpr int64_t MAX_TABLE_ROWS = 0xFFFFFFFDll;  // keys are 32-bit; the next stands for padding, the last for none
 
 gba_status fail(gba_worker* w, gba_status s, const char* msg) {
   snprintf(w->last_error, sizeof w->last_error, "%s", msg);
@@ -89,7 +89,7 @@ const char* bad_ids(const int64_t* ids, int64_t n) {
 
 const char* bad_mode(int32_t id_mode, int64_t rows) {
   if (id_mode != GBA_ID_DIRECT && id_mode != GBA_ID_MODULO) return "id_mode is neither DIRECT nor MODULO";
-  if (rows < 1 || rows >= MAX_TABLE_ROWS) return "rows of the table outside [1, 2^32 - 2)";
+  if (rows < 1 || rows > MAX_TABLE_ROWS) return "rows of the table outside [1, 2^32 - 3]";
   return nullptr;
 }
 

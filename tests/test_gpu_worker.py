@@ -628,6 +628,26 @@ def test_expanded_and_transposed_gradients_are_taken(w):
     assert torch.equal(w.layer_norm(x.t())[0], w.layer_norm(x.t().contiguous())[0])
 
 
+def test_no_tokens_and_no_rows(w):
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    W, g = torch.ones(4, 8, device="cuda"), torch.empty(0, 8, device="cuda")
+    assert w.embed(W, none).shape == (0, 8) and w.embed(W, none.view(0, 5)).shape == (0, 5, 8)
+    ids, rows, count = w.embed_grad(none, g, 4)
+    assert ids.numel() == rows.numel() == int(count) == 0
+    strided = torch.ones(4, 10, device="cuda")
+    for out in (W.clone(), strided[:, :8]):
+        w.embed_grad_dense(none, g, out, accumulate=True)
+        assert bool((out == 1.0).all())
+        w.embed_grad_dense(none, g, out)
+        assert not bool(out.any())
+    assert bool((strided[:, 8:] == 1.0).all())
+    y, mean, rstd = w.layer_norm(g)
+    dx, dgamma, dbeta = w.layer_norm_grad(g, g, None, mean, rstd)
+    assert y.shape == dx.shape == (0, 8) and not bool(dgamma.any()) and not bool(dbeta.any())
+    assert float(w.grad_norm([])) == 0.0 and float(w.clip_grads([g], 1.0)) == 0.0
+    w.sync()
+
+
 def test_bad_tensors_are_refused(w):
     ids = torch.tensor([1, 0], device="cuda")
     W = torch.ones(4, 8, device="cuda")
@@ -670,13 +690,14 @@ def test_calls_under_another_stream_are_ordered_with_it():
     w.close()
 
 
-def test_a_captured_sequence_replays():
+@pytest.mark.parametrize("n", [5000, 20_000])
+def test_a_captured_sequence_replays(n):
     """After a first run at the size, the calls allocate nothing and can be captured."""
     s = torch.cuda.Stream()
     with torch.cuda.stream(s):
         w = B.Worker()
         g = gen(11)
-        V, n, d = 700, 5000, 64
+        V, d = 700, 64
         weights, G = rand(g, V, d), rand(g, n, d)
         gamma = rand(g, d)
         ids = torch.randint(0, V, (n,), generator=g, device="cuda")
