@@ -252,7 +252,7 @@ struct GradPlan {
   size_t keys[2], vals[2], items, run_row, run_start, cuts, parts, huge, bytes;
   int64_t tiles, n_huge_done;
   int cut_lg;
-  bool small;  // keys, sort and items by one cluster
+  bool small;  // keys, sort and items by one cluster, or one block
 };
 
 // Floats from one item's sum to the next: vectors of them are aligned, whatever the width.
@@ -520,34 +520,46 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
   }
 }
 
-// ---- gradient: keys, sort and items of a small call, by one cluster ----------------------------
+// ---- gradient: keys, sort and items of a small call, by one cluster or block -------------------
 // The same passes over digits as the larger sort, with the keys in the shared memory of
 // eight blocks: a warp ranks its keys among equal digits, the blocks tell each other their
 // counts and send the keys to their places.  One launch instead of five or six whose work is a
 // few microseconds: whole calls of 1,000, 4,000, 8,000 and 16,000 tokens x 64 floats take 14.5,
 // 17.2, 22.0 and 29.9 us this way and 20.5, 25.9, 27.4 and 29.5 the other, so it is for up to
-// 8,192.  (One block alone takes 30 us for 6,656 keys: match.any gives an SM about one key every
-// two cycles.)
+// 8,192.  Up to 1,024 tokens one block does it without the cluster's barriers (30, 500 and 1,000
+// tokens 7.0, 10.7 and 12.4 us, by a cluster 11.1, 14.6 and 15.5; 6,656 keys would take it 30 us:
+// match.any gives an SM about one key every two cycles).
 constexpr int CL_BLOCKS = 8, CL_THREADS = 512, CL_WARPS = CL_THREADS / 32;
 constexpr int CL_RADIX = 512;  // a digit for each thread
 static_assert(CL_RADIX == CL_THREADS && 2 * CL_BLOCKS * CL_THREADS == SMALL_N, "");
 
-template <int I>  // keys a thread
-__global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
+template <int I, int BLOCKS>  // keys a thread, blocks
+__global__ void __cluster_dims__(BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
     k_token_small(KeyArgs ka, SortPlan plan, ItemArgs a, uint32_t* sorted, uint32_t* order, ErrSink err) {
   constexpr int PER = CL_THREADS * I;  // a block's
   __shared__ uint32_t s_keys[PER];
   __shared__ uint16_t s_vals[PER];
   __shared__ uint16_t s_cnt[CL_WARPS][CL_RADIX];  // per warp: counts, then offsets among equal digits
-  __shared__ uint32_t s_all[CL_BLOCKS][CL_RADIX];  // every block's counts of the pass
+  __shared__ uint32_t s_all[BLOCKS][CL_RADIX];  // every block's counts of the pass
   __shared__ uint32_t s_place[CL_RADIX];           // where this block's keys of a digit go
   __shared__ uint32_t s_scan[CL_RADIX / 32];
   __shared__ unsigned long long s_warp[CL_WARPS];
-  __shared__ unsigned long long s_sums[CL_BLOCKS];
-  __shared__ uint32_t s_bad[CL_BLOCKS];
+  __shared__ unsigned long long s_sums[BLOCKS];
+  __shared__ uint32_t s_bad[BLOCKS];
   follow();
-  auto cluster = cg::this_cluster();
-  const int me = (int)cluster.block_rank();
+  const int me = BLOCKS == 1 ? 0 : (int)cg::this_cluster().block_rank();
+  auto sync = [] {
+    if constexpr (BLOCKS == 1)
+      __syncthreads();
+    else
+      cg::this_cluster().sync();
+  };
+  auto of_block = [](auto* p, uint32_t b) {  // p of block b
+    if constexpr (BLOCKS == 1)
+      return p;
+    else
+      return cg::this_cluster().map_shared_rank(p, b);
+  };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t at = (uint32_t)(warp * 32 * I + lane), base = (uint32_t)(me * PER), lt = lanemask_lt();
   uint32_t key[I], val[I];
@@ -560,11 +572,11 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
   }
   if (me == 0 && tid == 0) *a.ctr = Counters{};
   if (a.present)
-    for (int64_t i = base / I + tid; i < (ka.V + 31) / 32; i += CL_BLOCKS * CL_THREADS) a.present[i] = 0u;
-  for (int64_t i = base / I + tid; i < a.n_huge_done; i += CL_BLOCKS * CL_THREADS) a.huge_done[i] = 0u;
+    for (int64_t i = base / I + tid; i < (ka.V + 31) / 32; i += BLOCKS * CL_THREADS) a.present[i] = 0u;
+  for (int64_t i = base / I + tid; i < a.n_huge_done; i += BLOCKS * CL_THREADS) a.huge_done[i] = 0u;
   const int any_bad = __syncthreads_or(bad);
-  cluster.sync();  // every block has started: its shared memory may be written
-  if (tid < CL_BLOCKS) cluster.map_shared_rank(s_bad, tid)[me] = any_bad ? 1u : 0u;
+  sync();  // every block has started: its shared memory may be written
+  if (tid < BLOCKS) of_block(s_bad, tid)[me] = any_bad ? 1u : 0u;
 
   for (int pass = 0; pass < plan.passes; ++pass) {
     const int shift = plan.shift[pass];
@@ -591,11 +603,11 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
       own += c;
     }
 #pragma unroll
-    for (int b = 0; b < CL_BLOCKS; ++b) cluster.map_shared_rank(&s_all[me][tid], b)[0] = own;
-    cluster.sync();  // and every block has read the keys of the pass before
+    for (int b = 0; b < BLOCKS; ++b) of_block(&s_all[me][tid], b)[0] = own;
+    sync();  // and every block has read the keys of the pass before
     if (pass == 0) {  // the same answer in every block
       uint32_t failed = 0u;
-      for (int b = 0; b < CL_BLOCKS; ++b) failed |= s_bad[b];
+      for (int b = 0; b < BLOCKS; ++b) failed |= s_bad[b];
       if (failed) {
         if (me == 0 && tid == 0) raise_error(err, ERR_ID_RANGE);
         return;
@@ -603,7 +615,7 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
     }
     uint32_t total = 0u, before_me = 0u;
 #pragma unroll
-    for (int b = 0; b < CL_BLOCKS; ++b) {
+    for (int b = 0; b < BLOCKS; ++b) {
       const uint32_t c = s_all[b][tid];
       if (b < me) before_me += c;
       total += c;
@@ -627,10 +639,10 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
       const uint32_t d = (key[j] >> shift) & mask;
       const uint32_t pos = s_place[d] + s_cnt[warp][d] + rank[j];  // a permutation of 0 .. 8 PER - 1
       const uint32_t block = pos / PER, slot = pos % PER;
-      cluster.map_shared_rank(s_keys, block)[slot] = key[j];
-      cluster.map_shared_rank(s_vals, block)[slot] = (uint16_t)val[j];
+      of_block(s_keys, block)[slot] = key[j];
+      of_block(s_vals, block)[slot] = (uint16_t)val[j];
     }
-    cluster.sync();
+    sync();
 #pragma unroll
     for (int j = 0; j < I; ++j) {
       key[j] = s_keys[at + j * 32];
@@ -645,7 +657,7 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
       order[p] = val[j];
     }
   }
-  cluster.sync();  // the marks look at other blocks' keys
+  sync();  // the marks look at other blocks' keys
   Marks m[I];
   unsigned long long sum = 0ull;
 #pragma unroll
@@ -665,11 +677,11 @@ __global__ void __cluster_dims__(CL_BLOCKS, 1, 1) __launch_bounds__(CL_THREADS)
     if (w < warp) before += s_warp[w];
     mine += s_warp[w];
   }
-  if (tid < CL_BLOCKS) cluster.map_shared_rank(s_sums, tid)[me] = mine;
-  cluster.sync();
+  if (tid < BLOCKS) of_block(s_sums, tid)[me] = mine;
+  sync();
   unsigned long long all = 0ull;
 #pragma unroll
-  for (int b = 0; b < CL_BLOCKS; ++b) {
+  for (int b = 0; b < BLOCKS; ++b) {
     if (b < me) before += s_sums[b];
     all += s_sums[b];
   }
@@ -1075,8 +1087,12 @@ cudaError_t launch_embed_grad(const EmbedGradArgs& a, char* ws, int64_t wait_ns,
   if (p.small) {
     order = at(p.vals[0]);
     ia.keys = at(p.keys[0]);
-    auto kernel = a.n <= CL_BLOCKS * CL_THREADS ? k_token_small<1> : k_token_small<2>;
-    e = launch_following(kernel, dim3(CL_BLOCKS), CL_THREADS, 0, s, ka, p.sort, ia, at(p.keys[0]), at(p.vals[0]),
+    const bool one = a.n <= 2 * CL_THREADS;
+    auto kernel = a.n <= CL_THREADS               ? k_token_small<1, 1>
+                  : one                           ? k_token_small<2, 1>
+                  : a.n <= CL_BLOCKS * CL_THREADS ? k_token_small<1, CL_BLOCKS>
+                                                  : k_token_small<2, CL_BLOCKS>;
+    e = launch_following(kernel, dim3(one ? 1 : CL_BLOCKS), CL_THREADS, 0, s, ka, p.sort, ia, at(p.keys[0]), at(p.vals[0]),
                          a.err);
     if (e != cudaSuccess) return e;
   } else {

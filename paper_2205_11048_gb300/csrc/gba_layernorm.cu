@@ -655,10 +655,13 @@ __global__ void __launch_bounds__(LANES ? THREADS : 512) k_layer_norm_grad(Layer
   f2 dg[P], db[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) dg[i] = db[i] = pair(0.f, 0.f);
+  // The checks of a row's end leave no registers for the next row's loads beside 16 columns of 16
+  // bits (f16 136,696 x 432: 107 us with them in flight, 79 without).
+  constexpr bool AHEAD = FETCH && !(sizeof(T) == 2 && E == 16);
   if (at.whole)
     grad_rows<T, V, E, LANES, FETCH, true>(a, sp, at, s_sum, dg, db);
   else
-    grad_rows<T, V, E, LANES, FETCH, false>(a, sp, at, s_sum, dg, db);
+    grad_rows<T, V, E, LANES, AHEAD, false>(a, sp, at, s_sum, dg, db);
   write_partial<V, E, LANES>(a, sp, at, dg, db, s_part);
 }
 
@@ -919,6 +922,17 @@ cudaError_t launch_ring(F* kernel, const RingShape& r, const LayerNormArgs& a, c
   return launch_following(kernel, dim3(grid), 32 * r.split.W * r.groups, r.smem, s, a, r.split, r.stages, w.err, w.limit_ns);
 }
 
+template <typename T, int V, int E>
+cudaError_t norm_wide(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
+  auto smem_of = [](int w) { return (size_t)w * 32 * E * 2 * sizeof(float); };
+  static const Residency held(k_layer_norm<T, V, E, false>, E, smem_of);
+  int threads;
+  const Split sp = warps_of(a.d, E, &threads);
+  return launch_following(k_layer_norm<T, V, E, false>,
+                          dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s, a,
+                          sp);
+}
+
 template <typename T, int V>
 cudaError_t norm_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cudaStream_t s) {
   constexpr int EL = E_LANES<V>, E = E_NORM<T, V>;
@@ -945,13 +959,13 @@ cudaError_t norm_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cuda
   if (a.d > MOST_WARPS * 32 * E)
     return launch_following(k_layer_norm_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 2)),
                             WIDE_THREADS, 0, s, a);
-  auto smem_of = [](int w) { return (size_t)w * 32 * E * 2 * sizeof(float); };
-  static const Residency held(k_layer_norm<T, V, E, false>, E, smem_of);
-  int threads;
-  const Split sp = warps_of(a.d, E, &threads);
-  return launch_following(k_layer_norm<T, V, E, false>,
-                          dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s, a,
-                          sp);
+  // rows of one warp and two or three vectors a lane hold no more than that (bf16 100,000 x 400:
+  // 33 us, and 52 with four)
+  if constexpr (E > 2 * V && V > 1) {
+    if (a.d <= 64 * V) return norm_wide<T, V, 2 * V>(a, num_sms, s);
+    if (a.d <= 96 * V) return norm_wide<T, V, 3 * V>(a, num_sms, s);
+  }
+  return norm_wide<T, V, E>(a, num_sms, s);
 }
 
 // How a gradient's rows are held: a vector a lane, with the next row's loads in flight, without

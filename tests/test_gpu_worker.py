@@ -512,6 +512,13 @@ def test_layer_norm_of_many_wide_rows(w, dtype, n, d, extra):
     check_layer_norm(w, dtype, n, d, extra, extra, False)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS.get)
+@pytest.mark.parametrize("n,d", [(50, 136), (41, 150), (40, 392), (700, 432), (9, 512), (33, 600), (21, 776), (5, 78),
+                                 (6, 260), (3, 1030)])
+def test_layer_norm_of_rows_about_a_warp_wide(w, dtype, n, d):
+    check_layer_norm(w, dtype, n, d, 0, 0, True)
+
+
 def check_layer_norm(w, dtype, n, d, extra, offset, own_params):
     g = gen(n + d)
     eps = 1e-5
