@@ -10,10 +10,11 @@
 // (two sums over lanes and warps, a root, addresses) costs as many instructions as ten
 // columns or so, so a thread of a wide row holds 64 bytes of it (backward 32 of each of the
 // two), the arithmetic is done on pairs, and a warp whose columns all exist checks none of
-// them.  Backward, a block keeps its threads' shares of
-// dgamma and dbeta in registers over all the rows it takes and leaves one partial row; a
-// second kernel adds the partial rows in order.  Rows too wide for a block's registers are
-// read again from L2 instead.
+// them.  Rows off the 16-byte boundary are read by the vectors that fit them, elements at
+// worst: by aligned words and a shift, as the lookup reads them, f16 35,710 x 1,161 took 83 us
+// against 49.  Backward, a block keeps its threads' shares of dgamma and dbeta in registers over
+// all the rows it takes and leaves one partial row; a second kernel adds the partial rows in
+// order.  Rows too wide for a block's registers are read again from L2 instead.
 //
 // Measured, of the copy bandwidth of 6.7 TB/s: forward bf16 32,768 x 4,096 94 us (86%),
 // 65,536 x 1,024 46.5 (86%), float32 16,384 x 4,096 88 (91%), f16 35,710 x 1,161 49 (50%, single
