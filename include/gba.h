@@ -331,9 +331,13 @@ gba_status gba_join(gba_handle* h);
  * order fixed by the sizes: the same call gives the same bits.
  *
  * All work of a worker handle is issued on its stream, in call order, and uses
- * the handle's workspace, which grows on demand (a call that grows it waits for
- * the stream; the calls that follow at that size or below allocate nothing and
- * may be captured into a CUDA graph).  Pointers are device memory.  A call that
+ * the handle's workspace, which grows on demand (a call that grows it allocates; the
+ * calls that follow at that size or below do not and may be captured into a CUDA
+ * graph).  A captured call works on the workspace of its capture: workspaces that
+ * larger ones replaced are kept, up to four times the last one's size in all, so
+ * graphs can be replayed until gba_worker_destroy.  A replay is work of the
+ * handle like any other: not beside its other calls or replays, but ordered with
+ * them.  Pointers are device memory.  A call that
  * returns an error has enqueued nothing that writes to its outputs, except for
  * GBA_E_CUDA.  What only a kernel can see (an id out of range, a bounded wait
  * that gave up) is kept until gba_worker_sync reports it.
@@ -361,7 +365,8 @@ typedef struct {
  * the last gba_worker_sync: GBA_E_ID_RANGE (an id out of range) or
  * GBA_E_DEVICE_TIMEOUT; the handle can be used on.
  * gba_worker_last_error - text of the handle's last failure ("" if none).
- * gba_worker_destroy - wait for the stream and free the workspace (NULL: no-op). */
+ * gba_worker_destroy - wait for the stream and free the workspaces (NULL: no-op);
+ * graphs that hold calls of the handle must not run any more. */
 gba_status gba_worker_create(void* cuda_stream, gba_worker** out);
 gba_status gba_worker_sync(gba_worker* w);
 const char* gba_worker_last_error(gba_worker* w);

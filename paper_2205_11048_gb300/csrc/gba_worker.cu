@@ -21,6 +21,10 @@ struct gba_worker {
   cudaEvent_t event = nullptr;  // orders a lookup in a server's table
   char* ws = nullptr;
   size_t ws_bytes = 0;
+  // Workspaces that a larger one took the place of.  Graphs captured before hold their addresses.
+  // One is at least 1.25 times the one before, and the first 256 bytes, so 128 are never reached.
+  char* old_ws[128];
+  int n_old = 0;
   uint32_t* words = nullptr;   // device: the latched errors, a ticket
   uint32_t* h_flag = nullptr;  // mapped pinned: something is latched
   ErrSink sink{};
@@ -45,17 +49,15 @@ gba_status cuda_fail(gba_worker* w, cudaError_t e, const char* what) {
   return e == cudaErrorMemoryAllocation ? GBA_E_OOM : GBA_E_CUDA;
 }
 
-// The workspace, at least `bytes` of it.
+// The workspace, at least `bytes` of it.  What it replaces lives on until the handle is destroyed.
 gba_status reserve(gba_worker* w, size_t bytes) {
   if (bytes <= w->ws_bytes) return GBA_OK;
-  const size_t want = bytes + bytes / 4;
-  cudaError_t e = cudaStreamSynchronize(w->stream);  // earlier calls still use the old one
-  if (e != cudaSuccess) return cuda_fail(w, e, "wait for the worker's stream");
-  cudaFree(w->ws);
-  w->ws = nullptr;
-  w->ws_bytes = 0;
-  e = cudaMalloc((void**)&w->ws, want);
+  const size_t want = (bytes + bytes / 4 + 255) / 256 * 256;
+  char* ws = nullptr;
+  const cudaError_t e = cudaMalloc((void**)&ws, want);
   if (e != cudaSuccess) return cuda_fail(w, e, "allocate the worker's workspace");
+  if (w->ws) w->old_ws[w->n_old++] = w->ws;
+  w->ws = ws;
   w->ws_bytes = want;
   return GBA_OK;
 }
@@ -234,6 +236,7 @@ void gba_worker_destroy(gba_worker* w) {
   if (!w) return;
   cudaSetDevice(w->device);
   cudaStreamSynchronize(w->stream);
+  for (int i = 0; i < w->n_old; ++i) cudaFree(w->old_ws[i]);
   cudaFree(w->ws);
   cudaFree(w->words);
   if (w->h_flag) cudaFreeHost(w->h_flag);
