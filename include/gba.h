@@ -393,7 +393,9 @@ gba_status gba_embed(gba_worker* w, const gba_matrix* weights, int32_t id_mode,
  * reserved id INT64_MIN counts as out of range).  Ordered, on the device, after
  * every step of h enqueued so far and before every later one, whatever the two
  * handles' streams.  Both handles belong to one device and are used by the
- * calling thread.
+ * calling thread.  A captured lookup (worker and server on one stream, the server's
+ * steps joined before) reads the table as it is when the graph runs, a HASH table that
+ * has grown since too; the program orders the replays with the server's steps.
  */
 gba_status gba_embed_table(gba_worker* w, gba_handle* h, int32_t t, const int64_t* ids,
                            int64_t n, float scale, int64_t pad_id, const gba_matrix* out);

@@ -129,8 +129,13 @@ __global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
   const int64_t groups = (int64_t)gridDim.x * (THREADS >> lg);
   const int64_t g0 = ((int64_t)blockIdx.x * THREADS + threadIdx.x) >> lg;
   const int64_t c0 = ((int64_t)blockIdx.y * K * L + l) * V;
-  const char* lo = static_cast<const char*>(a.w);
-  const char* hi = lo + ((uint64_t)(a.V - 1) * (uint64_t)a.w_stride + (uint64_t)a.d) * sizeof(TI);
+  // A HASH table is where its description says at the time: a captured lookup runs on after the
+  // table has moved to more slots.
+  const bool hash = a.id_mode == GBA_ID_HASH;
+  const TI* w = static_cast<const TI*>(hash ? static_cast<const void*>(a.hinfo->w) : a.w);
+  const uint64_t rows = hash ? a.hinfo->mask + 1 : (uint64_t)a.V;
+  const char* lo = reinterpret_cast<const char*>(w);
+  const char* hi = lo + ((rows - 1) * (uint64_t)a.w_stride + (uint64_t)a.d) * sizeof(TI);
   int64_t next = g0 < a.n ? a.ids[g0] : 0;
   for (int64_t i = g0; i < a.n; i += groups) {
     const int64_t id = next;
@@ -157,7 +162,7 @@ __global__ void __launch_bounds__(THREADS) k_embed(EmbedArgs a, int lg) {
         zero = true;
       }
     }
-    const TI* src = static_cast<const TI*>(a.w) + row * (uint64_t)a.w_stride;
+    const TI* src = w + row * (uint64_t)a.w_stride;
     TO* dst = static_cast<TO*>(a.out) + (uint64_t)i * (uint64_t)a.out_stride;
     std::conditional_t<R != EVEN, Loose<TI>, Pack<TI, V>> in[K];
     if (!zero && !fresh) {

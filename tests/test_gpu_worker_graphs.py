@@ -54,3 +54,34 @@ def test_a_graph_outlives_the_growth_of_the_workspace(n, more):
         w.sync()
         del graph
     w.close()
+
+
+@pytest.mark.parametrize("dim", [20, 33])
+def test_a_captured_lookup_follows_a_hash_table_that_grows(dim):
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        w = B.Worker()
+        srv = B.GBA([(64, dim, B.HASH, 4096, B.opt_desc(B.ADAGRAD, 0.05))], 0, None, 1, 4, seed=11)
+        none = torch.empty(0, device="cuda")
+        ids = torch.arange(3000, device="cuda") * 7_777_777_777 - 2**40
+        asked = torch.cat([ids[::7], ids[:1] + 1])
+        first = ids[:20].clone()
+        srv.push(0, [first], [torch.ones(20, dim, device="cuda")], none, 1)
+        assert srv.try_apply() == 1
+        w.embed_table(srv, 0, asked, scale=3.0)
+        srv.sync()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            y = w.embed_table(srv, 0, asked, scale=3.0)
+        for step in (1, 2):
+            srv.push(step, [ids], [torch.ones(3000, dim, device="cuda")], none, 1)
+            assert srv.try_apply() == 1
+            graph.replay()
+            got = y.clone()
+            assert torch.equal(got, w.embed_table(srv, 0, asked, scale=3.0))
+            assert torch.equal(got, (srv.pull(0, asked).double() * 3.0).float())
+        w.sync()
+        srv.sync()
+        del graph
+        srv.close()
+    w.close()
