@@ -920,6 +920,10 @@ __device__ __forceinline__ void add_parts(const SumArgs& a, uint32_t first_cut, 
   }
 }
 
+// hi is the plain sum.  Once that is an infinity its correction is a NaN (inf - inf), and the sum
+// is what a run of one item gives: the infinity, or the NaN that hi has become since.
+__device__ __forceinline__ float sum_value(const CSum& x) { return isfinite(x.hi) ? csum_value(x) : x.hi; }
+
 // aligned: rows of the output start on 16 bytes and are whole numbers of them.
 __device__ __forceinline__ void write_parts(const SumArgs& a, uint32_t run, int64_t c, const CSum (&x)[4],
                                             bool aligned) {
@@ -927,7 +931,7 @@ __device__ __forceinline__ void write_parts(const SumArgs& a, uint32_t run, int6
   float* dst = sum_at(a, run, c);
   float y[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) y[j] = csum_value(x[j]);
+  for (int j = 0; j < 4; ++j) y[j] = sum_value(x[j]);
   if (aligned) {
     write_sum<4>(a, dst, y);
     return;
