@@ -862,6 +862,15 @@ Split warps_of(int32_t d, int E, int* threads) {
   return s;
 }
 
+// Lets launches of a kernel on the current device use `most` bytes of dynamic shared memory.  The
+// attribute belongs to a device and a process may use several, so each launch of more than
+// SMEM_FREE sets it (48 KB are allowed without, the kernel's own included).
+constexpr size_t SMEM_FREE = 47 * 1024;
+template <typename F>
+cudaError_t allow_smem(F* kernel, size_t most) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 // Blocks of a kernel for wide rows that an SM holds, for each number of warps of a row.
 struct Residency {
   int blocks[MOST_WARPS + 1];
@@ -922,7 +931,7 @@ bool ring_serves(const RingShape& r, int64_t n, int num_sms) {
 template <typename F>
 cudaError_t launch_ring(F* kernel, const RingShape& r, const LayerNormArgs& a, const RingWait& w, unsigned grid,
                         cudaStream_t s) {
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+  const cudaError_t e = allow_smem(kernel, 220 * 1024);
   if (e != cudaSuccess) return e;
   return launch_following(kernel, dim3(grid), 32 * r.split.W * r.groups, r.smem, s, a, r.split, r.stages, w.err, w.limit_ns);
 }
@@ -933,6 +942,10 @@ cudaError_t norm_wide(const LayerNormArgs& a, int num_sms, cudaStream_t s) {
   static const Residency held(k_layer_norm<T, V, E, false>, E, smem_of);
   int threads;
   const Split sp = warps_of(a.d, E, &threads);
+  if (smem_of(sp.W) > SMEM_FREE) {  // the same limit each time, whatever other threads launch
+    const cudaError_t e = allow_smem(k_layer_norm<T, V, E, false>, smem_of(MOST_WARPS));
+    if (e != cudaSuccess) return e;
+  }
   return launch_following(k_layer_norm<T, V, E, false>,
                           dim3(grid_of(a.n, sp, threads, num_sms, held.blocks[sp.W])), threads, smem_of(sp.W), s, a,
                           sp);
