@@ -871,18 +871,19 @@ cudaError_t allow_smem(F* kernel, size_t most) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
 }
 
-// Blocks of a kernel for wide rows that an SM holds, for each number of warps of a row.
+// Blocks of a kernel for wide rows that an SM holds, for each number of warps of a row.  The answers
+// depend on the attribute, which comes first, and are those of any device that runs this
+// architecture's code.
 struct Residency {
   int blocks[MOST_WARPS + 1];
   template <typename F, typename S>
   Residency(F* kernel, int E, S smem_of) {
+    if (smem_of(MOST_WARPS) > SMEM_FREE) allow_smem(kernel, smem_of(MOST_WARPS));
     for (int w = 1; w <= MOST_WARPS; ++w) {
       int threads;
       warps_of(w * 32 * E, E, &threads);
       const size_t smem = smem_of(w);
       blocks[w] = 0;
-      if (smem > 48 * 1024)
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
       if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks[w], kernel, threads, smem) != cudaSuccess ||
           blocks[w] < 1)
         blocks[w] = 1;

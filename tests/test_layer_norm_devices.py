@@ -45,3 +45,13 @@ def test_every_width_is_launched_on_every_device(F, type, grad):
                 for stride in (d, d + 4, d + 1):
                     assert F.fake_layer_norm(n, d, stride, type, grad) == 0, (device, d, n, stride)
     assert F.fake_refused() == 0
+
+
+@pytest.mark.parametrize("type,d,stride", [
+    (B.BF16, 5120, 5124), (B.BF16, 5124, 5128), (B.F16, 6144, 6148), (B.BF16, 6148, 6156), (B.F32, 5632, 5634),
+    (B.F32, 5634, 5636), (B.F32, 6144, 6146), (B.F32, 6146, 6150), (B.F32, 6143, 6143)])
+def test_the_grid_fills_the_sms_whatever_the_parameters_shared_memory(F, type, d, stride):
+    """Parameters of 48 KB to the byte, a little less and a little more."""
+    assert F.fake_layer_norm(1_000_000, d, stride, type, 0) == 0
+    assert F.fake_held() >= 3
+    assert F.fake_grid() == 152 * F.fake_held()
