@@ -534,12 +534,6 @@ def _type_of(t):
         _refuse(f"tensors are float32, bfloat16 or float16, not {t.dtype}")
 
 
-def _on_gpu(*tensors):
-    for t in tensors:
-        if t is not None and not t.is_cuda:
-            _refuse("a tensor is not on the GPU")
-
-
 def _matrix(t):
     """t as a gba_matrix: two dimensions, rows of consecutive elements."""
     shape, strides = t.shape, t.stride()
@@ -570,8 +564,10 @@ class GradParts:
         out = grads if out is None else list(out)
         if len(out) != len(grads):
             _refuse("as many outputs as gradients")
+        self.device = (grads[0].get_device() if grads else None)  # checked against the worker's
         for t in (*grads, *out):
-            _on_gpu(t)
+            if t.get_device() != self.device or self.device < 0:
+                _refuse("gradients and their outputs are on one GPU")
             if not t.is_contiguous():
                 _refuse("gradients and their outputs are contiguous")
         for g, o in zip(grads, out):
@@ -634,6 +630,17 @@ class Worker:
         if status < 0:
             self._check(status, name)
 
+    def _mine(self, *tensors):
+        for t in tensors:
+            if t is not None and t.get_device() != self._index:
+                _refuse("a tensor is not on the worker's GPU")
+
+    def _parts(self, grads):
+        p = grads if isinstance(grads, GradParts) else GradParts(grads)
+        if p.n and p.device != self._index:
+            _refuse("a tensor is not on the worker's GPU")
+        return p
+
     def _new(self, *shape, dtype=None):
         return self.torch.empty(shape, dtype=dtype or self.torch.float32, device=self._device)
 
@@ -648,20 +655,20 @@ class Worker:
     def _ids(self, ids):
         if ids.dtype != self.torch.int64:
             _refuse("ids are int64")
-        _on_gpu(ids)
+        self._mine(ids)
         return ids.contiguous()
 
     def _embed_out(self, ids, d, dtype, out):
         if out is None:
             out = self._new(*ids.shape, d, dtype=dtype)
-        _on_gpu(out)
+        self._mine(out)
         flat = out if out.dim() == 2 else out.view(ids.numel(), d)
         return out, _matrix(flat)
 
     def embed(self, weights, ids, scale=1.0, pad_id=None, dtype=None, id_mode=DIRECT, out=None):
         """scale * weights[ids] in dtype (default: the weights'); padding gives zeros."""
         ids = self._ids(ids)
-        _on_gpu(weights)
+        self._mine(weights)
         out, om = self._embed_out(ids, weights.shape[-1], dtype or weights.dtype, out)
         self._call("gba_embed", _matrix(weights), id_mode, ids.data_ptr(), ids.numel(), scale,
                    NO_PAD if pad_id is None else pad_id, om)
@@ -683,7 +690,7 @@ class Worker:
         order; those after repeat the last one's id with zeros."""
         torch = self.torch
         ids, grad = self._ids(ids), _rows_of(grad)
-        _on_gpu(grad)
+        self._mine(grad)
         n, d = ids.numel(), grad.shape[1]
         ids_out = self._new(n, dtype=torch.int64)
         rows_out = self._new(n, d)
@@ -696,14 +703,14 @@ class Worker:
     def embed_grad_dense(self, ids, grad, out, scale=1.0, pad_id=None, id_mode=DIRECT, accumulate=False):
         """The lookup's gradient over all rows of the table, into (or added to) out."""
         ids, grad = self._ids(ids), _rows_of(grad)
-        _on_gpu(grad, out)
+        self._mine(grad, out)
         self._call("gba_embed_grad_dense", ids.data_ptr(), ids.numel(), _matrix(grad), id_mode, scale,
                    NO_PAD if pad_id is None else pad_id, _matrix(out), int(accumulate))
         return out
 
     def grad_norm(self, grads):
         """The 2-norm of all the tensors together (a list, or grad_parts of it), on the device."""
-        p = grads if isinstance(grads, GradParts) else GradParts(grads)
+        p = self._parts(grads)
         norm = self._new()
         self._call("gba_grad_norm", p.array, p.n, norm.data_ptr())
         return norm
@@ -711,7 +718,7 @@ class Worker:
     def clip_grads(self, grads, max_norm):
         """Scales the tensors (a list, or grad_parts of it) by min(1, max_norm / (norm + 1e-6)),
         in place or into the parts' outputs; returns the norm."""
-        p = grads if isinstance(grads, GradParts) else GradParts(grads)
+        p = self._parts(grads)
         norm = self._new()
         self._call("gba_clip_grads", p.array, p.n, max_norm, norm.data_ptr())
         return norm
@@ -722,7 +729,7 @@ class Worker:
             if p is None:
                 at.append(None)
                 continue
-            _on_gpu(p)
+            self._mine(p)
             if p.numel() != d or not p.is_contiguous():
                 _refuse("a parameter has a value per column")
             if kind is not None and kind != _type_of(p):
@@ -733,7 +740,7 @@ class Worker:
 
     def layer_norm(self, x, gamma=None, beta=None, eps=1e-5):
         """(y, mean, rstd) of the rows of x (its last dimension)."""
-        _on_gpu(x)
+        self._mine(x)
         rows = _rows_of(x)
         n, d = rows.shape
         y = self._new(n, d, dtype=x.dtype)
@@ -746,7 +753,7 @@ class Worker:
     def layer_norm_grad(self, dy, x, gamma, mean, rstd):
         """(dx, dgamma, dbeta) from the gradient of layer_norm's y and its mean and rstd."""
         torch = self.torch
-        _on_gpu(dy, x, mean, rstd)
+        self._mine(dy, x, mean, rstd)
         xr, dr = _rows_of(x), _rows_of(dy)
         n, d = xr.shape
         if mean.numel() != n or rstd.numel() != n or {mean.dtype, rstd.dtype} != {torch.float32}:
