@@ -337,7 +337,8 @@ gba_status gba_join(gba_handle* h);
  * larger ones replaced are kept, up to four times the last one's size in all, so
  * graphs can be replayed until gba_worker_destroy.  A replay is work of the
  * handle like any other: not beside its other calls or replays, but ordered with
- * them.  Pointers are device memory.  A call that
+ * them.  Pointers are memory of the handle's device, which need not be the current
+ * one (the current one stays what it was).  A call that
  * returns an error has enqueued nothing that writes to its outputs, except for
  * GBA_E_CUDA.  What only a kernel can see (an id out of range, a bounded wait
  * that gave up) is kept until gba_worker_sync reports it.

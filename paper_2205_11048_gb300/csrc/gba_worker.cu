@@ -49,6 +49,21 @@ gba_status cuda_fail(gba_worker* w, cudaError_t e, const char* what) {
   return e == cudaErrorMemoryAllocation ? GBA_E_OOM : GBA_E_CUDA;
 }
 
+// Makes the handle's device current for a call, and the caller's again at its end.
+struct OnDevice {
+  int before = -1;
+  bool moved = false;
+  explicit OnDevice(int device) {
+    moved = cudaGetDevice(&before) == cudaSuccess && before != device;
+    if (moved) cudaSetDevice(device);
+  }
+  ~OnDevice() {
+    if (moved) cudaSetDevice(before);
+  }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+};
+
 // The workspace, at least `bytes` of it.  What it replaces lives on until the handle is destroyed.
 gba_status reserve(gba_worker* w, size_t bytes) {
   if (bytes <= w->ws_bytes) return GBA_OK;
@@ -215,7 +230,7 @@ gba_status gba_worker_create(void* cuda_stream, gba_worker** out) {
 
 gba_status gba_worker_sync(gba_worker* w) {
   if (!w) return GBA_E_ARG;
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   cudaError_t e = cudaStreamSynchronize(w->stream);
   if (e != cudaSuccess) return cuda_fail(w, e, "wait for the worker's stream");
   if (*(volatile uint32_t*)w->h_flag == 0u) return GBA_OK;
@@ -234,7 +249,7 @@ const char* gba_worker_last_error(gba_worker* w) { return w ? w->last_error : ""
 
 void gba_worker_destroy(gba_worker* w) {
   if (!w) return;
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   cudaStreamSynchronize(w->stream);
   for (int i = 0; i < w->n_old; ++i) cudaFree(w->old_ws[i]);
   cudaFree(w->ws);
@@ -252,7 +267,7 @@ gba_status gba_embed(gba_worker* w, const gba_matrix* weights, int32_t id_mode, 
   if (!bad) bad = bad_matrix(out);
   if (!bad && overlap(weights->data, span(weights), out->data, span(out))) bad = "out overlaps the weights";
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   EmbedArgs a{};
   a.w = weights->data;
   a.w_stride = weights->stride;
@@ -266,11 +281,12 @@ gba_status gba_embed(gba_worker* w, const gba_matrix* weights, int32_t id_mode, 
 gba_status gba_embed_table(gba_worker* w, gba_handle* h, int32_t t, const int64_t* ids, int64_t n,
                            float scale, int64_t pad_id, const gba_matrix* out) {
   if (!w) return GBA_E_ARG;
+  const OnDevice on(w->device);
   TableView v{};
-  const gba_status st = table_view(h, t, &v);
+  const gba_status st = table_view(h, t, &v);  // makes the server's device current
+  if (st != GBA_OK || v.device != w->device) cudaSetDevice(w->device);
   if (st != GBA_OK) return fail(w, st, "no such table of a working handle");
   if (v.device != w->device) return fail(w, GBA_E_ARG, "the worker and the server are on different devices");
-  cudaSetDevice(w->device);
   EmbedArgs a{};
   a.w = v.w;
   a.w_stride = v.dim;
@@ -310,7 +326,7 @@ gba_status gba_embed_grad(gba_worker* w, const int64_t* ids, int64_t n, const gb
                overlap(ids, (uint64_t)n * 8, ids_out, (uint64_t)n * 8)))
     bad = "an output overlaps an input";
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   if (n == 0) {
     const cudaError_t e = cudaMemsetAsync(n_out, 0, 8, w->stream);
     return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "clear n_out");
@@ -348,7 +364,7 @@ gba_status gba_embed_grad_dense(gba_worker* w, const int64_t* ids, int64_t n, co
                overlap(ids, (uint64_t)n * 8, out->data, span(out))))
     bad = "an output overlaps an input";
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   EmbedGradArgs a{};
   a.ids = ids;
   a.n = n;
@@ -373,7 +389,7 @@ gba_status gba_grad_norm(gba_worker* w, const gba_grad_part* parts, int32_t n_pa
   if (!bad && !norm) bad = "norm is NULL";
   if (!bad) bad = bad_floats(norm);
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   return run_norm(w, parts, n_parts, false, 0.f, norm);
 }
 
@@ -384,7 +400,7 @@ gba_status gba_clip_grads(gba_worker* w, const gba_grad_part* parts, int32_t n_p
   if (!bad && !(max_norm >= 0.f)) bad = "max_norm is negative or NaN";
   if (!bad) bad = bad_floats(norm);
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   return run_norm(w, parts, n_parts, true, max_norm, norm);
 }
 
@@ -402,7 +418,7 @@ gba_status gba_layer_norm(gba_worker* w, const gba_matrix* x, const void* gamma,
   if (!bad && !(eps >= 0.f && std::isfinite(eps))) bad = "eps is negative or not finite";
   if (bad) return fail(w, GBA_E_ARG, bad);
   if (x->rows == 0) return GBA_OK;
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   LayerNormArgs a{};
   a.x = x->data;
   a.x_stride = x->stride;
@@ -436,7 +452,7 @@ gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_ma
   for (const float* p : {mean, rstd, (const float*)dgamma, (const float*)dbeta})
     if (!bad) bad = bad_floats(p);
   if (bad) return fail(w, GBA_E_ARG, bad);
-  cudaSetDevice(w->device);
+  const OnDevice on(w->device);
   if (x->rows == 0) {
     for (float* p : {dgamma, dbeta}) {
       const cudaError_t e = p ? cudaMemsetAsync(p, 0, (size_t)x->cols * 4, w->stream) : cudaSuccess;
