@@ -587,10 +587,10 @@ def grad_parts(grads, out=None):
 
 
 class Worker:
-    """A worker's operators on the current CUDA device: lookups and their gradient, norm and
-    clipping, layer norm (see include/gba.h).
+    """A worker's operators on one CUDA device: lookups and their gradient, norm and clipping,
+    layer norm (see include/gba.h).
 
-    Work is issued on `stream` (default: the current one).  A call made while another stream
+    Work is issued on `stream` (default: the current one), on the stream's device.  A call made while another stream
     is current orders the two both ways, so tensors of the current stream can be passed and
     results used there."""
 
@@ -601,10 +601,11 @@ class Worker:
         self.h = None
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self._raw_stream = self.stream.cuda_stream
-        self._index = torch.cuda.current_device()
-        self._device = torch.device("cuda", self._index)
+        self._device = self.stream.device
+        self._index = self._device.index
         h = _P()
-        check(self.L.gba_worker_create(self._raw_stream, ctypes.byref(h)), what="gba_worker_create")
+        with torch.cuda.device(self._device):
+            check(self.L.gba_worker_create(self._raw_stream, ctypes.byref(h)), what="gba_worker_create")
         self.h = h
 
     def close(self):

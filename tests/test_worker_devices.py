@@ -99,3 +99,41 @@ def test_parts_made_for_another_device_are_refused(w, device):
     assert w.L.calls == []
     w.grad_norm(B.grad_parts([]))
     assert w.L.calls == ["gba_grad_norm"]
+
+
+def test_a_worker_is_made_on_its_streams_device(monkeypatch):
+    made = []
+
+    class Current:  # stands for torch.cuda.device
+        now = 0
+
+        def __init__(self, device):
+            self.device = torch.device(device).index
+
+        def __enter__(self):
+            self.before, Current.now = Current.now, self.device
+
+        def __exit__(self, *_):
+            Current.now = self.before
+
+    class Stream:
+        cuda_stream, device = 5, torch.device("cuda", 1)
+
+    class Maker:
+        def gba_worker_create(self, stream, out):
+            made.append((stream, Current.now))
+            return B.GBA_OK
+
+        def gba_worker_destroy(self, h):
+            pass
+
+    monkeypatch.setattr(B, "load", Maker)
+    monkeypatch.setattr(torch.cuda, "device", Current)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: Current.now)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream)
+    for stream in (Stream, None):
+        w = B.Worker(stream)
+        assert made.pop() == (5, 1) and Current.now == 0
+        with pytest.raises(B.GBAError):
+            w._mine(on(0, 3))
+        w._mine(on(1, 3))
