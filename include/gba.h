@@ -340,7 +340,10 @@ gba_status gba_join(gba_handle* h);
  * them.  Pointers are memory of the handle's device, which need not be the current
  * one (the current one stays what it was).  A call that
  * returns an error has enqueued nothing that writes to its outputs, except for
- * GBA_E_CUDA.  What only a kernel can see (an id out of range, a bounded wait
+ * GBA_E_CUDA.  No output may overlap an input or another output unless its
+ * description allows it; this is checked, except among the arrays of layer norm that
+ * are no matrices (gamma, beta, mean, rstd, dgamma, dbeta) and between the parts of a
+ * list.  What only a kernel can see (an id out of range, a bounded wait
  * that gave up) is kept until gba_worker_sync reports it.
  */
 typedef struct gba_worker gba_worker;
@@ -449,8 +452,8 @@ typedef struct {
 
 /*
  * gba_grad_norm - the 2-norm of all elements of n_parts (up to 2^20) tensors together,
- * as one device float32 (out is not looked at).  Squares neither overflow nor vanish: the
- * norm is right wherever it is a float32.
+ * as one device float32, written when all have been read (out is not looked at).  Squares
+ * neither overflow nor vanish: the norm is right wherever it is a float32.
  * gba_clip_grads - the norm N, and out = c * grad with c = min(1, max_norm / (N + 1e-6))
  * for every part (norm may be NULL).  With a norm that is infinite c is 0, with a NaN it
  * is NaN: the gradients of such a message are lost, and *norm says so.  max_norm >= 0.

@@ -115,6 +115,7 @@ gba_status run_embed(gba_worker* w, EmbedArgs& a, int32_t type, const int64_t* i
   const char* bad = bad_matrix(out);
   if (!bad) bad = bad_ids(ids, n);
   if (!bad && (out->rows != n || out->cols != a.d)) bad = "out is not n x the table's width";
+  if (!bad && overlap(ids, (uint64_t)n * 8, out->data, span(out))) bad = "out overlaps the ids";
   if (!bad && type != GBA_F32 && out->type != GBA_F32 && out->type != type)
     bad = "weights of 16 bits give their own type or float32";
   if (bad) return fail(w, GBA_E_ARG, bad);
@@ -140,7 +141,8 @@ gba_status run_embed_grad(gba_worker* w, EmbedGradArgs& a) {
   return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "launch the lookup's gradient");
 }
 
-const char* bad_parts(const gba_grad_part* parts, int32_t n_parts, bool clip) {
+// norm: where clipping writes it (it reads the gradients again after that), or null
+const char* bad_parts(const gba_grad_part* parts, int32_t n_parts, bool clip, const float* norm) {
   if (n_parts < 0 || n_parts > (1 << 20)) return "n_parts outside [0, 2^20]";
   if (n_parts > 0 && !parts) return "parts is NULL";
   for (int32_t i = 0; i < n_parts; ++i) {
@@ -154,6 +156,9 @@ const char* bad_parts(const gba_grad_part* parts, int32_t n_parts, bool clip) {
     if (p.out_type < GBA_F32 || p.out_type > GBA_F16) return "unknown type";
     if (!p.out) return "a part's out is NULL";
     if ((uintptr_t)p.out % type_bytes(p.out_type) != 0) return "a part's out is not aligned to its type";
+    if (norm && (overlap(norm, 4, p.grad, (uint64_t)p.n * type_bytes(p.type)) ||
+                 overlap(norm, 4, p.out, (uint64_t)p.n * type_bytes(p.out_type))))
+      return "norm overlaps a part";
     if (p.out == p.grad) {
       if (p.out_type != p.type) return "a part clipped in place keeps its type";
     } else if (overlap(p.grad, (uint64_t)p.n * type_bytes(p.type), p.out,
@@ -322,9 +327,16 @@ gba_status gba_embed_grad(gba_worker* w, const int64_t* ids, int64_t n, const gb
   if (!bad && n > 0 && (!ids_out || !rows_out)) bad = "ids_out or rows_out is NULL";
   if (!bad && ((uintptr_t)ids_out % 8 != 0 || (uintptr_t)rows_out % 16 != 0))
     bad = "ids_out not 8-byte or rows_out not 16-byte aligned";
-  if (!bad && (overlap(grad->data, span(grad), rows_out, (uint64_t)n * grad->cols * 4) ||
-               overlap(ids, (uint64_t)n * 8, ids_out, (uint64_t)n * 8)))
-    bad = "an output overlaps an input";
+  if (!bad) {
+    const struct {
+      const void* p;
+      uint64_t bytes;
+    } at[] = {{ids, (uint64_t)n * 8}, {grad->data, span(grad)},  // the inputs, then the outputs
+              {ids_out, (uint64_t)n * 8}, {rows_out, (uint64_t)n * grad->cols * 4}, {n_out, 8}};
+    for (int i = 2; i < 5; ++i)
+      for (int j = 0; j < i; ++j)
+        if (overlap(at[i].p, at[i].bytes, at[j].p, at[j].bytes)) bad = "an output overlaps an input or another output";
+  }
   if (bad) return fail(w, GBA_E_ARG, bad);
   const OnDevice on(w->device);
   if (n == 0) {
@@ -385,7 +397,7 @@ gba_status gba_embed_grad_dense(gba_worker* w, const int64_t* ids, int64_t n, co
 
 gba_status gba_grad_norm(gba_worker* w, const gba_grad_part* parts, int32_t n_parts, float* norm) {
   if (!w) return GBA_E_ARG;
-  const char* bad = bad_parts(parts, n_parts, false);
+  const char* bad = bad_parts(parts, n_parts, false, nullptr);
   if (!bad && !norm) bad = "norm is NULL";
   if (!bad) bad = bad_floats(norm);
   if (bad) return fail(w, GBA_E_ARG, bad);
@@ -396,7 +408,7 @@ gba_status gba_grad_norm(gba_worker* w, const gba_grad_part* parts, int32_t n_pa
 gba_status gba_clip_grads(gba_worker* w, const gba_grad_part* parts, int32_t n_parts, float max_norm,
                           float* norm) {
   if (!w) return GBA_E_ARG;
-  const char* bad = bad_parts(parts, n_parts, true);
+  const char* bad = bad_parts(parts, n_parts, true, norm);
   if (!bad && !(max_norm >= 0.f)) bad = "max_norm is negative or NaN";
   if (!bad) bad = bad_floats(norm);
   if (bad) return fail(w, GBA_E_ARG, bad);
