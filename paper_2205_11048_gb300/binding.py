@@ -540,8 +540,27 @@ def _matrix(t):
     if len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
         _refuse("a matrix has two dimensions, and rows of consecutive elements")
     rows, cols = shape
+    if cols > INT32_MAX:
+        _refuse("a matrix has too many columns")
     return gba_matrix(t.data_ptr() if rows else None, rows, strides[0] if rows > 1 else max(cols, 1), cols,
                       _type_of(t))
+
+
+# ctypes keeps an integer's low bits, so what does not fit is refused before it.
+def _int64(x):
+    if not -2**63 <= x < 2**63:
+        _refuse(f"{x} is no 64-bit integer")
+    return x
+
+
+def _pad(pad_id):
+    return NO_PAD if pad_id is None else _int64(pad_id)
+
+
+def _mode(id_mode):
+    if id_mode != DIRECT and id_mode != MODULO:
+        _refuse("id_mode is neither DIRECT nor MODULO")
+    return id_mode
 
 
 def _rows_of(t):
@@ -671,8 +690,8 @@ class Worker:
         ids = self._ids(ids)
         self._mine(weights)
         out, om = self._embed_out(ids, weights.shape[-1], dtype or weights.dtype, out)
-        self._call("gba_embed", _matrix(weights), id_mode, ids.data_ptr(), ids.numel(), scale,
-                   NO_PAD if pad_id is None else pad_id, om)
+        self._call("gba_embed", _matrix(weights), _mode(id_mode), ids.data_ptr(), ids.numel(), scale,
+                   _pad(pad_id), om)
         return out
 
     def embed_table(self, server, t, ids, scale=1.0, pad_id=None, dtype=None, out=None):
@@ -682,7 +701,7 @@ class Worker:
         ids = self._ids(ids)
         out, om = self._embed_out(ids, server.dims[t], dtype or self.torch.float32, out)
         self._call("gba_embed_table", server.h, t, ids.data_ptr(), ids.numel(), scale,
-                   NO_PAD if pad_id is None else pad_id, om)
+                   _pad(pad_id), om)
         return out
 
     def embed_grad(self, ids, grad, rows, scale=1.0, pad_id=None, id_mode=DIRECT):
@@ -696,8 +715,8 @@ class Worker:
         ids_out = self._new(n, dtype=torch.int64)
         rows_out = self._new(n, d)
         count = self._new(dtype=torch.int64)
-        self._call("gba_embed_grad", ids.data_ptr(), n, _matrix(grad), rows, id_mode, scale,
-                   NO_PAD if pad_id is None else pad_id, ids_out.data_ptr(), rows_out.data_ptr(),
+        self._call("gba_embed_grad", ids.data_ptr(), n, _matrix(grad), _int64(rows), _mode(id_mode), scale,
+                   _pad(pad_id), ids_out.data_ptr(), rows_out.data_ptr(),
                    count.data_ptr())
         return ids_out, rows_out, count
 
@@ -705,8 +724,8 @@ class Worker:
         """The lookup's gradient over all rows of the table, into (or added to) out."""
         ids, grad = self._ids(ids), _rows_of(grad)
         self._mine(grad, out)
-        self._call("gba_embed_grad_dense", ids.data_ptr(), ids.numel(), _matrix(grad), id_mode, scale,
-                   NO_PAD if pad_id is None else pad_id, _matrix(out), int(accumulate))
+        self._call("gba_embed_grad_dense", ids.data_ptr(), ids.numel(), _matrix(grad), _mode(id_mode), scale,
+                   _pad(pad_id), _matrix(out), int(accumulate))
         return out
 
     def grad_norm(self, grads):
