@@ -14,7 +14,8 @@
 // worst: by aligned words and a shift, as the lookup reads them, f16 35,710 x 1,161 took 83 us
 // against 49.  Backward, a block keeps its threads' shares of dgamma and dbeta in registers over
 // all the rows it takes and leaves one partial row; a second kernel adds the partial rows in
-// order.  Rows too wide for a block's registers are read again from L2 instead.
+// order; calls of very many rows are several such launches.  Rows too wide for a block's registers
+// are read again from L2 instead.
 //
 // Measured, of the copy bandwidth of 6.7 TB/s: forward bf16 32,768 x 4,096 94 us (86%),
 // 65,536 x 1,024 46.5 (86%), float32 16,384 x 4,096 88 (91%), f16 35,710 x 1,161 49 (50%, single
@@ -818,9 +819,11 @@ __global__ void __launch_bounds__(THREADS) k_layer_norm_columns(LayerNormArgs a)
   }
 }
 
-// The partial rows, added in order: a block takes 32 columns, each of its warps a share of
-// the rows.  blockIdx.y: dgamma or dbeta.
-__global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int parts) {
+// The partial rows of a launch of `parts` blocks, [2][parts][d], or of `chunks` such launches (MANY),
+// added in order: a block takes 32 columns, each of its warps a share of every launch's rows.
+// blockIdx.y: dgamma or dbeta.
+template <bool MANY>
+__global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int parts, int chunks) {
   constexpr int WARPS = 32;
   __shared__ float s[WARPS][33];
   follow();
@@ -835,6 +838,15 @@ __global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int
   if (c < a.d)
 #pragma unroll 8
     for (int i = lo; i < hi; ++i) x += p[(int64_t)i * a.d + c];
+  if (MANY)
+    for (int k = 1; k < chunks; ++k) {
+      p += (int64_t)2 * parts * a.d;
+      float y = 0.f;
+      if (c < a.d)
+#pragma unroll 8
+        for (int i = lo; i < hi; ++i) y += p[(int64_t)i * a.d + c];
+      x += y;
+    }
   s[warp][lane] = x;
   __syncthreads();
   if (warp == 0 && c < a.d) {
@@ -846,7 +858,12 @@ __global__ void __launch_bounds__(1024) k_layer_norm_params(LayerNormArgs a, int
 
 // ---- launches ------------------------------------------------------------------------
 
-constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns
+constexpr int64_t WIDE_SPLIT = 64;  // rows of blocks of k_layer_norm_columns, at least
+// The most rows that a thread adds to its share of dgamma and dbeta, one after the other in float32.
+// Calls of more rows are several launches, whose partial rows are added in the end, so that what
+// the sums lose does not grow with the rows (dbeta of 5 10^6 x 1,003 equal float32: off by 2.2e-6 of
+// itself, and by 4.6e-5 in one launch; 10^6 x 1,040 float32 2.06 ms, and 2.00 in one).
+constexpr int64_t CHAIN = 512;
 
 // The lanes of a narrow row of d columns, E to a lane.
 Split lanes_of(int32_t d, int E) {
@@ -995,7 +1012,15 @@ struct GradShape {
   RingShape ring;
   Split split;
   int threads;
-  int parts;  // blocks, and partial rows
+  int parts;  // blocks of a launch, and its partial rows
+  int chunks;    // launches
+  int64_t rows;  // of each
+  // A block holds `groups` rows at a time.
+  void split_rows(int64_t n, int groups) {
+    const int64_t per_pass = (int64_t)parts * groups, passes = (n + per_pass - 1) / per_pass;
+    chunks = (int)((passes + CHAIN - 1) / CHAIN);
+    rows = (passes + chunks - 1) / chunks * per_pass;
+  }
 };
 
 // float32 rows come through the ring (4,096 x 8,192: 82 us from registers, 69 this way).  16-bit ones
@@ -1015,6 +1040,7 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
     g.split = lanes_of(a.d, EL);
     g.threads = THREADS;
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held);
+    g.split_rows(a.n, g.threads / g.split.L);
     return g;
   }
   if constexpr (GRAD_RING<T, V>)
@@ -1024,6 +1050,7 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
       if (ring_serves(g.ring, a.n, num_sms)) {
         g.way = Way::RING;
         g.parts = (int)std::min<int64_t>(num_sms, (a.n + g.ring.groups - 1) / g.ring.groups);
+        g.split_rows(a.n, g.ring.groups);
         return g;
       }
     }
@@ -1032,13 +1059,17 @@ GradShape grad_shape(const LayerNormArgs& a, int num_sms) {
     g.way = Way::FETCH;
     g.split = warps_of(a.d, E, &g.threads);
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, held.blocks[g.split.W]);
+    g.split_rows(a.n, g.threads / (32 * g.split.W));
   } else if (E < 16 && a.d <= MOST_WARPS * 32 * 16) {
     g.way = Way::PLAIN;
     g.split = warps_of(a.d, 16, &g.threads);
     g.parts = (int)grid_of(a.n, g.split, g.threads, num_sms, 1);
+    g.split_rows(a.n, g.threads / (32 * g.split.W));
   } else {
     g.way = Way::WIDE;
-    g.parts = (int)std::min(a.n, WIDE_SPLIT);
+    g.parts = (int)std::min(a.n, std::min<int64_t>(65535, std::max(WIDE_SPLIT, (a.n + CHAIN - 1) / CHAIN)));
+    g.chunks = 1;
+    g.rows = a.n;
   }
   return g;
 }
@@ -1047,7 +1078,7 @@ template <typename T, int V>
 cudaError_t grad_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cudaStream_t s) {
   constexpr int EL = E_LANES<V>, E = E_GRAD<T, V>;
   const GradShape g = grad_shape<T, V>(a, num_sms);
-  cudaError_t e;
+  cudaError_t e = cudaSuccess;
   if (g.way == Way::WIDE) {
     const int64_t per = (int64_t)THREADS * V;
     e = launch_following(k_layer_norm_columns<T, V>, dim3((unsigned)((a.d + per - 1) / per), (unsigned)g.parts),
@@ -1055,18 +1086,30 @@ cudaError_t grad_as(const LayerNormArgs& a, const RingWait& w, int num_sms, cuda
     if (e == cudaSuccess)
       e = launch_following(k_layer_norm_grad_wide<T, V>, dim3((unsigned)std::min<int64_t>(a.n, num_sms * 4)),
                            WIDE_GRAD_THREADS, 0, s, a);
-  } else if (g.way == Way::RING) {
-    e = cudaErrorInvalidValue;
-    if constexpr (GRAD_RING<T, V>)
-      e = launch_ring(k_layer_norm_grad_ring<T, V, E_GRAD_RING>, g.ring, a, w, (unsigned)g.parts, s);
   } else {
     auto kernel = g.way == Way::LANES ? k_layer_norm_grad<T, V, EL, true, true> : k_layer_norm_grad<T, V, E, false, true>;
     if constexpr (E < 16)
       if (g.way == Way::PLAIN) kernel = k_layer_norm_grad<T, V, 16, false, false>;
-    e = launch_following(kernel, dim3(g.parts), g.threads, 0, s, a, g.split);
+    LayerNormArgs c = a;
+    for (int k = 0; k < g.chunks; ++k) {
+      const int64_t first = k * g.rows;
+      c.x = static_cast<const T*>(a.x) + first * a.x_stride;
+      c.dy = static_cast<const T*>(a.dy) + first * a.dy_stride;
+      c.y = static_cast<T*>(a.y) + first * a.y_stride;
+      c.mean = a.mean + first;
+      c.rstd = a.rstd + first;
+      c.n = std::min(g.rows, a.n - first);
+      c.parts = a.parts + (size_t)k * 2 * g.parts * a.d;
+      e = cudaErrorInvalidValue;
+      if (g.way != Way::RING)
+        e = launch_following(kernel, dim3(g.parts), g.threads, 0, s, c, g.split);
+      else if constexpr (GRAD_RING<T, V>)
+        e = launch_ring(k_layer_norm_grad_ring<T, V, E_GRAD_RING>, g.ring, c, w, (unsigned)g.parts, s);
+      if (e != cudaSuccess) return e;
+    }
   }
   if (e != cudaSuccess || (!a.dgamma && !a.dbeta)) return e;
-  return launch_following(k_layer_norm_params, dim3((unsigned)((a.d + 31) / 32), 2), 1024, 0, s, a, g.parts);
+  return launch_following(g.chunks > 1 ? k_layer_norm_params<true> : k_layer_norm_params<false>, dim3((unsigned)((a.d + 31) / 32), 2), 1024, 0, s, a, g.parts, g.chunks);
 }
 
 // Calls f with the vector width of a's matrices.
@@ -1098,8 +1141,11 @@ cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, const RingWa
 }
 
 size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms) {
-  const int parts = with_type(type, a, [&](auto x, auto v) { return grad_shape<decltype(x), v()>(a, num_sms).parts; });
-  return (size_t)parts * 2 * (size_t)a.d * sizeof(float);
+  const size_t parts = with_type(type, a, [&](auto x, auto v) {
+    const GradShape g = grad_shape<decltype(x), v()>(a, num_sms);
+    return (size_t)g.parts * g.chunks;
+  });
+  return parts * 2 * (size_t)a.d * sizeof(float);
 }
 
 cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
