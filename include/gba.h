@@ -455,9 +455,10 @@ typedef struct {
  * as one device float32, written when all have been read (out is not looked at).  Squares
  * neither overflow nor vanish: the norm is right wherever it is a float32.
  * gba_clip_grads - the norm N, and out = c * grad with c = min(1, max_norm / (N + 1e-6))
- * for every part (norm may be NULL).  With a norm that is infinite c is 0, with a NaN it
- * is NaN: the gradients of such a message are lost, and *norm says so.  max_norm >= 0.
- * The description may be reused or freed when the call returns.  No part may overlap
+ * for every part (norm may be NULL).  With a norm that is infinite c is 0 (NaN if max_norm
+ * is infinite too), with a NaN it is NaN: the gradients of such a message are lost, and
+ * *norm says so.  max_norm >= 0.  The description may be reused or freed when the call
+ * returns (a captured call keeps the addresses in it).  No part may overlap
  * another part's out.
  */
 gba_status gba_grad_norm(gba_worker* w, const gba_grad_part* parts, int32_t n_parts, float* norm);

@@ -576,7 +576,9 @@ def _rows_of(t):
 
 class GradParts:
     """A list of gradient tensors (and of what receives them clipped), as the library takes
-    it.  It refers to the tensors' memory and keeps them alive."""
+    it.  It holds the tensors and the addresses that they had when it was made: gradients that
+    are made anew (set to None between steps) or given other storage need a new list.  Making one
+    costs about 1.2 us a tensor of Python, so it pays to keep it for gradients that stay."""
 
     def __init__(self, grads, out=None):
         grads = list(grads)
@@ -611,7 +613,11 @@ class Worker:
 
     Work is issued on `stream` (default: the current one), on the stream's device.  A call made while another stream
     is current orders the two both ways, so tensors of the current stream can be passed and
-    results used there."""
+    results used there.
+
+    The operators work on the tensors' data: nothing is recorded for autograd, results never
+    require gradients, and what is written in place (out, clipped gradients) does not count as a
+    change of the tensor there.  Tensors are on the worker's device."""
 
     def __init__(self, stream=None):
         import torch
@@ -686,7 +692,8 @@ class Worker:
         return out, _matrix(flat)
 
     def embed(self, weights, ids, scale=1.0, pad_id=None, dtype=None, id_mode=DIRECT, out=None):
-        """scale * weights[ids] in dtype (default: the weights'); padding gives zeros."""
+        """scale * weights[ids] in dtype (default: the weights'), or into out, in out's type; padding
+        gives zeros."""
         ids = self._ids(ids)
         self._mine(weights)
         out, om = self._embed_out(ids, weights.shape[-1], dtype or weights.dtype, out)

@@ -532,9 +532,9 @@ __global__ void __launch_bounds__(THREADS) k_token_items(ItemArgs a, ErrSink err
 // The same passes over digits as the larger sort, with the keys in the shared memory of
 // eight blocks: a warp ranks its keys among equal digits, the blocks tell each other their
 // counts and send the keys to their places.  One launch instead of five or six whose work is a
-// few microseconds: whole calls of 1,000, 4,000, 8,000 and 16,000 tokens x 64 floats take 14.5,
-// 17.2, 22.0 and 29.9 us this way and 20.5, 25.9, 27.4 and 29.5 the other, so it is for up to
-// 8,192.  Up to 1,024 tokens one block does it without the cluster's barriers (30, 500 and 1,000
+// few microseconds: whole calls of 1,000, 4,000 and 8,000 tokens x 64 floats take 14.5, 17.2 and
+// 22.0 us by a cluster and 20.5, 25.9 and 27.4 the other way; with four keys a thread, which are
+// not built, 16,000 took 29.9 against 29.5.  So it is for up to 8,192.  Up to 1,024 tokens one block does it without the cluster's barriers (30, 500 and 1,000
 // tokens 7.0, 10.7 and 12.4 us, by a cluster 11.1, 14.6 and 15.5; 6,656 keys would take it 30 us:
 // match.any gives an SM about one key every two cycles).
 constexpr int CL_BLOCKS = 8, CL_THREADS = 512, CL_WARPS = CL_THREADS / 32;

@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
 template <typename T, int V>
 __global__ void __launch_bounds__(WIDE_THREADS) k_layer_norm_wide(LayerNormArgs a) {
   __shared__ float s_sum[2][32][1];
-    follow();
+  follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
@@ -744,7 +744,7 @@ __global__ void __launch_bounds__(RING_WARPS_GRAD * 32, 1)
 template <typename T, int V>
 __global__ void __launch_bounds__(WIDE_GRAD_THREADS) k_layer_norm_grad_wide(LayerNormArgs a) {
   __shared__ float s_sum[2][WIDE_GRAD_THREADS / 32][2];
-    follow();
+  follow();
   const float inv_d = 1.f / (float)a.d;
   const int64_t step = (int64_t)blockDim.x * V;
   int flip = 0;

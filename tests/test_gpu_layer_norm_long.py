@@ -21,6 +21,8 @@ def _built():
     import __graft_entry__
     __graft_entry__.build()
     torch.cuda.set_device(0)
+    yield
+    torch.cuda.empty_cache()  # tens of GB
 
 
 @pytest.mark.parametrize("n,d", [(5_000_000, 1003), (4_000_000, 1040)])
