@@ -25,6 +25,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int NORM_BLOCKS = 5, CLIP_BLOCKS = 4;  // that an SM holds
+constexpr int MOST_V = 8;  // elements of a vector of 16 bytes, at most
 
 struct Part {
   const void* grad;
@@ -206,7 +207,8 @@ __device__ __forceinline__ void clip_piece(const Part& p, uint32_t k, int unit, 
   const int64_t per = unit / V, lo = (int64_t)k * per;
   const int64_t hi = lo + per < lay.vecs ? lo + per : lay.vecs;
   const int lane = threadIdx.x & 31;
-  float* mine = swap + (threadIdx.x >> 5) * (32 * V);  // the warp's
+  // the warp's, the same for every type: another warp may be at a piece of another type
+  float* mine = swap + (threadIdx.x >> 5) * (32 * MOST_V);
   // first: the warp's first vector, of which `count` are left
   auto scaled = [&](const Pack<T, V>& w, int64_t first, int count) {
     float x[V];
@@ -263,7 +265,7 @@ __device__ __forceinline__ void clip_out(const Part& p, uint32_t k, int unit, fl
 template <int CAP>
 __global__ void __launch_bounds__(THREADS, CLIP_BLOCKS)
     k_grad_clip(const __grid_constant__ PartList<CAP> l, const float* coef) {
-  __shared__ __align__(16) float swap[THREADS * 8];
+  __shared__ __align__(16) float swap[THREADS * MOST_V];
   follow();
   const float c = *(const volatile float*)coef;
   for (uint32_t b = blockIdx.x; b < l.pieces; b += gridDim.x) {
