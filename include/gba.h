@@ -486,6 +486,186 @@ gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_ma
                                const float* rstd, const gba_matrix* dx, float* dgamma,
                                float* dbeta);
 
+/* ---- a block of a model over tokens --------------------------------------
+ *
+ * What stands between a lookup and a message in such a model: gba_gated_scan moves
+ * information along the sequences, gba_residual_norm joins a block's output into the
+ * residual stream and takes the norm for the next block, and gba_adamw updates the
+ * weights that a worker keeps itself.  The conventions are those of the operators
+ * above.
+ */
+
+/* The norm of a row: NONE; RMS, x / sqrt(mean(x^2) + eps); LAYER, the same of x minus
+ * its mean. */
+typedef enum { GBA_NORM_NONE = 0, GBA_NORM_RMS = 1, GBA_NORM_LAYER = 2 } gba_norm_kind;
+
+/* What a gate multiplies by: 1, the gate, sigmoid(gate), gate * sigmoid(gate). */
+typedef enum { GBA_GATE_NONE = 0, GBA_GATE_MUL = 1, GBA_GATE_SIGMOID = 2, GBA_GATE_SILU = 3 } gba_gate_kind;
+
+/* The parameters of gba_residual_norm.  Each weight and bias has cols values of
+ * param_type, or is NULL (1 and 0). */
+typedef struct {
+  int32_t post_norm;  /* gba_norm_kind of the block's output */
+  int32_t pre_norm;   /* gba_norm_kind of the sum, for the next block */
+  int32_t gate;       /* gba_gate_kind */
+  int32_t param_type; /* gba_dtype */
+  const void* post_weight;
+  const void* post_bias;
+  const void* pre_weight; /* NULL with pre_norm NONE, and so is pre_bias */
+  const void* pre_bias;
+  float eps;            /* >= 0 */
+  float residual_scale; /* finite, as is block_scale */
+  float block_scale;
+} gba_block;
+
+/*
+ * gba_residual_norm - the end of a block and the norm before the next, for every row:
+ *   u = post_norm(x) * post_weight + post_bias       (a scale per channel with NONE)
+ *   z = residual_scale * residual + block_scale * act(gate) * u
+ *   y = pre_norm(z) * pre_weight + pre_bias
+ * y is formed from z before its rounding.
+ * x          the block's output.
+ * residual   of x's shape, of x's type or float32 (NULL: no such term; then
+ *            residual_scale is not used).
+ * gate       of x's shape and type (NULL with GBA_GATE_NONE).
+ * z          of the residual's type, or without one of x's or float32; NULL: not kept.
+ *            May be the residual itself.
+ * y          of x's shape and type; NULL with pre_norm NONE.
+ * stats      rows x 4 device float32, 16-byte aligned, for the gradient: the mean and
+ *            the reciprocal deviation of x, and of z (0 and 1 for NONE, mean 0 for
+ *            RMS).  NULL: not kept.
+ */
+gba_status gba_residual_norm(gba_worker* w, const gba_block* b, const gba_matrix* x,
+                             const gba_matrix* residual, const gba_matrix* gate,
+                             const gba_matrix* z, const gba_matrix* y, float* stats);
+
+/* Device float32 arrays of cols values that receive the gradients of a gba_block's
+ * parameters, summed over all rows (overwritten; any may be NULL). */
+typedef struct {
+  float* post_weight;
+  float* post_bias;
+  float* pre_weight;
+  float* pre_bias;
+} gba_block_grads;
+
+/*
+ * gba_residual_norm_grad - from the gradients dy of y (NULL with pre_norm NONE) and dz of
+ * z (of z's type; NULL: none), with x, the gate, z as it was kept and the stats of the
+ * forward pass:
+ * dx         of x's shape and type.
+ * dresidual  of the residual's type (z's); NULL: not formed.  May be dz itself.
+ * dgate      of x's type; NULL only with GBA_GATE_NONE.
+ * z          NULL with pre_norm NONE.
+ */
+gba_status gba_residual_norm_grad(gba_worker* w, const gba_block* b, const gba_matrix* dy,
+                                  const gba_matrix* dz, const gba_matrix* x, const gba_matrix* z,
+                                  const gba_matrix* gate, const float* stats,
+                                  const gba_matrix* dx, const gba_matrix* dresidual,
+                                  const gba_matrix* dgate, const gba_block_grads* grads);
+
+/* How a forget gate f is given: SIGMOID, the decay is a = 1 / (1 + exp(-f)); LOG, it is
+ * a = exp(min(f, 0)). */
+typedef enum { GBA_DECAY_SIGMOID = 0, GBA_DECAY_LOG = 1 } gba_decay;
+
+/* The gates of a gba_gated_scan and its sequences.  Without arrays every sequence has
+ * rows / n_seq rows, one after another.  lengths: of those rows the first lengths[i]
+ * belong to sequence i (a padded batch).  offsets: sequence i has the rows offsets[i] up
+ * to offsets[i + 1] (a packed batch).  Either is a device int64 array, 8-byte aligned,
+ * NULL if not used. */
+typedef struct {
+  int32_t decay;          /* gba_decay */
+  int32_t tied;           /* 1: the input is weighted by 1 - a; 0: by 1 */
+  int64_t n_seq;          /* 0 only with 0 rows, < 2^29 */
+  const int64_t* lengths; /* n_seq values within 0 .. rows / n_seq */
+  const int64_t* offsets; /* n_seq + 1 values within 0 .. rows, ascending */
+} gba_scan;
+
+/*
+ * gba_gated_scan - for every channel of every sequence, from its first row on:
+ *   h = a * h + (1 - a) * x   or   h = a * h + x,   y = h
+ * h before the first row is the sequence's row of state, or 0.
+ * x, f       of one shape and type.  Up to 2^30 - 1 rows.
+ * state      n_seq x cols, float32 (NULL: zeros).
+ * y          of x's shape, of x's type or float32.  Rows that belong to no sequence
+ *            become zeros, whatever x and f hold there.
+ * state_out  n_seq x cols, float32: h after the last row (state's row of an empty
+ *            sequence).  NULL: not kept.  May be state itself.
+ * One row a sequence is a step of generation.  An infinity or a NaN makes what follows it in
+ * its channel of its sequence infinite or NaN, and nothing else.  Offsets or lengths
+ * that are not as described are latched (gba_worker_sync returns GBA_E_ARG) and the
+ * call's results are undefined.
+ */
+gba_status gba_gated_scan(gba_worker* w, const gba_scan* s, const gba_matrix* x,
+                          const gba_matrix* f, const gba_matrix* state, const gba_matrix* y,
+                          const gba_matrix* state_out);
+
+/*
+ * gba_gated_scan_grad - from the gradients dy of y and dstate_out of the last states
+ * (NULL: none), with x, f, state and y as the forward pass had and gave them:
+ * dx, df     of x's shape and type; rows that belong to no sequence become zeros.
+ * dstate     n_seq x cols, float32, of the first states; NULL: not formed.  May be
+ *            dstate_out itself.
+ * y and dy are of one type (x's or float32).  What is rounded in y is rounded in df's h.
+ * With LOG, df is 0 where f > 0.
+ */
+gba_status gba_gated_scan_grad(gba_worker* w, const gba_scan* s, const gba_matrix* dy,
+                               const gba_matrix* dstate_out, const gba_matrix* x,
+                               const gba_matrix* f, const gba_matrix* state, const gba_matrix* y,
+                               const gba_matrix* dx, const gba_matrix* df,
+                               const gba_matrix* dstate);
+
+/* One tensor of gba_adamw: n consecutive parameters with their gradient and states.
+ * States in 32 bits: m and v are n float32, the scales NULL.  In 8 bits: m and v are n
+ * bytes, and every 256 elements from the first on share a float32 of m_scale and one of
+ * v_scale ((n + 255) / 256 each).  A byte of m is an 8-bit float with 4 exponent and 3
+ * mantissa bits (e4m3), a byte c of v stands for 0 if c is 0 and else for
+ * (1 + c % 8 / 8) * 2^(c / 8 - 31); the value is that times the scale.  All bytes and
+ * scales zero are states of zeros. */
+typedef struct {
+  void* weight;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;         /* receives the new weights too, in copy_type; NULL: no copy */
+  int64_t n;          /* 0 .. 2^40 */
+  int32_t type;       /* gba_dtype of the weights */
+  int32_t grad_type;
+  int32_t copy_type;
+  int32_t bits;       /* 32 or 8 */
+  float weight_decay; /* >= 0 */
+} gba_adamw_part;
+
+typedef struct {
+  double lr; /* >= 0 */
+  double beta1, beta2; /* within [0, 1) */
+  double eps;          /* > 0 */
+  const float* lr_now; /* device float32 that takes lr's place (NULL: lr), for captured calls */
+  const float* norm;   /* device float32, the norm of all gradients (NULL: no clipping) */
+  float max_norm;      /* >= 0; with norm */
+} gba_adamw_desc;
+
+/*
+ * gba_adamw - one step of AdamW over n_parts (up to 2^20) tensors:
+ *   g = min(1, max_norm / (norm + 1e-6)) * grad,   t = *step + 1
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   weight = (1 - lr weight_decay) weight - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * step       device int64, the steps taken so far; the call adds 1.
+ * With a norm that is infinite or NaN the call changes nothing, *step neither (copies are
+ * not written).  Without norm a gradient that is infinite or NaN spoils its element, in 8
+ * bits up to the 256 elements that share its scales.  *step >= 0.  8-bit states are rounded to the nearest code; the weights move by m and v
+ * from before that rounding, and a v above 0 does not become 0.  The description may be
+ * reused or freed when the call returns (a captured call keeps the addresses in it).  No
+ * array may overlap another.
+ * gba_adamw_values - the states of the parts as float32: m_out[i] and v_out[i] receive
+ * part i's n values each.
+ */
+gba_status gba_adamw(gba_worker* w, const gba_adamw_part* parts, int32_t n_parts,
+                     const gba_adamw_desc* d, int64_t* step);
+gba_status gba_adamw_values(gba_worker* w, const gba_adamw_part* parts, int32_t n_parts,
+                            float* const* m_out, float* const* v_out);
+
 /* ---- instrumentation and test entry points ----------------------------- */
 
 /* gba_set_timing - when on, every kernel launch is bracketed by CUDA events on

@@ -30,6 +30,9 @@ STATUS_NAMES = {0: "GBA_OK", -1: "GBA_E_ARG", -2: "GBA_E_ID_RANGE", -3: "GBA_E_O
 ADAGRAD, ADAM = 0, 1
 DIRECT, MODULO, HASH = 0, 1, 2
 F32, BF16, F16 = 0, 1, 2
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+GATES = {"none": 0, "mul": 1, "sigmoid": 2, "silu": 3}
+DECAYS = {"sigmoid": 0, "log": 1}
 NO_PAD = -2**63
 INT32_MAX = 2**31 - 1
 KERNEL_NAMES = ["weights", "sort_hist", "sort_pass", "seg_scan", "row_long", "row_apply",
@@ -86,6 +89,34 @@ class gba_matrix(ctypes.Structure):
 class gba_grad_part(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
                 ("type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+class gba_block(ctypes.Structure):
+    _fields_ = [("post_norm", ctypes.c_int32), ("pre_norm", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("param_type", ctypes.c_int32), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("block_scale", ctypes.c_float)]
+
+
+class gba_block_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("post_weight", "post_bias", "pre_weight", "pre_bias")]
+
+
+class gba_scan(ctypes.Structure):
+    _fields_ = [("decay", ctypes.c_int32), ("tied", ctypes.c_int32), ("n_seq", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("offsets", ctypes.c_void_p)]
+
+
+class gba_adamw_part(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("weight", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+        ("copy_type", ctypes.c_int32), ("bits", ctypes.c_int32), ("weight_decay", ctypes.c_float)]
+
+
+class gba_adamw_desc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("lr_now", ctypes.c_void_p), ("norm", ctypes.c_void_p),
+                ("max_norm", ctypes.c_float)]
 
 
 _P = ctypes.c_void_p
@@ -152,6 +183,15 @@ _SIGNATURES = {
                                       ctypes.c_float, _P]),
     "gba_layer_norm": (ctypes.c_int, [_P, _M, _P, _P, ctypes.c_int32, ctypes.c_float, _M, _P, _P]),
     "gba_layer_norm_grad": (ctypes.c_int, [_P, _M, _M, _P, ctypes.c_int32, _P, _P, _M, _P, _P]),
+    "gba_residual_norm": (ctypes.c_int, [_P, ctypes.POINTER(gba_block), _M, _M, _M, _M, _M, _P]),
+    "gba_residual_norm_grad": (ctypes.c_int, [_P, ctypes.POINTER(gba_block), _M, _M, _M, _M, _M, _P, _M, _M, _M,
+                                              ctypes.POINTER(gba_block_grads)]),
+    "gba_gated_scan": (ctypes.c_int, [_P, ctypes.POINTER(gba_scan), _M, _M, _M, _M, _M]),
+    "gba_gated_scan_grad": (ctypes.c_int, [_P, ctypes.POINTER(gba_scan)] + [_M] * 9),
+    "gba_adamw": (ctypes.c_int, [_P, ctypes.POINTER(gba_adamw_part), ctypes.c_int32,
+                                 ctypes.POINTER(gba_adamw_desc), _P]),
+    "gba_adamw_values": (ctypes.c_int, [_P, ctypes.POINTER(gba_adamw_part), ctypes.c_int32, ctypes.POINTER(_P),
+                                        ctypes.POINTER(_P)]),
 }
 
 _lib = None
@@ -574,6 +614,18 @@ def _rows_of(t):
     return t
 
 
+def _opt(t):
+    return None if t is None else _matrix(t)
+
+
+def _shaped(t, like):
+    return t if t is None or t.shape == like.shape else t.view(like.shape)
+
+
+def _addresses(tensors):
+    return (ctypes.c_void_p * max(1, len(tensors)))(*[t.data_ptr() for t in tensors])
+
+
 class GradParts:
     """A list of gradient tensors (and of what receives them clipped), as the library takes
     it.  It holds the tensors and the addresses that they had when it was made: gradients that
@@ -607,9 +659,152 @@ def grad_parts(grads, out=None):
     return GradParts(grads, out)
 
 
+class ResidualNorm:
+    """The parameters of Worker.residual_norm: what it normalises and how, and the tensors of its
+    weights and biases (of one type; held, and read where they are when a call runs)."""
+
+    def __init__(self, post_norm="none", pre_norm="none", gate="none", post_weight=None, post_bias=None,
+                 pre_weight=None, pre_bias=None, eps=1e-6, residual_scale=1.0, block_scale=1.0):
+        try:
+            kinds = NORMS[post_norm], NORMS[pre_norm], GATES[gate]
+        except (KeyError, TypeError):
+            _refuse(f"norms are one of {list(NORMS)}, gates one of {list(GATES)}")
+        self.tensors = (post_weight, post_bias, pre_weight, pre_bias)
+        there = [p for p in self.tensors if p is not None]
+        if pre_norm == "none" and (pre_weight is not None or pre_bias is not None):
+            _refuse("parameters of a norm that is not taken")
+        for p in there:
+            if not p.is_contiguous() or p.numel() != there[0].numel() or _type_of(p) != _type_of(there[0]):
+                _refuse("the parameters of a block have a value per column and one type")
+            if p.get_device() != there[0].get_device():
+                _refuse("the parameters of a block are on one GPU")
+        self.pre, self.gate = pre_norm != "none", gate != "none"
+        self.cols = there[0].numel() if there else None
+        self.device = there[0].get_device() if there else None
+        self.block = gba_block(*kinds, _type_of(there[0]) if there else F32,
+                               *[None if p is None else p.data_ptr() for p in self.tensors], eps, residual_scale,
+                               block_scale)
+
+
+def residual_norm(**how):
+    """A block's norms, gate and residual, made once (see ResidualNorm)."""
+    return ResidualNorm(**how)
+
+
+class Sequences:
+    """Where n sequences lie among the rows of a scan: of equal length, one after another; with
+    lengths (an int64 tensor of n), the first lengths[i] rows of each of those; with offsets (of
+    n + 1), sequence i has the rows offsets[i] up to offsets[i + 1]."""
+
+    def __init__(self, n, lengths=None, offsets=None):
+        if not 0 <= n < 2**29:
+            _refuse("from 0 to 2^29 - 1 sequences")
+        if lengths is not None and offsets is not None:
+            _refuse("lengths and offsets")
+        for t, many in ((lengths, n), (offsets, n + 1)):
+            if t is not None and (str(t.dtype) != "torch.int64" or t.numel() != many or not t.is_contiguous()):
+                _refuse("lengths are n and offsets n + 1 int64")
+        self.n, self.lengths, self.offsets = n, lengths, offsets
+
+
+def sequences(n, lengths=None, offsets=None):
+    """The sequences of a scan, made once (see Sequences)."""
+    return Sequences(n, lengths, offsets)
+
+
+class AdamWStates:
+    """AdamW's states of a list of weights, which it holds: m and v (lists of float32 tensors, or
+    of uint8 with 8 bits and their m_scale and v_scale), step (a device int64) and, if given,
+    copies of the weights that follow them.  States that are not given start as zeros."""
+
+    def __init__(self, weights, bits=32, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, copies=None, m=None, v=None,
+                 m_scale=None, v_scale=None, step=None):
+        import torch
+        self.weights = list(weights)
+        if bits not in (32, 8):
+            _refuse("states have 32 or 8 bits")
+        self.bits, self.betas, self.eps = bits, (float(betas[0]), float(betas[1])), float(eps)
+        n = len(self.weights)
+        self.device = self.weights[0].get_device() if n else None
+        self.decays = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        where = self.weights[0].device if n else "cuda"
+
+        def states(given, kind, size):
+            if given is None:
+                return [torch.zeros(size(w.numel()), dtype=kind, device=where) for w in self.weights]
+            given = list(given)
+            if len(given) != n or any(t.dtype != kind or t.numel() != size(w.numel())
+                                      for t, w in zip(given, self.weights)):
+                _refuse("a state has its weight's size, and its own type")
+            return given
+
+        def scales(k):
+            return (k + 255) // 256
+
+        def same(k):
+            return k
+
+        kind = torch.float32 if bits == 32 else torch.uint8
+        if bits == 8 and ((m is None) != (m_scale is None) or (v is None) != (v_scale is None)):
+            _refuse("8-bit states come with their scales")
+        if bits == 32 and (m_scale is not None or v_scale is not None):
+            _refuse("scales of states in 32 bits")
+        self.m, self.v = states(m, kind, same), states(v, kind, same)
+        self.m_scale = states(m_scale, torch.float32, scales) if bits == 8 else None
+        self.v_scale = states(v_scale, torch.float32, scales) if bits == 8 else None
+        self.copies = None if copies is None else list(copies)
+        if len(self.decays) != n or (self.copies is not None and len(self.copies) != n):
+            _refuse("a weight decay and a copy for each weight")
+        if self.copies is not None and any(c.numel() != w.numel() for c, w in zip(self.copies, self.weights)):
+            _refuse("a copy has its weight's size")
+        self.step = torch.zeros((), dtype=torch.int64, device=where) if step is None else step
+        if self.step.dtype != torch.int64 or self.step.numel() != 1:
+            _refuse("step is one int64")
+        for t in (*self.weights, *self.m, *self.v, *(self.m_scale or ()), *(self.v_scale or ()), *(self.copies or ()),
+                  self.step):
+            if t.get_device() < 0 or (n and t.get_device() != self.device):
+                _refuse("weights, states and step are on one GPU")
+            if not t.is_contiguous():
+                _refuse("weights and states are contiguous")
+
+    def parts(self, grads):
+        """The list of weights with their gradients, made once for gradients that stay."""
+        return AdamWParts(self, grads)
+
+
+class AdamWParts:
+    """What Worker.adamw takes: states and gradients, by their addresses when it was made."""
+
+    def __init__(self, states, grads):
+        grads = list(grads)
+        if len(grads) != len(states.weights):
+            _refuse("as many gradients as weights")
+        for g, w in zip(grads, states.weights):
+            if g.get_device() != states.device or not g.is_contiguous() or g.numel() != w.numel():
+                _refuse("a gradient is contiguous, of its weight's size and on its GPU")
+        self.states, self.grads, self.n = states, grads, len(grads)
+        self.device = states.step.get_device()
+
+        def at(ts, i):
+            return None if ts is None else ts[i].data_ptr()
+
+        self.array = (gba_adamw_part * max(1, self.n))(*[
+            gba_adamw_part(w.data_ptr(), g.data_ptr(), at(states.m, i), at(states.v, i), at(states.m_scale, i),
+                           at(states.v_scale, i), at(states.copies, i), w.numel(), _type_of(w), _type_of(g),
+                           F32 if states.copies is None else _type_of(states.copies[i]), states.bits,
+                           states.decays[i])
+            for i, (w, g) in enumerate(zip(states.weights, grads))])
+
+
+def adamw_states(weights, **how):
+    """AdamW's states of a list of weights (see AdamWStates)."""
+    return AdamWStates(weights, **how)
+
+
 class Worker:
     """A worker's operators on one CUDA device: lookups and their gradient, norm and clipping,
-    layer norm (see include/gba.h).
+    layer norm, and those of a block: norms with a gate and the residual, gated scans, AdamW (see
+    include/gba.h).
 
     Work is issued on `stream` (default: the current one), on the stream's device.  A call made while another stream
     is current orders the two both ways, so tensors of the current stream can be passed and
@@ -792,3 +987,155 @@ class Worker:
         self._call("gba_layer_norm_grad", _matrix(dr), _matrix(xr), pg, ptype, mean.data_ptr(),
                    rstd.data_ptr(), _matrix(dx), dgamma.data_ptr(), dbeta.data_ptr())
         return dx if x.dim() == 2 else dx.view(x.shape), dgamma, dbeta
+
+    def _block(self, block, x, *others):
+        """Rows of x and of the others (None stays None), checked against the block and the worker."""
+        if not isinstance(block, ResidualNorm):
+            _refuse("a block is made by residual_norm()")
+        if block.device is not None and block.device != self._index:
+            _refuse("a parameter is not on the worker's GPU")
+        self._mine(x, *others)
+        if block.cols is not None and block.cols != x.shape[-1]:
+            _refuse("a parameter has a value per column")
+        for t in others:
+            if t is not None and t.shape != x.shape:
+                _refuse("tensors of different shapes")
+        return [None if t is None else _rows_of(t) for t in (x, *others)]
+
+    def residual_norm(self, block, x, residual=None, gate=None, keep_sum=True, sum_out=None, sum_dtype=None):
+        """(y, z, stats): z = residual_scale * residual + block_scale * act(gate) * post_norm(x) and
+        y = pre_norm(z), with the parameters of block (None where its pre_norm is none).  z goes to
+        sum_out (the residual itself, say); keep_sum=False: it is not kept.  Without a residual z
+        has the type sum_dtype (default: x's), else the residual's."""
+        rows, res, g, so = self._block(block, x, residual, gate, sum_out)
+        if so is not None and (so.data_ptr() != sum_out.data_ptr() or not keep_sum):
+            _refuse("sum_out has rows of consecutive elements, and is kept")
+        n, d = rows.shape
+        y = self._new(n, d, dtype=x.dtype) if block.pre else None
+        z = so
+        if z is None and keep_sum:
+            z = self._new(n, d, dtype=residual.dtype if residual is not None else sum_dtype or x.dtype)
+        stats = self._new(n, 4)
+        self._call("gba_residual_norm", block.block, _matrix(rows), _opt(res), _opt(g), _opt(z), _opt(y),
+                   stats.data_ptr())
+        return (_shaped(y, x), sum_out if sum_out is not None else _shaped(z, x), stats)
+
+    def residual_norm_grad(self, block, dy, dz, x, z, stats, gate=None, residual=True):
+        """The gradients of residual_norm's inputs and parameters, from those of y and z (dy None
+        where block has no pre_norm, dz None for none) and what it took and gave: a dict of dx,
+        dresidual (unless residual is False), dgate and dpost_weight, dpost_bias, dpre_weight and
+        dpre_bias, each if what it belongs to is there."""
+        if not block.pre:
+            z = None
+        if z is None and dz is None:
+            _refuse("neither dy nor dz")
+        xr, dyr, dzr, zr, g = self._block(block, x, dy, dz, z, gate)
+        self._mine(stats)
+        n, d = xr.shape
+        if stats.dtype != self.torch.float32 or stats.numel() != 4 * n or not stats.is_contiguous():
+            _refuse("stats are those of residual_norm")
+        wide = (z if z is not None else dz).dtype
+        out = {"dx": self._new(n, d, dtype=x.dtype)}
+        if residual:
+            out["dresidual"] = self._new(n, d, dtype=wide)
+        if gate is not None:
+            out["dgate"] = self._new(n, d, dtype=x.dtype)
+        sums = gba_block_grads()
+        for name, p in zip(("post_weight", "post_bias", "pre_weight", "pre_bias"), block.tensors):
+            if p is not None:
+                out["d" + name] = t = self._new(d)
+                setattr(sums, name, t.data_ptr())
+        self._call("gba_residual_norm_grad", block.block, _opt(dyr), _opt(dzr), _matrix(xr), _opt(zr), _opt(g),
+                   stats.data_ptr(), _matrix(out["dx"]), _opt(out.get("dresidual")), _opt(out.get("dgate")), sums)
+        for k in ("dx", "dresidual", "dgate"):
+            if k in out:
+                out[k] = _shaped(out[k], x)
+        return out
+
+    def _scan(self, seq, decay, tied, x, *others):
+        if not isinstance(seq, Sequences):
+            _refuse("sequences are made by sequences()")
+        if decay not in DECAYS:
+            _refuse(f"decays are one of {list(DECAYS)}")
+        self._mine(x, seq.lengths, seq.offsets, *others)
+        for t in others:
+            if t is not None and t.shape != x.shape:
+                _refuse("tensors of different shapes")
+        desc = gba_scan(DECAYS[decay], int(bool(tied)), seq.n,
+                        None if seq.lengths is None else seq.lengths.data_ptr(),
+                        None if seq.offsets is None else seq.offsets.data_ptr())
+        return desc, [_rows_of(t) for t in (x, *others)]
+
+    def _state(self, t, seq, d):
+        if t is None:
+            return None
+        self._mine(t)
+        t = t if t.dim() == 2 else t.view(seq.n, d)
+        if tuple(t.shape) != (seq.n, d) or t.dtype != self.torch.float32:
+            _refuse("states are float32, a row for each sequence")
+        return t
+
+    def gated_scan(self, x, f, seq, decay="sigmoid", tied=True, state=None, state_out=None, dtype=None):
+        """(y, last): y = h with h = a h + (1 - a) x (a h + x unless tied) along the sequences of
+        the rows of x, from state (default zeros); a = sigmoid(f), or exp(min(f, 0)) with decay
+        "log".  last: h after each sequence's last row, into state_out if given (state itself, for
+        steps in place).  dtype: of y (x's or float32)."""
+        desc, (xr, fr) = self._scan(seq, decay, tied, x, f)
+        n, d = xr.shape
+        st, so = self._state(state, seq, d), self._state(state_out, seq, d)
+        if so is None:
+            so = self._new(seq.n, d)
+        y = self._new(n, d, dtype=dtype or x.dtype)
+        self._call("gba_gated_scan", desc, _matrix(xr), _matrix(fr), _opt(st), _matrix(y), _matrix(so))
+        return _shaped(y, x), state_out if state_out is not None else so
+
+    def gated_scan_grad(self, dy, x, f, y, seq, decay="sigmoid", tied=True, state=None, dstate=None):
+        """(dx, df, dstate) from the gradients of gated_scan's y and (dstate, default none) of its
+        last states; the last is None without a state."""
+        desc, (xr, fr, yr, dr) = self._scan(seq, decay, tied, x, f, y, dy)
+        n, d = xr.shape
+        st, ds = self._state(state, seq, d), self._state(dstate, seq, d)
+        dx, df = self._new(n, d, dtype=x.dtype), self._new(n, d, dtype=x.dtype)
+        out = None if st is None else self._new(seq.n, d)
+        self._call("gba_gated_scan_grad", desc, _matrix(dr), _opt(ds), _matrix(xr), _matrix(fr), _opt(st),
+                   _matrix(yr), _matrix(dx), _matrix(df), _opt(out))
+        return _shaped(dx, x), _shaped(df, x), out
+
+    def _adamw(self, parts):
+        if not isinstance(parts, AdamWParts):
+            _refuse("parts are made by AdamWStates.parts()")
+        if parts.device != self._index:
+            _refuse("a tensor is not on the worker's GPU")
+        return parts.states
+
+    def adamw(self, parts, lr, norm=None, max_norm=None):
+        """One step of AdamW over the weights of parts (AdamWStates.parts of their gradients), in
+        place.  lr: a number, or a device float32 that is read when the call runs.  norm (a device
+        float32, of grad_norm say) and max_norm clip the gradients on the way; with a norm that is
+        infinite or NaN nothing changes."""
+        st, torch = self._adamw(parts), self.torch
+        if (norm is None) != (max_norm is None):
+            _refuse("norm and max_norm go together")
+        now = lr if hasattr(lr, "data_ptr") else None
+        for t in (now, norm):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != 1):
+                _refuse("lr and norm are one float32")
+        self._mine(now, norm)
+        desc = gba_adamw_desc(0.0 if now is not None else lr, *st.betas, st.eps,
+                              None if now is None else now.data_ptr(), None if norm is None else norm.data_ptr(),
+                              0.0 if max_norm is None else max_norm)
+        self._call("gba_adamw", parts.array, parts.n, desc, st.step.data_ptr())
+
+    def adamw_values(self, parts, m_out=None, v_out=None):
+        """The states of parts as float32: (list of m, list of v), into the given lists of tensors."""
+        st = self._adamw(parts)
+        m_out, v_out = [[self._new(w.numel()) for w in st.weights] if o is None else list(o) for o in (m_out, v_out)]
+        for o in (m_out, v_out):
+            if len(o) != parts.n:
+                _refuse("as many outputs as weights")
+            self._mine(*o)
+            for t, w in zip(o, st.weights):
+                if t.numel() != w.numel() or t.dtype != self.torch.float32 or not t.is_contiguous():
+                    _refuse("an output is float32, contiguous and of its weight's size")
+        self._call("gba_adamw_values", parts.array, parts.n, _addresses(m_out), _addresses(v_out))
+        return m_out, v_out

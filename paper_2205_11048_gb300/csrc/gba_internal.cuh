@@ -10,6 +10,7 @@ namespace gba {
 constexpr uint32_t ERR_ID_RANGE = 1u;
 constexpr uint32_t ERR_TIMEOUT = 2u;
 constexpr uint32_t ERR_INTERNAL = 4u;
+constexpr uint32_t ERR_SEQUENCES = 8u;
 
 // Where kernels report a failure: the step's own word (later kernels of the
 // same step skip their work when it is set), the handle's word (what the host

@@ -1,5 +1,5 @@
 // Internal declarations of the worker's operators (lookup, its gradient, norm and
-// clipping, layer norm), shared by their translation units.
+// clipping, layer norm, and those of a block), shared by their translation units.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -258,5 +258,75 @@ cudaError_t launch_layer_norm(const LayerNormArgs& a, int32_t type, const RingWa
 size_t layer_norm_grad_workspace(const LayerNormArgs& a, int32_t type, int num_sms);
 cudaError_t launch_layer_norm_grad(const LayerNormArgs& a, int32_t type, const RingWait& w, int num_sms,
                                    cudaStream_t s);
+
+// ---- the end of a block and the norm before the next ----------------------------------
+struct Rows {
+  const void* p;  // null: not there
+  int64_t stride;
+};
+struct OutRows {
+  void* p;
+  int64_t stride;
+};
+struct ResNormArgs {
+  Rows x, r, g;     // the block's output, the residual, the gate
+  OutRows z, y;
+  float4* stats;
+  Rows dy, dz, zin; // of the gradient, whose input z is
+  OutRows dx, dr, dg;
+  const void* post_weight;
+  const void* post_bias;
+  const void* pre_weight;
+  const void* pre_bias;
+  float* sums[4];   // gradients of those, in that order; null: not wanted
+  float* parts;     // workspace of the gradient
+  int64_t n;
+  int32_t d;
+  int32_t post, pre, gate, param_type;
+  float eps, rscale, bscale;
+};
+// type: of x; wide: of the residual and z
+cudaError_t launch_residual_norm(const ResNormArgs& a, int32_t type, int32_t wide, int num_sms, cudaStream_t s);
+size_t residual_norm_grad_workspace(const ResNormArgs& a, int32_t type, int32_t wide, int num_sms);
+cudaError_t launch_residual_norm_grad(const ResNormArgs& a, int32_t type, int32_t wide, int num_sms, cudaStream_t s);
+
+// ---- gated scan -----------------------------------------------------------------------
+struct ScanArgs {
+  Rows x, f;
+  Rows y;           // of the gradient
+  Rows dy;
+  OutRows out;      // y, or dx of the gradient
+  OutRows df;
+  const float* state;  // what comes in before a first row (the gradient's: after a last row), or null
+  int64_t state_stride;
+  float* last;         // what goes out behind a last row (before a first row), or null
+  int64_t last_stride;
+  const float* h0;     // the gradient's: the first states, or null
+  int64_t h0_stride;
+  const int64_t* lengths;
+  const int64_t* offsets;
+  int64_t n_seq, n;    // sequences, rows
+  int32_t d;
+  int32_t decay, tied;
+  ErrSink err;
+};
+size_t scan_workspace(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int num_sms);
+// out_type: of y (and dy)
+cudaError_t launch_scan(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, char* ws, int64_t wait_ns,
+                        int num_sms, cudaStream_t s);
+
+// ---- AdamW ------------------------------------------------------------------------------
+struct AdamWArgs {
+  float lr, beta1, beta2, rest1, rest2, eps;  // rest: 1 - beta
+  double log1, log2;                          // logarithms of the betas
+  const float* lr_now;
+  const float* norm;
+  float max_norm;
+  int64_t* step;
+  uint32_t* ticket;  // a zero word that is zero again afterwards
+};
+cudaError_t launch_adamw(const gba_adamw_part* parts, int32_t n_parts, AdamWArgs a, int num_sms, cudaStream_t s);
+cudaError_t launch_adamw_values(const gba_adamw_part* parts, int32_t n_parts, float* const* m_out,
+                                float* const* v_out, int num_sms, cudaStream_t s);
 
 }  // namespace gba
