@@ -19,7 +19,8 @@ LIB = os.path.join(HERE, "libgba.so")
 SOURCES = ["gba_host.cu", "gba_sort.cu", "gba_rows.cu", "gba_dense.cu", "gba_misc.cu",
            "gba_noalloc.cu", "gba_pull.cu", "gba_push.cu", "gba_tokens.cu",
            "gba_worker.cu", "gba_embed.cu", "gba_norm.cu", "gba_layernorm.cu",
-           "gba_block.cu", "gba_resnorm.cu", "gba_scan.cu", "gba_adamw.cu"]
+           "gba_block.cu", "gba_resnorm.cu", "gba_scan.cu", "gba_scan_grad.cu",
+           "gba_adamw.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include")]
 
@@ -35,7 +36,8 @@ def _stale(obj: str, src: str) -> bool:
     if not os.path.exists(obj):
         return True
     deps = [src, os.path.join(CSRC, "gba_internal.cuh"), os.path.join(CSRC, "gba_worker.cuh"),
-            os.path.join(CSRC, "gba_worker_handle.cuh"), os.path.join(ROOT, "include", "gba.h")]
+            os.path.join(CSRC, "gba_worker_handle.cuh"), os.path.join(CSRC, "gba_scan.cuh"),
+            os.path.join(ROOT, "include", "gba.h")]
     return any(os.path.getmtime(d) > os.path.getmtime(obj) for d in deps)
 
 

@@ -115,7 +115,7 @@ gba_status run_scan(gba_worker* w, const ScanArgs& a, int32_t type, int32_t out_
   if (a.n == 0 && (a.n_seq == 0 || !a.last)) return GBA_OK;
   const gba_status st = reserve(w, scan_workspace(a, type, out_type, grad, w->num_sms));
   if (st != GBA_OK) return st;
-  const cudaError_t e = launch_scan(a, type, out_type, grad, w->ws, WAIT_NS, w->num_sms, w->stream);
+  const cudaError_t e = launch_scan(a, type, out_type, grad, w->ws, w->num_sms, w->stream);
   return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "launch the scan");
 }
 

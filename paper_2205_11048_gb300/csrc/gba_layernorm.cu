@@ -64,39 +64,6 @@ __device__ __forceinline__ void params_at(const void* p, int32_t type, int64_t c
   }
 }
 
-// ---- two floats in one operation ---------------------------------------------------
-struct f2 {
-  unsigned long long u;
-};
-__device__ __forceinline__ f2 pair(float lo, float hi) {
-  f2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void split(f2 a, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.u));
-}
-__device__ __forceinline__ f2 add2(f2 a, f2 b) {
-  f2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-  return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-  return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
-  f2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
-  return r;
-}
-__device__ __forceinline__ float both(f2 a) {
-  float lo, hi;
-  split(a, lo, hi);
-  return lo + hi;
-}
-
 // ---- how a block's threads share rows ----------------------------------------------
 // LANES: a row belongs to L lanes of a warp, and a lane's piece k of V columns is the row's
 // piece k L + lane.  Otherwise it belongs to W warps, warp w holds the 32 E columns from

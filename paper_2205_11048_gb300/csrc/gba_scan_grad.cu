@@ -1,0 +1,205 @@
+// The gradient of the gated scan (see gba_scan.cu), a scan from the last row to the first:
+//   G_t = dy_t + S_(t+1),  S_t = a_t G_t,  dx = G (1 - a) or G,  df = G (h_(t-1) - x or 0) a (1 - a or 1).
+#include "gba_scan.cuh"
+
+namespace gba {
+
+namespace {
+
+constexpr int STAGES = 2;
+
+template <typename T, typename O, int TX, int STEPS, bool LOOSE, bool TAIL>
+struct Shared {
+  Joint<TX, STEPS> j;
+  struct {
+    Stage<T, TX, STEPS, LOOSE> f;
+    Stage<O, TX, STEPS, LOOSE> dy;
+    Stage<T, TX, TAIL ? 1 : STEPS, LOOSE> x;  // not needed for a segment's pair
+    Stage<O, TX, TAIL ? 1 : STEPS, LOOSE> y;
+    Marks<TX, STEPS> marks;
+  } in[STAGES];
+  char swap[LOOSE ? SCAN_THREADS * V * 4 : 16];
+};
+
+// TAIL: only the pair of each segment but the last, from its last entry on.
+template <typename T, typename O, int TX, int STEPS, bool LOOSE, bool TAIL>
+__global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArgs a, ScanPlan plan) {
+  extern __shared__ __align__(16) char smem[];
+  auto& sh = *reinterpret_cast<Shared<T, O, TX, STEPS, LOOSE, TAIL>*>(smem);
+  using At = Spot<TX, STEPS>;
+  follow();
+  const At at(plan);
+  const bool in = at.c < a.d;
+  // the segment's rows, from the last on
+  int64_t hi = a.n - (int64_t)at.seg * plan.rows;
+  const int64_t lo = hi > plan.rows ? hi - plan.rows : 0;
+  Pairs run;
+  run.clear();
+  if constexpr (TAIL) {
+    const int32_t m = mark_of(plan, lo - 1);
+    if (m == NONE || (m & LAST)) return;  // nothing goes there
+    if (plan.marks) {
+      for (int64_t low = lo; low < hi; low += SCAN_THREADS) {
+        const int64_t r = low + threadIdx.x;
+        const int32_t q = r < hi ? plan.marks[r] : 0;
+        if (__syncthreads_or(q == NONE || (q & LAST))) {
+          hi = low + SCAN_THREADS < hi ? low + SCAN_THREADS : hi;
+          break;
+        }
+      }
+    } else {
+      const int64_t behind = (lo + plan.each - 1) / plan.each * plan.each;  // of the sequence that lo is in
+      if (behind < hi) hi = behind;
+    }
+  } else if (plan.chained && at.seg > 0) {
+    const int32_t m = mark_of(plan, hi - 1);
+    if (m != NONE && !(m & LAST)) into_segment(sh.j, plan, at, run);
+  }
+  const int tiles = (int)((hi - lo + At::ROWS - 1) / At::ROWS);
+  int64_t row = hi - 1 - at.ty * STEPS, ahead = row;
+  uint32_t pos = place_of(plan, row - (STEPS - 1));
+  auto fetch = [&](int to) {
+    auto& s = sh.in[to];
+    s.f.template fetch<true>(a.f, at, ahead, lo, hi, a.d, a.n);
+    s.dy.template fetch<true>(a.dy, at, ahead, lo, hi, a.d, a.n);
+    if constexpr (!TAIL) {
+      if (a.tied) s.x.template fetch<true>(a.x, at, ahead, lo, hi, a.d, a.n);
+      s.y.template fetch<true>(a.y, at, ahead - 1, lo > 0 ? lo - 1 : 0, hi, a.d, a.n);
+    }
+    s.marks.template fetch<true>(plan, at, ahead, lo, hi);
+    ahead -= At::ROWS;
+    copies_begun();
+  };
+#pragma unroll
+  for (int k = 0; k < STAGES; ++k) fetch(k);
+  int stage = 0;
+  for (int t = 0; t < tiles; ++t, row -= At::ROWS, pos = moved<true>(plan, pos, At::ROWS)) {
+    copies_done<STAGES - 1>();
+    if constexpr (LOOSE) sync_row<TX>();
+    auto& here = sh.in[stage];
+    Vec A[STEPS], R[STEPS];  // the decays, and what dx and df have of 1 - a
+    if (a.decay == GBA_DECAY_SIGMOID) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], R[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) log_gates(here.f.get(i, at), a.tied, A[i], R[i]);
+    }
+    Pairs mine;  // S -> A S + h
+    mine.clear();
+    int32_t m[STEPS];
+    const bool mixed = here.marks.template get<true>(plan, at, row, lo, hi, pos, m);
+    if (!mixed) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) mine.then(A[i], A[i] * here.dy.get(i, at), false);
+    } else {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        Vec dy = here.dy.get(i, at);
+        if (m[i] == NONE) {
+          if (!inside(row - i, lo, hi)) continue;  // no row of the segment: it changes nothing
+          dy.fill(0.f);
+          mine.then(A[i], dy, true);
+          continue;
+        }
+        if ((m[i] & LAST) && a.state && in) dy = dy + state_row<LOOSE>(a.state, a.state_stride, m[i], at.c, a.d);
+        mine.then(A[i], A[i] * dy, m[i] & LAST);
+      }
+    }
+    sh.j.put(t & 1, at, mine);
+    __syncthreads();
+    Vec v;
+    sh.j.then(t & 1, at, run, v);
+    if constexpr (!TAIL) {
+      // dx and df of position i, from the gradient v that comes to it and h before it
+      auto outputs = [&](int i, const Vec& decay, const Vec& rest, const Vec& h) {
+        v = v + here.dy.get(i, at);  // G
+        Vec dx = v, df;
+        v = v * decay;  // S
+        if (a.tied) {
+          float x[V], y[V];
+          here.x.get(i, at).get(x);
+          h.get(y);
+#pragma unroll
+          for (int j = 0; j < V; ++j) y[j] -= x[j];
+          Vec diff;
+          diff.set(y);
+          dx = dx * rest;
+          df = v * diff;
+        } else {
+          df = v * h;
+        }
+        if (a.decay == GBA_DECAY_SIGMOID) {
+          df = df * rest;
+        } else {
+          float f[V], g[V];
+          here.f.get(i, at).get(f);
+          df.get(g);
+#pragma unroll
+          for (int j = 0; j < V; ++j) g[j] = f[j] > 0.f ? 0.f : g[j];
+          df.set(g);
+        }
+        put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, dx, sh.swap);
+        put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, df, sh.swap);
+      };
+      if (LOOSE || in) {
+        if (!mixed) {
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) outputs(i, A[i], R[i], here.y.get(i, at));
+        } else {
+#pragma unroll
+          for (int i = 0; i < STEPS; ++i) {
+            if (!inside(row - i, lo, hi)) break;
+            if (m[i] == NONE) {
+              v.fill(0.f);
+              put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, v, sh.swap);
+              put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, v, sh.swap);
+              continue;
+            }
+            Vec h = here.y.get(i, at);
+            if ((m[i] & FIRST) && in) h = state_row<LOOSE>(a.h0, a.h0_stride, m[i], at.c, a.d);
+            if ((m[i] & LAST) && in) v = state_row<LOOSE>(a.state, a.state_stride, m[i], at.c, a.d);
+            outputs(i, A[i], R[i], h);
+            if (a.last && (m[i] & FIRST) && in) keep_row<LOOSE>(a.last, a.last_stride, m[i], at.c, a.d, v);
+          }
+        }
+      }
+    }
+    if constexpr (LOOSE) sync_row<TX>();  // the row's lanes have read this stage
+    fetch(stage);
+    stage = stage == STAGES - 1 ? 0 : stage + 1;
+  }
+  copies_done<0>();
+  if constexpr (TAIL) {
+    if (at.ty == 0) run.put(plan.words + (size_t)at.seg * plan.pad + (size_t)at.col * At::COLS + at.tx * V);
+  }
+}
+
+template <typename T, typename O, int TX, int STEPS, bool LOOSE>
+cudaError_t start(const ScanArgs& a, const ScanPlan& p, cudaStream_t s) {
+  if (p.chained) {
+    const cudaError_t e = start_scan<Shared<T, O, TX, STEPS, LOOSE, true>>(
+        k_scan_grad<T, O, TX, STEPS, LOOSE, true>, (p.n_segs - 1) * p.n_cols, a, p, s);
+    if (e != cudaSuccess) return e;
+  }
+  return start_scan<Shared<T, O, TX, STEPS, LOOSE, false>>(k_scan_grad<T, O, TX, STEPS, LOOSE, false>,
+                                                           p.n_segs * p.n_cols, a, p, s);
+}
+
+template <typename T, typename O>
+cudaError_t launch_as(const ScanArgs& a, const ScanPlan& p, cudaStream_t s) {
+  if (p.tx == 8)
+    return p.loose ? start<T, O, 8, SCAN_STEPS, true>(a, p, s) : start<T, O, 8, SCAN_STEPS, false>(a, p, s);
+  if (p.loose) return start<T, O, 32, SCAN_STEPS, true>(a, p, s);
+  return p.steps == SCAN_STEPS ? start<T, O, 32, SCAN_STEPS, false>(a, p, s) : start<T, O, 32, SCAN_FEW, false>(a, p, s);
+}
+
+}  // namespace
+
+cudaError_t start_scan_grad(const ScanArgs& a, int32_t type, int32_t out_type, const ScanPlan& p, cudaStream_t s) {
+  if (type == GBA_F32) return launch_as<float, float>(a, p, s);
+  if (type == GBA_BF16) return out_type == GBA_F32 ? launch_as<bf16, float>(a, p, s) : launch_as<bf16, bf16>(a, p, s);
+  return out_type == GBA_F32 ? launch_as<f16, float>(a, p, s) : launch_as<f16, f16>(a, p, s);
+}
+
+}  // namespace gba

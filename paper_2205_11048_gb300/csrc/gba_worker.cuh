@@ -73,10 +73,23 @@ struct Pack {
     for (int i = 0; i < V; ++i) x[i] = to_float(t[i]);
   }
   __device__ __forceinline__ void set(const float (&x)[V]) {
-    T t[V];
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {  // two in one conversion
+      using Two = std::conditional_t<std::is_same_v<T, bf16>, __nv_bfloat162, __half2>;
+      Two t[V / 2];
 #pragma unroll
-    for (int i = 0; i < V; ++i) t[i] = from_float<T>(x[i]);
-    memcpy(w, t, sizeof t);
+      for (int i = 0; i < V / 2; ++i) {
+        if constexpr (std::is_same_v<T, bf16>)
+          t[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        else
+          t[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      }
+      memcpy(w, t, sizeof t);
+    } else {
+      T t[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) t[i] = from_float<T>(x[i]);
+      memcpy(w, t, sizeof t);
+    }
   }
 };
 
@@ -121,6 +134,39 @@ struct Loose {
     for (int j = 0; j < V; ++j) x[j] = to_float(t[j]);
   }
 };
+
+// ---- two floats in one operation ---------------------------------------------------
+struct f2 {
+  unsigned long long u;
+};
+__device__ __forceinline__ f2 pair(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.u) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void split(f2 a, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.u));
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+  return r;
+}
+__device__ __forceinline__ float both(f2 a) {
+  float lo, hi;
+  split(a, lo, hi);
+  return lo + hi;
+}
 
 // The most elements (a power of two, at most `most`) that an access may take of rows of
 // `cols` elements of `bytes` each, `stride` apart from `p` on.
@@ -312,8 +358,8 @@ struct ScanArgs {
 };
 size_t scan_workspace(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int num_sms);
 // out_type: of y (and dy)
-cudaError_t launch_scan(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, char* ws, int64_t wait_ns,
-                        int num_sms, cudaStream_t s);
+cudaError_t launch_scan(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, char* ws, int num_sms,
+                        cudaStream_t s);
 
 // ---- AdamW ------------------------------------------------------------------------------
 struct AdamWArgs {

@@ -20,7 +20,7 @@ cudaError_t launch_residual_norm_grad(const ResNormArgs& a, int32_t, int32_t, in
   return cudaSuccess;
 }
 size_t scan_workspace(const ScanArgs& a, int32_t, int32_t, bool, int) { return 256 + (size_t)a.n * 4; }
-cudaError_t launch_scan(const ScanArgs& a, int32_t, int32_t, bool, char* ws, int64_t, int, cudaStream_t) {
+cudaError_t launch_scan(const ScanArgs& a, int32_t, int32_t, bool, char* ws, int, cudaStream_t) {
   ++g_block_launches;
   fake_need(ws, 256 + (size_t)a.n * 4);
   return cudaSuccess;

@@ -430,21 +430,38 @@ def flags(at, rows, inside):
     return e
 
 
+def gate_units(f, a, rest, decay):
+    """How far a gate's decay and one minus it may be off, of themselves, in units of U.  With
+    t = exp(-f) from the hardware's power of two, which is off by 2^-22 of itself (4 U), and a
+    rounded argument (|f| U): a = 1/(1+t) by t/(1+t) = 1-a times that, and t a by 1/(1+t) = a
+    times it, with 4 for the sum, the quotient and the product; exp(f) by all of it, and
+    1 - exp(f) by CUDA's expm1f within 2."""
+    own = f.abs().clamp(max=100.0) + 4.0
+    if decay == "log":
+        return own + 1.0, torch.full_like(own, 3.0)
+    return own * rest + 4.0, own * a + 4.0
+
+
 def plain_scan(x, f, first, length, decay, tied, state):
-    """(y, last) in 64 bits, with the bound of their rounding in units of U: every value takes C
-    roundings in its own making, and a step passes on what was off, times the decay."""
-    C = 12
-    a, rest = decays(f.double(), decay)
+    """(y, last) in 64 bits, with the bound of their rounding in units of U: a step passes on what
+    was off, times the decay, and adds what its gates are off and four roundings (of the input, of
+    its own sum, and of the pairs that it is joined through)."""
+    f = f.double()
+    a, rest = decays(f, decay)
+    ua, ub = gate_units(f, a, rest, decay)
     b = rest * x.double() if tied else x.double()
     rows, d = x.shape
     begin, end, on, inside = where_rows(first, length, rows)
     last = torch.zeros(len(first), d, dtype=torch.float64, device="cuda") if state is None else state.double().clone()
-    b, mb = torch.where(inside[:, None], b, 0.0), torch.where(inside[:, None], b.abs(), 0.0)
+    b = torch.where(inside[:, None], b, 0.0)
+    own = b.abs()
+    mb = own.clone()
     b[begin] += a[begin] * last[on]
     mb[begin] += a[begin] * last[on].abs()
     entry = flags(begin, rows, inside)
     y, m = recurrence(a, b, entry), recurrence(a, mb, entry)
-    off = recurrence(a, C * m, entry)
+    more = ua * (m - own) + (ub * own if tied else 0.0) + 4.0 * m
+    off = recurrence(a, torch.where(inside[:, None], more, 0.0), entry)
     last[on] = y[end]
     e = torch.zeros_like(last)
     e[on] = off[end]
@@ -452,32 +469,38 @@ def plain_scan(x, f, first, length, decay, tied, state):
 
 
 def plain_scan_grad(dy, x, f, y, first, length, decay, tied, state, dlast):
-    C = 16
-    a, rest = decays(f.double(), decay)
+    f = f.double()
+    a, rest = decays(f, decay)
+    ua, ub = gate_units(f, a, rest, decay)
     rows, d = x.shape
     begin, end, on, inside = where_rows(first, length, rows)
+    own = inside[:, None]
+    a, ua = torch.where(own, a, 0.0), torch.where(own, ua, 0.0)
     S = torch.zeros(len(first), d, dtype=torch.float64, device="cuda") if dlast is None else dlast.double().clone()
-    G = torch.where(inside[:, None], dy.double(), 0.0)
+    G = torch.where(own, dy.double(), 0.0)
     mG = G.abs()
     G[end] += S[on]
     mG[end] += S[on].abs()
     entry = flags(end, rows, inside)
-    after = torch.cat([a[1:], torch.zeros_like(a[:1])])  # what the next row's gradient comes here through
+    # what the next row's gradient comes here through
+    nothing = torch.zeros_like(a[:1])
+    after, uafter = torch.cat([a[1:], nothing]), torch.cat([ua[1:], nothing])
     G, mG = recurrence(after, G, entry, True), recurrence(after, mG, entry, True)
-    eG = recurrence(after, C * mG, entry, True)
-    h = torch.cat([torch.zeros_like(a[:1]), y[:-1].double()])
+    passed = torch.where(entry[:, None], 0.0, after * torch.cat([mG[1:], nothing]))
+    eG = recurrence(after, uafter * passed + 4.0 * mG, entry, True)
+    h = torch.cat([nothing, y[:-1].double()])
     h[begin] = 0.0 if state is None else state.double()[on]
     mh = h.abs()
     if tied:
         h, mh = h - x.double(), mh + x.double().abs()
-    s = a * rest if decay == "sigmoid" else torch.where(f.double() > 0, 0.0, a)
-    r = rest if tied else torch.ones_like(G)
-    own = inside[:, None]
-    out = {"dx": torch.where(own, G * r, 0.0), "ex": torch.where(own, eG * r + C * mG * r, 0.0),
-           "df": torch.where(own, G * h * s, 0.0), "ef": torch.where(own, eG * h.abs() * s + C * mG * mh * s, 0.0)}
+    s = a * rest if decay == "sigmoid" else torch.where(f > 0, 0.0, a)
+    us = ua + ub if decay == "sigmoid" else ua
+    r, ur = (rest, ub) if tied else (torch.ones_like(G), 0.0)
+    out = {"dx": G * r, "ex": eG * r + (ur + 2.0) * mG * r, "df": G * h * s, "ef": eG * h.abs() * s + (us + 5.0) * mG * mh * s}
+    out = {k: torch.where(own, v, 0.0) for k, v in out.items()}
     e = torch.zeros_like(S)
     S[on] = (a * G)[begin]
-    e[on] = (a * eG + C * a * mG)[begin]
+    e[on] = (a * eG + (ua + 2.0) * a * mG)[begin]
     return out, S, e
 
 
