@@ -132,11 +132,14 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
   for (int k = 0; k < STAGES - 1; ++k) fetch(k);
   int stage = 0;
   for (int t = 0; t < tiles; ++t, row += At::ROWS, pos = moved<false>(plan, pos, At::ROWS)) {
-    fetch(stage == 0 ? STAGES - 1 : stage - 1);  // its rows were done with before the last barrier
+    sync_row<TX>();  // the row's lanes have done with the stage that is filled next
+    fetch(stage == 0 ? STAGES - 1 : stage - 1);
     copies_done<STAGES - 1>();
-    if constexpr (LOOSE) sync_row<TX>();
+    sync_row<TX>();
     const auto& here = sh.in[stage];
-    Vec A[STEPS], B[STEPS];  // h -> A h + B, or B at an entry
+    Pairs mine;
+    mine.clear();
+    Vec A[STEPS], B[STEPS];  // h -> A h + B
     if (a.decay == GBA_DECAY_SIGMOID) {
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], B[i]);
@@ -151,11 +154,10 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) B[i] = here.x.get(i, at);
     }
-    Pairs mine;
-    mine.clear();
     int32_t m[STEPS];
-    const bool mixed = here.marks.template get<false>(plan, at, row, lo, hi, pos, m);
+    const bool mixed = here.marks.template mixed<false>(plan, at, row, lo, hi, pos);
     if (mixed) {
+      here.marks.template all<false>(plan, at, row, lo, hi, m);
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
         if (m[i] == NONE) {
@@ -202,6 +204,9 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
 }
 
 // ---- launches ------------------------------------------------------------------------------
+constexpr int64_t WAVES = 1;    // blocks for each place on the SMs
+constexpr int64_t SHORT = 256;  // rows of a segment of whole sequences, about
+
 struct Shape {
   ScanPlan p;
   bool marks;
@@ -220,30 +225,33 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
             fits(a.out.p, a.out.stride, grad ? b : ob);
   if (grad) ok = ok && fits(a.y.p, a.y.stride, ob) && fits(a.dy.p, a.dy.stride, ob) && fits(a.df.p, a.df.stride, b);
   p.loose = !ok;
+  p.num_sms = num_sms;
   p.tx = a.d <= 16 * V ? 8 : 32;
   const uint32_t cols = (uint32_t)(p.tx * V);
   p.n_cols = (uint32_t)((a.d + cols - 1) / cols);
   p.pad = p.n_cols * cols;
   p.each = (uint32_t)(a.n_seq > 0 ? a.n / a.n_seq : 0);
   s.marks = a.offsets || a.lengths;
-  const int64_t ty = SCAN_THREADS / p.tx, slots = (int64_t)num_sms * (grad ? GRAD_BLOCKS : SCAN_BLOCKS);
+  // blocks that run at a time: 16-bit rows of four (the gradient: three) fit an SM, float32 rows of one less
+  const bool wide = grad ? b == 4 || ob == 4 : b == 4;
+  const int64_t ty = SCAN_THREADS / p.tx, slots = (int64_t)num_sms * ((grad ? GRAD_BLOCKS : SCAN_BLOCKS) - wide);
   const bool few = (a.n + ty * SCAN_STEPS - 1) / (ty * SCAN_STEPS) * p.n_cols < num_sms;
   p.steps = few && !p.loose && p.tx == 32 ? SCAN_FEW : SCAN_STEPS;
-  const int64_t tile = ty * p.steps, want = std::max<int64_t>(1, slots / p.n_cols);  // segments
+  const int64_t tile = ty * p.steps, want = std::max<int64_t>(1, WAVES * slots / p.n_cols);
   int64_t rows = std::max((a.n + want - 1) / want, tile);
   if (s.marks) {
     rows = (rows + tile - 1) / tile * tile;
     p.chained = rows < a.n;
   } else if (a.n > 0) {
-    const int64_t each = p.each, whole = (rows + each - 1) / each * each;
-    // sequences are not split where most of the GPU has one, or their segments are about as long
-    if (whole <= rows + rows / 2 || a.n_seq * p.n_cols * 3 >= slots * 2) {
-      rows = whole;
+    const int64_t each = p.each;
+    if (each <= 2 * rows || a.n_seq * p.n_cols >= (int64_t)num_sms * (grad ? 8 : 5) / 4) {
+      // whole sequences, which need nothing of one another, so the segments may be short
+      rows = std::max(tile, std::min(rows, SHORT));
+      rows = std::max<int64_t>(1, (rows + each / 2) / each) * each;
     } else {
-      const int64_t pieces = std::max<int64_t>(1, want / a.n_seq);  // no more blocks than run at a time
-      rows = (each + pieces - 1) / pieces;
-      rows = (rows + tile - 1) / tile * tile;
-      p.chained = true;
+      const int64_t pieces = std::max<int64_t>(1, want / a.n_seq);
+      p.chained = pieces > 1;
+      rows = pieces == 1 ? each : ((each + pieces - 1) / pieces + tile - 1) / tile * tile;
     }
   }
   p.rows = rows;

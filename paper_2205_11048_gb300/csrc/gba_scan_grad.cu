@@ -75,36 +75,36 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
   int stage = 0;
   for (int t = 0; t < tiles; ++t, row -= At::ROWS, pos = moved<true>(plan, pos, At::ROWS)) {
     copies_done<STAGES - 1>();
-    if constexpr (LOOSE) sync_row<TX>();
+    sync_row<TX>();
     auto& here = sh.in[stage];
-    Vec A[STEPS], R[STEPS];  // the decays, and what dx and df have of 1 - a
-    if (a.decay == GBA_DECAY_SIGMOID) {
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], R[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) log_gates(here.f.get(i, at), a.tied, A[i], R[i]);
-    }
     Pairs mine;  // S -> A S + h
     mine.clear();
-    int32_t m[STEPS];
-    const bool mixed = here.marks.template get<true>(plan, at, row, lo, hi, pos, m);
-    if (!mixed) {
+    Vec A[STEPS], R[STEPS];  // the decays, and what dx and df have of 1 - a
+    // Rows where sequences begin or end, or that are none, go one after another, in code of few
+    // instructions: unrolled like the others they leave no room in the instruction cache (65,536 x
+    // 2,048 in 64 sequences 398 us instead of 364; branches within one unrolled loop, 484).
+    const bool mixed = here.marks.template mixed<true>(plan, at, row, lo, hi, pos);
+    if (mixed) {
+#pragma unroll 1
+      for (int i = 0; i < STEPS && row - i >= lo; ++i) {
+        const int32_t m = here.marks.get(plan, at, i, row - i);
+        Vec g, rest, dy = here.dy.get(i, at);
+        gates(a.decay, false, here.f.get(i, at), g, rest);
+        if (m != NONE && (m & LAST) && a.state && in) dy = dy + state_row<LOOSE>(a.state, a.state_stride, m, at.c, a.d);
+        dy = g * dy;
+        if (m == NONE) dy.fill(0.f);
+        mine.then(g, dy, m == NONE || (m & LAST));
+      }
+    } else {
+      if (a.decay == GBA_DECAY_SIGMOID) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], R[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) log_gates(here.f.get(i, at), a.tied, A[i], R[i]);
+      }
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) mine.then(A[i], A[i] * here.dy.get(i, at), false);
-    } else {
-#pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        Vec dy = here.dy.get(i, at);
-        if (m[i] == NONE) {
-          if (!inside(row - i, lo, hi)) continue;  // no row of the segment: it changes nothing
-          dy.fill(0.f);
-          mine.then(A[i], dy, true);
-          continue;
-        }
-        if ((m[i] & LAST) && a.state && in) dy = dy + state_row<LOOSE>(a.state, a.state_stride, m[i], at.c, a.d);
-        mine.then(A[i], A[i] * dy, m[i] & LAST);
-      }
     }
     sh.j.put(t & 1, at, mine);
     __syncthreads();
@@ -142,30 +142,30 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
         put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, dx, sh.swap);
         put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, df, sh.swap);
       };
-      if (LOOSE || in) {
-        if (!mixed) {
-#pragma unroll
-          for (int i = 0; i < STEPS; ++i) outputs(i, A[i], R[i], here.y.get(i, at));
-        } else {
-#pragma unroll
-          for (int i = 0; i < STEPS; ++i) {
-            if (!inside(row - i, lo, hi)) break;
-            if (m[i] == NONE) {
-              v.fill(0.f);
-              put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, v, sh.swap);
-              put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, v, sh.swap);
-              continue;
-            }
-            Vec h = here.y.get(i, at);
-            if ((m[i] & FIRST) && in) h = state_row<LOOSE>(a.h0, a.h0_stride, m[i], at.c, a.d);
-            if ((m[i] & LAST) && in) v = state_row<LOOSE>(a.state, a.state_stride, m[i], at.c, a.d);
-            outputs(i, A[i], R[i], h);
-            if (a.last && (m[i] & FIRST) && in) keep_row<LOOSE>(a.last, a.last_stride, m[i], at.c, a.d, v);
+      if (mixed) {
+#pragma unroll 1
+        for (int i = 0; i < STEPS && row - i >= lo; ++i) {
+          if (!LOOSE && !in) break;
+          const int32_t m = here.marks.get(plan, at, i, row - i);
+          if (m == NONE) {
+            v.fill(0.f);
+            put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, v, sh.swap);
+            put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, v, sh.swap);
+            continue;
           }
+          Vec g, rest, h = here.y.get(i, at);
+          gates(a.decay, a.tied, here.f.get(i, at), g, rest);
+          if ((m & FIRST) && in) h = state_row<LOOSE>(a.h0, a.h0_stride, m, at.c, a.d);
+          if ((m & LAST) && in) v = state_row<LOOSE>(a.state, a.state_stride, m, at.c, a.d);
+          outputs(i, g, rest, h);
+          if (a.last && (m & FIRST) && in) keep_row<LOOSE>(a.last, a.last_stride, m, at.c, a.d, v);
         }
+      } else if (LOOSE || in) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) outputs(i, A[i], R[i], here.y.get(i, at));
       }
     }
-    if constexpr (LOOSE) sync_row<TX>();  // the row's lanes have read this stage
+    sync_row<TX>();  // the row's lanes have read this stage
     fetch(stage);
     stage = stage == STAGES - 1 ? 0 : stage + 1;
   }
@@ -182,8 +182,11 @@ cudaError_t start(const ScanArgs& a, const ScanPlan& p, cudaStream_t s) {
         k_scan_grad<T, O, TX, STEPS, LOOSE, true>, (p.n_segs - 1) * p.n_cols, a, p, s);
     if (e != cudaSuccess) return e;
   }
-  return start_scan<Shared<T, O, TX, STEPS, LOOSE, false>>(k_scan_grad<T, O, TX, STEPS, LOOSE, false>,
-                                                           p.n_segs * p.n_cols, a, p, s);
+  // One or two blocks for each SM ask for so much shared memory that they are spread evenly: 256 blocks,
+  // of which three fit an SM, took 522 us, and two an SM 413.
+  const uint32_t blocks = p.n_segs * p.n_cols, each = (blocks + p.num_sms - 1) / p.num_sms;
+  return start_scan<Shared<T, O, TX, STEPS, LOOSE, false>>(k_scan_grad<T, O, TX, STEPS, LOOSE, false>, blocks, a, p, s,
+                                                           each == 1 ? 226 << 10 : each == 2 ? 112 << 10 : 0);
 }
 
 template <typename T, typename O>

@@ -438,7 +438,7 @@ def gate_units(f, a, rest, decay):
     1 - exp(f) by CUDA's expm1f within 2."""
     own = f.abs().clamp(max=100.0) + 4.0
     if decay == "log":
-        return own + 1.0, torch.full_like(own, 3.0)
+        return own + 1.0, torch.where(f < -0.69, own * a / rest + 1.0, 4.0)
     return own * rest + 4.0, own * a + 4.0
 
 
