@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(MARK_THREADS)
   const int64_t id = (int64_t)blockIdx.x * MARK_THREADS + threadIdx.x, all = (int64_t)gridDim.x * MARK_THREADS;
   if (marks)
     for (int64_t t = id; t < a.n; t += all) {
-      int32_t m = NONE;
+      int32_t m;
       if (a.offsets) {
         int64_t lo = -1, hi = a.n_seq + 1;  // offsets[lo] <= t < offsets[hi]
         while (hi - lo > 1) {
@@ -45,9 +45,12 @@ __global__ void __launch_bounds__(MARK_THREADS)
         }
         if (lo >= 0 && lo < a.n_seq)
           m = (int32_t)lo * 4 + (a.offsets[lo] == t ? FIRST : 0) + (a.offsets[lo + 1] == t + 1 ? LAST : 0);
+        else  // before the first or behind the last
+          m = -(int32_t)(lo < 0 && a.offsets[0] < a.n ? a.offsets[0] - t : a.n - t);
       } else {
         const int64_t seq = t / each, pos = t - seq * each, len = a.lengths[seq];
-        if (pos < len) m = (int32_t)seq * 4 + (pos == 0 ? FIRST : 0) + (pos + 1 == len || pos + 1 == each ? LAST : 0);
+        m = pos < len ? (int32_t)seq * 4 + (pos == 0 ? FIRST : 0) + (pos + 1 == len || pos + 1 == each ? LAST : 0)
+                      : -(int32_t)(each - pos);
       }
       marks[t] = m;
     }
@@ -80,7 +83,6 @@ struct Shared {
     Stage<T, TX, STEPS, LOOSE> x, f;
     Marks<TX, STEPS> marks;
   } in[STAGES];
-  char swap[LOOSE ? SCAN_THREADS * V * 4 : 16];
 };
 
 // TAIL: only the pair of each segment but the last, from its last entry on.
@@ -98,13 +100,13 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
   run.clear();
   if constexpr (TAIL) {
     const int32_t m = mark_of(plan, hi);  // of the next segment
-    if (m == NONE || (m & FIRST)) return;  // nothing goes there
+    if (m < 0 || (m & FIRST)) return;  // nothing goes there
     // rows before the last entry do not matter
     if (plan.marks) {
       for (int64_t top = hi; top > lo; top -= SCAN_THREADS) {
         const int64_t r = top - 1 - threadIdx.x;
         const int32_t q = r >= lo ? plan.marks[r] : 0;
-        const int found = __syncthreads_or(q == NONE || (q & FIRST) ? (int)(r - lo) + 1 : 0);
+        const int found = __syncthreads_or(q < 0 || (q & FIRST) ? (int)(r - lo) + 1 : 0);
         if (found) {  // at least one in these rows: start with the lowest of them, the others follow
           lo = top - SCAN_THREADS > lo ? top - SCAN_THREADS : lo;
           break;
@@ -116,16 +118,20 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
     }
   } else if (plan.chained && at.seg > 0) {
     const int32_t m = mark_of(plan, lo);
-    if (m != NONE && !(m & FIRST)) into_segment(sh.j, plan, at, run);
+    if (m >= 0 && !(m & FIRST)) into_segment(sh.j, plan, at, run);
   }
   const int tiles = (int)((hi - lo + At::ROWS - 1) / At::ROWS);
   int64_t row = lo + at.ty * STEPS, ahead = row;
   uint32_t pos = place_of(plan, row);
+  int32_t mark = coming<STEPS, false>(plan, ahead, lo, hi);
   auto fetch = [&](int to) {
-    sh.in[to].f.template fetch<false>(a.f, at, ahead, lo, hi, a.d, a.n);
-    sh.in[to].x.template fetch<false>(a.x, at, ahead, lo, hi, a.d, a.n);
+    if (mark > -STEPS) {  // else none of the rows belongs to a sequence
+      sh.in[to].f.template fetch<false>(a.f, at, ahead, lo, hi, a.d, a.n);
+      sh.in[to].x.template fetch<false>(a.x, at, ahead, lo, hi, a.d, a.n);
+    }
     sh.in[to].marks.template fetch<false>(plan, at, ahead, lo, hi);
     ahead += At::ROWS;
+    mark = coming<STEPS, false>(plan, ahead, lo, hi);
     copies_begun();
   };
 #pragma unroll
@@ -160,13 +166,13 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
       here.marks.template all<false>(plan, at, row, lo, hi, m);
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        if (m[i] == NONE) {
+        if (m[i] < 0) {
           B[i].fill(0.f);
           if (!inside(row + i, lo, hi)) continue;  // no row of the segment: it changes nothing
         } else if ((m[i] & FIRST) && a.state && in) {
-          B[i] = fma_v(A[i], state_row<LOOSE>(a.state, a.state_stride, m[i], at.c, a.d), B[i]);
+          B[i] = fma_v(A[i], state_row<TX, LOOSE>(a.state, a.state_stride, m[i], at.c, a.d), B[i]);
         }
-        mine.then(A[i], B[i], m[i] == NONE || (m[i] & FIRST));
+        mine.then(A[i], B[i], m[i] < 0 || (m[i] & FIRST));
       }
     } else {
 #pragma unroll
@@ -178,20 +184,20 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
     Vec h;
     sh.j.then(t & 1, at, run, h);
     if constexpr (!TAIL) {
-      if (LOOSE || in) {
+      if (in) {
         if (mixed) {
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
             if (!inside(row + i, lo, hi)) break;
-            h = m[i] == NONE || (m[i] & FIRST) ? B[i] : fma_v(A[i], h, B[i]);
-            if (a.last && m[i] != NONE && (m[i] & LAST) && in) keep_row<LOOSE>(a.last, a.last_stride, m[i], at.c, a.d, h);
-            put_row<O, TX, STEPS, LOOSE>(a.out, at, row + i, a.d, h, sh.swap);
+            h = m[i] < 0 || (m[i] & FIRST) ? B[i] : fma_v(A[i], h, B[i]);
+            if (a.last && m[i] >= 0 && (m[i] & LAST) && in) keep_row<TX, LOOSE>(a.last, a.last_stride, m[i], at.c, a.d, h);
+            put_row<O, TX, STEPS, LOOSE>(a.out, at, row + i, a.d, h);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < STEPS; ++i) {
             h = fma_v(A[i], h, B[i]);
-            put_row<O, TX, STEPS, LOOSE>(a.out, at, row + i, a.d, h, sh.swap);
+            put_row<O, TX, STEPS, LOOSE>(a.out, at, row + i, a.d, h);
           }
         }
       }

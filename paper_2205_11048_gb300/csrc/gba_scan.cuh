@@ -9,7 +9,8 @@ namespace gba {
 constexpr int SCAN_THREADS = 128;
 constexpr int V = 4;  // channels of a thread
 
-constexpr int32_t NONE = -1;  // the mark of a row that belongs to no sequence; else sequence * 4 +
+// The mark of a row: sequence * 4 + FIRST + LAST, or where it belongs to none, below zero: minus how
+// many such rows follow one another from it on.
 constexpr int32_t FIRST = 1, LAST = 2;
 
 struct ScanPlan {
@@ -217,13 +218,13 @@ template <int TX, int STEPS>
 struct Spot {
   static constexpr int TY = SCAN_THREADS / TX, ROWS = TY * STEPS, COLS = TX * V;
   uint32_t seg, col;
-  int tx, ty, c;  // c: the thread's first channel
+  int tx, ty, c;  // c: the thread's first channel; the others follow it, or at TX from one another if loose
   __device__ __forceinline__ explicit Spot(const ScanPlan& plan) {
     seg = blockIdx.x / plan.n_cols;
     col = blockIdx.x - seg * plan.n_cols;
     tx = threadIdx.x % TX;
     ty = threadIdx.x / TX;
-    c = (int)col * COLS + tx * V;
+    c = (int)col * COLS + (plan.loose ? tx : tx * V);
   }
 };
 
@@ -238,9 +239,9 @@ __device__ __forceinline__ void sync_row() {
 
 __device__ __forceinline__ bool inside(int64_t row, int64_t lo, int64_t hi) { return row >= lo && row < hi; }
 
-// V channels at STEPS positions for each thread.  LOOSE: rows that do not lie on a vector's
-// boundary come by 4-byte words, neighbouring lanes at neighbouring words, which belong to other
-// lanes of the row: settle() is between.
+// V channels at STEPS positions for each thread.  LOOSE: of rows that do not lie on a vector's
+// boundary a thread has channels that are TX apart, so that neighbouring lanes are still at
+// neighbouring elements.
 template <typename T, int TX, int STEPS, bool LOOSE, bool HALVES = LOOSE && sizeof(T) == 2>
 struct Stage {
   static constexpr int B = V * (int)sizeof(T);
@@ -264,16 +265,13 @@ struct Stage {
           if (inside(BACK ? row - i : row + i, lo, hi)) copy_async<B>(at[i][threadIdx.x], p);
       }
     } else {
-      const int first = s.c - s.tx * V;  // of the lanes that share the row
-      T* to = &at[0][threadIdx.x - s.tx][0];
+      p += s.c;
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i, p += step, to += SCAN_THREADS * V)
+      for (int i = 0; i < STEPS; ++i, p += step)
         if (whole || inside(BACK ? row - i : row + i, lo, hi))
 #pragma unroll
-          for (int k = 0; k < V; ++k) {
-            const int e = k * TX + s.tx;
-            if (first + e < d) copy_async<sizeof(T)>(to + e, p + first + e);
-          }
+          for (int k = 0; k < V; ++k)
+            if (s.c + k * TX < d) copy_async<sizeof(T)>(&at[i][threadIdx.x][k], p + k * TX);
     }
   }
   __device__ __forceinline__ Vec get(int i, const Spot<TX, STEPS>&) const {
@@ -292,7 +290,7 @@ struct Stage<T, TX, STEPS, true, true> {
   template <bool BACK>
   __device__ __forceinline__ void fetch(const Rows& m, const Spot<TX, STEPS>& s, int64_t row, int64_t lo, int64_t hi,
                                         int d, int64_t n) {
-    const int first = s.c - s.tx * V, many = d - first < TX * V ? d - first : TX * V;
+    const int first = s.c - s.tx, many = d - first < TX * V ? d - first : TX * V;
     if (many <= 0) return;
     const uintptr_t base = (uintptr_t)m.p, end = base + ((n - 1) * m.stride + d) * 2;
 #pragma unroll
@@ -319,40 +317,35 @@ struct Stage<T, TX, STEPS, true, true> {
     }
   }
   __device__ __forceinline__ Vec get(int i, const Spot<TX, STEPS>& s) const {
-    const uint32_t* q = &at[i][s.ty][s.tx * 2];
-    const uint32_t a = q[0], b = q[1], c = q[2], shift = at[i][s.ty][WORDS] * 8;
-    const uint32_t w[2] = {__funnelshift_r(a, b, shift), __funnelshift_r(b, c, shift)};
+    // a row that was not fetched left anything there: whatever it is, the elements lie in the row's words
+    const T* q = reinterpret_cast<const T*>(at[i][s.ty]) + (at[i][s.ty][WORDS] >> 1 & 1) + s.tx;
+    T t[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) t[j] = q[j * TX];
     Pack<T, V> k;
-    memcpy(&k, w, sizeof k);
+    memcpy(&k, t, sizeof k);
     return vec_of(k);
   }
 };
 
-// Stores V channels of a row; LOOSE: through the lanes' shared memory.
+// Stores V channels of a row.
 template <typename T, int TX, int STEPS, bool LOOSE>
-__device__ __forceinline__ void put_row(const OutRows& m, const Spot<TX, STEPS>& s, int64_t row, int d,
-                                        const Vec& x, char* swap) {
+__device__ __forceinline__ void put_row(const OutRows& m, const Spot<TX, STEPS>& s, int64_t row, int d, const Vec& x) {
   const Pack<T, V> k = pack_of<T>(x);
-  T* p = static_cast<T*>(m.p) + row * m.stride;
+  T* p = static_cast<T*>(m.p) + row * m.stride + s.c;
   if constexpr (!LOOSE) {
-    k.store(p + s.c);
+    k.store(p);
   } else {
-    T* mine = reinterpret_cast<T*>(swap) + threadIdx.x * V;
-    const int first = s.c - s.tx * V;
-    sync_row<TX>();
-    memcpy(__builtin_assume_aligned(mine, V * sizeof(T)), &k, sizeof k);
-    sync_row<TX>();
-    const T* all = mine - s.tx * V;
+    T t[V];
+    memcpy(t, &k, sizeof t);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int e = j * TX + s.tx;
-      if (first + e < d) p[first + e] = all[e];
-    }
+    for (int j = 0; j < V; ++j)
+      if (s.c + j * TX < d) p[j * TX] = t[j];
   }
 }
 
 // V values of a row of states; they need no alignment where LOOSE.
-template <bool LOOSE>
+template <int TX, bool LOOSE>
 __device__ __forceinline__ Vec state_row(const float* p, int64_t stride, int32_t mark, int c, int d) {
   Vec r;
   r.fill(0.f);
@@ -361,7 +354,7 @@ __device__ __forceinline__ Vec state_row(const float* p, int64_t stride, int32_t
   if constexpr (LOOSE) {
     float v[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = c + j < d ? p[j] : 0.f;
+    for (int j = 0; j < V; ++j) v[j] = c + j * TX < d ? p[j * TX] : 0.f;
     r.set(v);
   } else {
     Pack<float, V> k;
@@ -370,7 +363,7 @@ __device__ __forceinline__ Vec state_row(const float* p, int64_t stride, int32_t
   }
   return r;
 }
-template <bool LOOSE>
+template <int TX, bool LOOSE>
 __device__ __forceinline__ void keep_row(float* p, int64_t stride, int32_t mark, int c, int d, const Vec& x) {
   p += (int64_t)(mark >> 2) * stride + c;
   if constexpr (LOOSE) {
@@ -378,7 +371,7 @@ __device__ __forceinline__ void keep_row(float* p, int64_t stride, int32_t mark,
     x.get(v);
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (c + j < d) p[j] = v[j];
+      if (c + j * TX < d) p[j * TX] = v[j];
   } else {
     pack_of<float>(x).store(p);
   }
@@ -409,9 +402,16 @@ struct Marks {
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int32_t m = at[s.ty][i];
-      special = special || m == NONE || (m & (FIRST | LAST));
+      special = special || m < 0 || (m & (FIRST | LAST));
     }
     return special;
+  }
+  // Whether none of them belongs to a sequence, where it matters: rows that were not fetched.
+  template <bool BACK>
+  __device__ __forceinline__ bool none(const ScanPlan& plan, const Spot<TX, STEPS>& s, int64_t row, int64_t lo,
+                                       int64_t hi) const {
+    const int64_t low = BACK ? row - (STEPS - 1) : row;
+    return plan.marks && inside(low, lo, hi) && at[s.ty][BACK ? STEPS - 1 : 0] <= -STEPS;
   }
   // The marks of all positions, of which those outside the segment are no rows.
   template <bool BACK>
@@ -420,7 +420,7 @@ struct Marks {
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
       const int64_t r = BACK ? row - i : row + i;
-      m[i] = inside(r, lo, hi) ? get(plan, s, i, r) : NONE;
+      m[i] = inside(r, lo, hi) ? get(plan, s, i, r) : -1;
     }
   }
   // The mark of position i, whose row is in the segment.
@@ -441,6 +441,13 @@ __device__ __forceinline__ uint32_t moved(const ScanPlan& plan, uint32_t pos, ui
   if (BACK) return pos >= by ? pos - by : plan.each - 1 - (by - 1 - pos) % plan.each;
   pos += by;
   return pos < plan.each ? pos : pos % plan.each;
+}
+
+// The mark of the lowest row of a stretch that is to be fetched, asked for a turn ahead.
+template <int STEPS, bool BACK>
+__device__ __forceinline__ int32_t coming(const ScanPlan& plan, int64_t row, int64_t lo, int64_t hi) {
+  const int64_t low = BACK ? row - (STEPS - 1) : row;
+  return plan.marks && inside(low, lo, hi) ? plan.marks[low] : 0;
 }
 
 // The mark of one row.

@@ -18,7 +18,6 @@ struct Shared {
     Stage<O, TX, TAIL ? 1 : STEPS, LOOSE> y;
     Marks<TX, STEPS> marks;
   } in[STAGES];
-  char swap[LOOSE ? SCAN_THREADS * V * 4 : 16];
 };
 
 // TAIL: only the pair of each segment but the last, from its last entry on.
@@ -37,12 +36,12 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
   run.clear();
   if constexpr (TAIL) {
     const int32_t m = mark_of(plan, lo - 1);
-    if (m == NONE || (m & LAST)) return;  // nothing goes there
+    if (m < 0 || (m & LAST)) return;  // nothing goes there
     if (plan.marks) {
       for (int64_t low = lo; low < hi; low += SCAN_THREADS) {
         const int64_t r = low + threadIdx.x;
         const int32_t q = r < hi ? plan.marks[r] : 0;
-        if (__syncthreads_or(q == NONE || (q & LAST))) {
+        if (__syncthreads_or(q < 0 || (q & LAST))) {
           hi = low + SCAN_THREADS < hi ? low + SCAN_THREADS : hi;
           break;
         }
@@ -53,21 +52,25 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
     }
   } else if (plan.chained && at.seg > 0) {
     const int32_t m = mark_of(plan, hi - 1);
-    if (m != NONE && !(m & LAST)) into_segment(sh.j, plan, at, run);
+    if (m >= 0 && !(m & LAST)) into_segment(sh.j, plan, at, run);
   }
   const int tiles = (int)((hi - lo + At::ROWS - 1) / At::ROWS);
   int64_t row = hi - 1 - at.ty * STEPS, ahead = row;
   uint32_t pos = place_of(plan, row - (STEPS - 1));
+  int32_t mark = coming<STEPS, true>(plan, ahead, lo, hi);
   auto fetch = [&](int to) {
     auto& s = sh.in[to];
-    s.f.template fetch<true>(a.f, at, ahead, lo, hi, a.d, a.n);
-    s.dy.template fetch<true>(a.dy, at, ahead, lo, hi, a.d, a.n);
-    if constexpr (!TAIL) {
-      if (a.tied) s.x.template fetch<true>(a.x, at, ahead, lo, hi, a.d, a.n);
-      s.y.template fetch<true>(a.y, at, ahead - 1, lo > 0 ? lo - 1 : 0, hi, a.d, a.n);
+    if (mark > -STEPS) {  // else none of the rows belongs to a sequence
+      s.f.template fetch<true>(a.f, at, ahead, lo, hi, a.d, a.n);
+      s.dy.template fetch<true>(a.dy, at, ahead, lo, hi, a.d, a.n);
+      if constexpr (!TAIL) {
+        if (a.tied) s.x.template fetch<true>(a.x, at, ahead, lo, hi, a.d, a.n);
+        s.y.template fetch<true>(a.y, at, ahead - 1, lo > 0 ? lo - 1 : 0, hi, a.d, a.n);
+      }
     }
     s.marks.template fetch<true>(plan, at, ahead, lo, hi);
     ahead -= At::ROWS;
+    mark = coming<STEPS, true>(plan, ahead, lo, hi);
     copies_begun();
   };
 #pragma unroll
@@ -84,16 +87,21 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
     // instructions: unrolled like the others they leave no room in the instruction cache (65,536 x
     // 2,048 in 64 sequences 398 us instead of 364; branches within one unrolled loop, 484).
     const bool mixed = here.marks.template mixed<true>(plan, at, row, lo, hi, pos);
-    if (mixed) {
+    const bool none = mixed && here.marks.template none<true>(plan, at, row, lo, hi);
+    if (none) {
+      Vec zero;
+      zero.fill(0.f);
+      mine.then(zero, zero, true);
+    } else if (mixed) {
 #pragma unroll 1
       for (int i = 0; i < STEPS && row - i >= lo; ++i) {
         const int32_t m = here.marks.get(plan, at, i, row - i);
         Vec g, rest, dy = here.dy.get(i, at);
         gates(a.decay, false, here.f.get(i, at), g, rest);
-        if (m != NONE && (m & LAST) && a.state && in) dy = dy + state_row<LOOSE>(a.state, a.state_stride, m, at.c, a.d);
+        if (m >= 0 && (m & LAST) && a.state && in) dy = dy + state_row<TX, LOOSE>(a.state, a.state_stride, m, at.c, a.d);
         dy = g * dy;
-        if (m == NONE) dy.fill(0.f);
-        mine.then(g, dy, m == NONE || (m & LAST));
+        if (m < 0) dy.fill(0.f);
+        mine.then(g, dy, m < 0 || (m & LAST));
       }
     } else {
       if (a.decay == GBA_DECAY_SIGMOID) {
@@ -139,28 +147,28 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
           for (int j = 0; j < V; ++j) g[j] = f[j] > 0.f ? 0.f : g[j];
           df.set(g);
         }
-        put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, dx, sh.swap);
-        put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, df, sh.swap);
+        put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, dx);
+        put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, df);
       };
       if (mixed) {
 #pragma unroll 1
         for (int i = 0; i < STEPS && row - i >= lo; ++i) {
-          if (!LOOSE && !in) break;
+          if (!in) break;
           const int32_t m = here.marks.get(plan, at, i, row - i);
-          if (m == NONE) {
+          if (m < 0) {
             v.fill(0.f);
-            put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, v, sh.swap);
-            put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, v, sh.swap);
+            put_row<T, TX, STEPS, LOOSE>(a.out, at, row - i, a.d, v);
+            put_row<T, TX, STEPS, LOOSE>(a.df, at, row - i, a.d, v);
             continue;
           }
           Vec g, rest, h = here.y.get(i, at);
           gates(a.decay, a.tied, here.f.get(i, at), g, rest);
-          if ((m & FIRST) && in) h = state_row<LOOSE>(a.h0, a.h0_stride, m, at.c, a.d);
-          if ((m & LAST) && in) v = state_row<LOOSE>(a.state, a.state_stride, m, at.c, a.d);
+          if ((m & FIRST) && in) h = state_row<TX, LOOSE>(a.h0, a.h0_stride, m, at.c, a.d);
+          if ((m & LAST) && in) v = state_row<TX, LOOSE>(a.state, a.state_stride, m, at.c, a.d);
           outputs(i, g, rest, h);
-          if (a.last && (m & FIRST) && in) keep_row<LOOSE>(a.last, a.last_stride, m, at.c, a.d, v);
+          if (a.last && (m & FIRST) && in) keep_row<TX, LOOSE>(a.last, a.last_stride, m, at.c, a.d, v);
         }
-      } else if (LOOSE || in) {
+      } else if (in) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) outputs(i, A[i], R[i], here.y.get(i, at));
       }
