@@ -109,11 +109,61 @@ __device__ __forceinline__ T* at(const OutRows& m, int64_t row) {
   return static_cast<T*>(m.p) + row * m.stride;
 }
 
+// ---- rows in shared memory -----------------------------------------------------------------
+// A thread's pieces of a row, under way while the row before is worked on.  Each thread copies what
+// it reads itself, so nothing is waited for but its own copies.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  if constexpr (BYTES == 2)
+    *static_cast<uint16_t*>(to) = *static_cast<const uint16_t*>(from);
+  else if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(to)), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>  // all but the last N groups of this thread
+__device__ __forceinline__ void copies_done() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <typename T, int V, int P, bool BLOCK>
+struct Rowed {
+  static constexpr int B = V * (int)sizeof(T);
+  T* at;
+  // the next matrix of a stage behind `base`, which moves on
+  __device__ __forceinline__ explicit Rowed(char*& base) {
+    at = reinterpret_cast<T*>(base) + threadIdx.x * V;
+    base += (size_t)blockDim.x * P * B;
+  }
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int d, const Place<BLOCK>& pl) const {
+    const T* p = static_cast<const T*>(m.p) + row * m.stride;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const int c = (k * pl.threads + pl.t) * V;
+      if (c < d) {
+        T* to = at + (size_t)k * blockDim.x * V;
+        if constexpr (B <= 16) {
+          copy_async<B>(to, p + c);
+        } else {
+          copy_async<16>(to, p + c);
+          copy_async<16>(to + 16 / sizeof(T), p + c + 16 / sizeof(T));
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int k, float (&x)[V]) const {
+    Pack<T, V> w;
+    w.load(at + (size_t)k * blockDim.x * V);
+    w.get(x);
+  }
+};
+
 // ---- forward -------------------------------------------------------------------------
-// The mean and the reciprocal deviation of a row in registers; columns past d do not count.
-template <int V, int P, bool BLOCK>
-__device__ __forceinline__ float2 row_stats(const float (&x)[P][V], int32_t kind, const ResNormArgs& a,
-                                            const Place<BLOCK>& at, float* red, int& turn) {
+// The mean and the reciprocal deviation of a row; value(p, x) gives piece p.
+template <int V, int P, bool BLOCK, typename F>
+__device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNormArgs& a, const Place<BLOCK>& at,
+                                            float* red, int& turn) {
   if (kind == GBA_NORM_NONE) return make_float2(0.f, 1.f);
   const float inv = 1.f / (float)a.d;
   float mean = 0.f;
@@ -121,70 +171,97 @@ __device__ __forceinline__ float2 row_stats(const float (&x)[P][V], int32_t kind
     float s[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < P; ++p)
+      if ((p * at.threads + at.t) * V < a.d) {
+        float x[V];
+        value(p, x);
 #pragma unroll
-      for (int j = 0; j < V; ++j) s[0] += x[p][j];  // zeros past d
+        for (int j = 0; j < V; ++j) s[0] += x[j];
+      }
     row_sums<1, BLOCK>(s, red, turn);
     mean = s[0] * inv;
   }
   float q[1] = {0.f};
 #pragma unroll
   for (int p = 0; p < P; ++p)
-    if ((p * at.threads + at.t) * V < a.d)
+    if ((p * at.threads + at.t) * V < a.d) {
+      float x[V];
+      value(p, x);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float e = x[p][j] - mean;
+        const float e = x[j] - mean;
         q[0] = fmaf(e, e, q[0]);
       }
+    }
   row_sums<1, BLOCK>(q, red, turn);
   return make_float2(mean, 1.f / sqrtf(q[0] * inv + a.eps));
 }
 
+// Shared memory of one row of a thread, forward and backward.
+template <typename T, typename R, int V, int P>
+constexpr size_t FORWARD_BYTES = (size_t)V * P * (2 * sizeof(T) + sizeof(R));
+template <typename T, typename R, int V, int P>
+constexpr size_t BACKWARD_BYTES = (size_t)V * P * (3 * sizeof(T) + 2 * sizeof(R));
+
 // B: the most threads of a block that holds one row; 0: a row is a warp's
 template <typename T, typename R, int V, int P, int B>
-__global__ void __launch_bounds__(B ? B : 256, B == 256 ? 3 : 1) k_residual_norm(ResNormArgs a) {
+__global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_norm(ResNormArgs a) {
   constexpr bool BLOCK = B > 0;
+  extern __shared__ __align__(16) char smem[];
   __shared__ float red[2 * 64];
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
-  for (int64_t row = pl.row; row < a.n; row += pl.step) {
-    float x[P][V], z[P][V], g[P][V];
-    Pack<T, V> px[P], pg[P];
-    Pack<R, V> pr[P];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const int c = (p * pl.threads + pl.t) * V;
-      if (c < a.d) {
-        px[p].load(at<T>(a.x, row) + c);
-        if (a.r.p) pr[p].load(at<R>(a.r, row) + c);
-        if (a.g.p) pg[p].load(at<T>(a.g, row) + c);
-      }
+  auto fetch = [&](int64_t row, int stage) {
+    char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
+    if (row < a.n) {
+      Rowed<R, V, P, BLOCK> r(base);
+      Rowed<T, V, P, BLOCK> x(base), g(base);
+      x.fetch(a.x, row, a.d, pl);
+      if (a.r.p) r.fetch(a.r, row, a.d, pl);
+      if (a.g.p) g.fetch(a.g, row, a.d, pl);
     }
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-      const bool in = (p * pl.threads + pl.t) * V < a.d;
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[p][j] = 0.f;
-      if (in) px[p].get(x[p]);
-    }
-    const float2 sx = row_stats<V, P, BLOCK>(x, a.post, a, pl, red, turn);
+    copies_begun();
+  };
+  fetch(pl.row, 0);
+  int stage = 0;
+  for (int64_t row = pl.row; row < a.n; row += pl.step, stage ^= 1) {
+    fetch(row + pl.step, stage ^ 1);
+    copies_done<1>();
+    char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
+    const Rowed<R, V, P, BLOCK> rs(base);
+    const Rowed<T, V, P, BLOCK> xs(base), gs(base);
+    const float2 sx = row_stats<V, P, BLOCK>([&](int p, float (&x)[V]) { xs.get(p, x); }, a.post, a, pl, red, turn);
+    float z[P][V];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * pl.threads + pl.t) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j) z[p][j] = 0.f;
       if (c < a.d) {
-        float w[V], b[V], r[V];
+        float x[V], w[V];
+        xs.get(p, x);
         params<V>(a.post_weight, a.param_type, c, 1.f, w);
-        params<V>(a.post_bias, a.param_type, c, 0.f, b);
-        if (a.g.p) pg[p].get(g[p]);
-        if (a.r.p) pr[p].get(r);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-          float u = fmaf((x[p][j] - sx.x) * sx.y, w[j], b[j]), slope;
-          if (a.gate != GBA_GATE_NONE) u *= gate_of(a.gate, g[p][j], slope);
-          z[p][j] = a.bscale * u;
-          if (a.r.p) z[p][j] = fmaf(a.rscale, r[j], z[p][j]);
+        for (int j = 0; j < V; ++j) z[p][j] = (x[j] - sx.x) * sx.y * w[j];
+        if (a.post_bias) {
+          params<V>(a.post_bias, a.param_type, c, 0.f, w);
+#pragma unroll
+          for (int j = 0; j < V; ++j) z[p][j] += w[j];
+        }
+        if (a.gate != GBA_GATE_NONE) {
+          gs.get(p, x);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            float slope;
+            z[p][j] *= gate_of(a.gate, x[j], slope);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[p][j] *= a.bscale;
+        if (a.r.p) {
+          rs.get(p, x);
+#pragma unroll
+          for (int j = 0; j < V; ++j) z[p][j] = fmaf(a.rscale, x[j], z[p][j]);
         }
         if (a.z.p) {
           Pack<R, V> o;
@@ -193,24 +270,34 @@ __global__ void __launch_bounds__(B ? B : 256, B == 256 ? 3 : 1) k_residual_norm
         }
       }
     }
-    const float2 sz = row_stats<V, P, BLOCK>(z, a.pre, a, pl, red, turn);
+    const float2 sz = row_stats<V, P, BLOCK>(
+        [&](int p, float (&x)[V]) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[j] = z[p][j];
+        },
+        a.pre, a, pl, red, turn);
     if (a.stats && pl.t == 0) a.stats[row] = make_float4(sx.x, sx.y, sz.x, sz.y);
     if (a.y.p)
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
         if (c < a.d) {
-          float w[V], b[V], y[V];
+          float w[V];
           params<V>(a.pre_weight, a.param_type, c, 1.f, w);
-          params<V>(a.pre_bias, a.param_type, c, 0.f, b);
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] = fmaf((z[p][j] - sz.x) * sz.y, w[j], b[j]);
+          for (int j = 0; j < V; ++j) z[p][j] = (z[p][j] - sz.x) * sz.y * w[j];
+          if (a.pre_bias) {
+            params<V>(a.pre_bias, a.param_type, c, 0.f, w);
+#pragma unroll
+            for (int j = 0; j < V; ++j) z[p][j] += w[j];
+          }
           Pack<T, V> o;
-          o.set(y);
+          o.set(z[p]);
           o.store(at<T>(a.y, row) + c);
         }
       }
   }
+  copies_done<0>();
 }
 
 constexpr int WIDE = 1024;
@@ -269,13 +356,6 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_wide(ResNormArgs a) {
 }
 
 // ---- gradient --------------------------------------------------------------------------
-// What one element needs of its row, and gives.
-struct Element {
-  float zh, gy;      // of the norm before the next block
-  float D;           // the gradient of z
-  float xh, e, gu;   // of the block's output
-};
-
 // Writes a block's partial sums of the parameters' gradients (4 x d) to its slot.
 template <int V, int P, bool BLOCK>
 __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& pl, float (&acc)[4][P][V],
@@ -319,8 +399,10 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
 }
 
 template <typename T, typename R, int V, int P, int B>
-__global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_residual_norm_grad(ResNormArgs a, int slots) {
+__global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
+    k_residual_norm_grad(ResNormArgs a, int slots) {
   constexpr bool BLOCK = B > 0;
+  extern __shared__ __align__(16) char smem[];
   __shared__ float red[2 * 64];
   __shared__ float joined[BLOCK ? 1 : 4 * 32 * P * V];
   int turn = 0;
@@ -336,27 +418,34 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_
       for (int j = 0; j < V; ++j) acc[k][p][j] = 0.f;
   float* slot = a.parts + (int64_t)blockIdx.x * slots * 4 * a.d;
   int chain = 0, filled = 0;
+  auto fetch = [&](int64_t row, int stage) {
+    char* base = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
+    if (row < a.n) {
+      Rowed<R, V, P, BLOCK> z(base), dz(base);
+      Rowed<T, V, P, BLOCK> dy(base), x(base), g(base);
+      if (a.dy.p) {
+        dy.fetch(a.dy, row, a.d, pl);
+        z.fetch(a.zin, row, a.d, pl);
+      }
+      if (a.dz.p) dz.fetch(a.dz, row, a.d, pl);
+      x.fetch(a.x, row, a.d, pl);
+      if (a.g.p) g.fetch(a.g, row, a.d, pl);
+    }
+    copies_begun();
+  };
+  fetch(pl.row, 0);
+  int stage = 0;
   // the block's threads go round together: flush() is for all of them
   const int64_t first = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5);
   int64_t row = pl.row;
-  for (int64_t base = first; base < a.n; base += pl.step, row += pl.step) {
+  for (int64_t base = first; base < a.n; base += pl.step, row += pl.step, stage ^= 1) {
+    fetch(row + pl.step, stage ^ 1);
     if (row < a.n) {
-      Pack<T, V> pdy[P], px[P], pg[P];
-      Pack<R, V> pdz[P], pz[P];
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int c = (p * pl.threads + pl.t) * V;
-        if (c < a.d) {
-          if (a.dy.p) {
-            pdy[p].load(at<T>(a.dy, row) + c);
-            pz[p].load(at<R>(a.zin, row) + c);
-          }
-          px[p].load(at<T>(a.x, row) + c);
-          if (a.dz.p) pdz[p].load(at<R>(a.dz, row) + c);
-          if (a.g.p) pg[p].load(at<T>(a.g, row) + c);
-        }
-      }
       const float4 st = a.stats[row];
+      copies_done<1>();
+      char* from = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
+      const Rowed<R, V, P, BLOCK> zs(from), dzs(from);
+      const Rowed<T, V, P, BLOCK> dys(from), xs(from), gs(from);
       float D[P][V];  // the gradient of z; first gy
       float s[2] = {0.f, 0.f};
       if (a.dy.p) {
@@ -364,16 +453,16 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_
         for (int p = 0; p < P; ++p) {
           const int c = (p * pl.threads + pl.t) * V;
           if (c < a.d) {
-            float dy[V], z[V], w[V];
-            pdy[p].get(dy);
-            pz[p].get(z);
+            float z[V], w[V];
+            dys.get(p, D[p]);
+            zs.get(p, z);
             params<V>(a.pre_weight, a.param_type, c, 1.f, w);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               const float zh = (z[j] - st.z) * st.w;
-              acc[2][p][j] = fmaf(dy[j], zh, acc[2][p][j]);
-              acc[3][p][j] += dy[j];
-              D[p][j] = dy[j] * w[j];
+              acc[2][p][j] = fmaf(D[p][j], zh, acc[2][p][j]);
+              acc[3][p][j] += D[p][j];
+              D[p][j] *= w[j];
               s[0] = fmaf(D[p][j], zh, s[0]);
               s[1] += D[p][j];
             }
@@ -384,59 +473,57 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_
         s[1] = a.pre == GBA_NORM_LAYER ? s[1] * inv : 0.f;
       }
       float q[2] = {0.f, 0.f};
-      float gu[P][V];
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
         if (c < a.d) {
-          float x[V], g[V], w[V], b[V], dg[V];
+          float x[V], v[V], w[V];
           if (a.dy.p) {
-            float z[V];
-            pz[p].get(z);
+            zs.get(p, v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] = st.w * (D[p][j] - s[1] - (z[j] - st.z) * st.w * s[0]);
+            for (int j = 0; j < V; ++j) D[p][j] = st.w * (D[p][j] - s[1] - (v[j] - st.z) * st.w * s[0]);
           } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) D[p][j] = 0.f;
           }
           if (a.dz.p) {
-            float dz[V];
-            pdz[p].get(dz);
+            dzs.get(p, v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] += dz[j];
+            for (int j = 0; j < V; ++j) D[p][j] += v[j];
           }
           if (a.dr.p) {
-            float dr[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) dr[j] = a.rscale * D[p][j];
+            for (int j = 0; j < V; ++j) v[j] = a.rscale * D[p][j];
             Pack<R, V> o;
-            o.set(dr);
+            o.set(v);
             o.store(at<R>(a.dr, row) + c);
           }
-          px[p].get(x);
-          if (a.g.p) pg[p].get(g);
+          xs.get(p, x);
           params<V>(a.post_weight, a.param_type, c, 1.f, w);
-          params<V>(a.post_bias, a.param_type, c, 0.f, b);
+#pragma unroll
+          for (int j = 0; j < V; ++j) x[j] = (x[j] - st.x) * st.y, D[p][j] *= a.bscale;
+          if (a.gate != GBA_GATE_NONE) {
+            float b[V];
+            gs.get(p, v);
+            params<V>(a.post_bias, a.param_type, c, 0.f, b);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+              float slope;
+              const float act = gate_of(a.gate, v[j], slope);
+              v[j] = D[p][j] * fmaf(x[j], w[j], b[j]) * slope;
+              D[p][j] *= act;
+            }
+            Pack<T, V> o;
+            o.set(v);
+            o.store(at<T>(a.dg, row) + c);
+          }
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            const float xh = (x[j] - st.x) * st.y;
-            float e = a.bscale * D[p][j];
-            if (a.gate != GBA_GATE_NONE) {
-              float slope;
-              const float act = gate_of(a.gate, g[j], slope);
-              dg[j] = e * fmaf(xh, w[j], b[j]) * slope;
-              e *= act;
-            }
-            acc[0][p][j] = fmaf(e, xh, acc[0][p][j]);
-            acc[1][p][j] += e;
-            gu[p][j] = e * w[j];
-            q[0] = fmaf(gu[p][j], xh, q[0]);
-            q[1] += gu[p][j];
-          }
-          if (a.g.p) {
-            Pack<T, V> o;
-            o.set(dg);
-            o.store(at<T>(a.dg, row) + c);
+            acc[0][p][j] = fmaf(D[p][j], x[j], acc[0][p][j]);
+            acc[1][p][j] += D[p][j];
+            D[p][j] *= w[j];  // gu
+            q[0] = fmaf(D[p][j], x[j], q[0]);
+            q[1] += D[p][j];
           }
         }
       }
@@ -451,12 +538,12 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
         if (c < a.d) {
-          float x[V], dx[V];
-          px[p].get(x);
+          float x[V];
+          xs.get(p, x);
 #pragma unroll
-          for (int j = 0; j < V; ++j) dx[j] = st.y * (gu[p][j] - q[1] - (x[j] - st.x) * st.y * q[0]);
+          for (int j = 0; j < V; ++j) x[j] = st.y * (D[p][j] - q[1] - (x[j] - st.x) * st.y * q[0]);
           Pack<T, V> o;
-          o.set(dx);
+          o.set(x);
           o.store(at<T>(a.dx, row) + c);
         }
       }
@@ -466,6 +553,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2) k_
       chain = 0;
     }
   }
+  copies_done<0>();
   for (; filled < slots; ++filled) flush<V, P, BLOCK>(a, pl, acc, slot + (int64_t)filled * 4 * a.d, joined);
 }
 
@@ -604,41 +692,53 @@ int vector_for(const ResNormArgs& a, int32_t type, int32_t wide, bool grad) {
 Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int num_sms) {
   Shape s{};
   s.v = vector_for(a, type, wide, grad);
-  const int d = a.d;
-  if (grad) {  // eight elements a thread, which four sums of a parameter's gradient go with
+  const int d = a.d, vecs = (d + s.v - 1) / s.v;
+  if (grad || s.v == 1) {  // eight elements a thread; the gradient's go with four sums of parameters' gradients
     s.packs = 8 / s.v;
     s.block = d > 256;
   } else {
-    const int vecs = (d + s.v - 1) / s.v;
-    if (s.v == 1) {
-      s.packs = 8;
-      s.block = d > 256;
-    } else if (vecs <= 128) {
-      s.packs = vecs <= 32 ? 1 : vecs <= 64 ? 2 : 4;
-      s.block = false;
-    } else {
-      s.packs = vecs <= 2048 ? 2 : 4;
-      s.block = true;
-    }
+    s.block = vecs > 128;
+    s.packs = s.block ? 2 : vecs <= 32 ? 1 : vecs <= 64 ? 2 : 4;
   }
   const int each = s.v * s.packs;
   s.threads = s.block ? ((d + each - 1) / each + 31) / 32 * 32 : 32;
   s.rows = s.block ? 1 : 8;
-  unsigned most = 8;  // blocks of an SM
-  if (s.threads > 1024) s.packs = 0, s.threads = WIDE, s.block = true, most = 2;
-  if (s.block) most = std::max(1u, 2048u / s.threads);
-  s.grid = (unsigned)std::min<int64_t>((a.n + s.rows - 1) / s.rows, (int64_t)num_sms * most);
+  // two rows of each block lie in shared memory; wider ones are read again for each sum
+  const size_t b = type_bytes(type), w = type_bytes(wide), room = 226 << 10;
+  const size_t bytes = 2 * (size_t)s.threads * s.rows * each * (grad ? 3 * b + 2 * w : 2 * b + w);
+  size_t most = 2;  // blocks of an SM
+  if (s.threads > 1024 || bytes > room) {
+    s.packs = 0;
+    s.threads = WIDE;
+    s.block = true;
+    s.rows = 1;
+  } else {
+    most = std::max<size_t>(1, std::min(room / (bytes + 5120), (size_t)(grad ? 512 : 1024) / (s.threads * s.rows)));
+  }
+  s.grid = (unsigned)std::min<int64_t>((a.n + s.rows - 1) / s.rows, (int64_t)num_sms * (int64_t)most);
   const int64_t chain = (a.n + (int64_t)s.grid * s.rows - 1) / ((int64_t)s.grid * s.rows);
   s.slots = (int)((chain + CHAIN - 1) / CHAIN);
   return s;
 }
 
+// Two rows of a block's threads lie in shared memory.
+template <typename K, typename... A>
+cudaError_t start(K kernel, unsigned grid, unsigned threads, size_t row_bytes, cudaStream_t s, A... args) {
+  const size_t bytes = 2 * threads * row_bytes;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e != cudaSuccess) return e;
+  return launch_following(kernel, dim3(grid), threads, bytes, s, args...);
+}
+
 template <typename T, typename R, int V, int P>
 cudaError_t forward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  const dim3 grid(h.grid);
-  if (!h.block) return launch_following(k_residual_norm<T, R, V, P, 0>, grid, 32 * h.rows, 0, s, a);
-  if (h.threads <= 256) return launch_following(k_residual_norm<T, R, V, P, 256>, grid, h.threads, 0, s, a);
-  return launch_following(k_residual_norm<T, R, V, P, 1024>, grid, h.threads, 0, s, a);
+  constexpr size_t each = FORWARD_BYTES<T, R, V, P>;
+  if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, h.grid, 32 * h.rows, each, s, a);
+  if constexpr (P <= 2 || V == 1) {  // four vectors a thread are a warp's
+    if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, h.grid, h.threads, each, s, a);
+    return start(k_residual_norm<T, R, V, P, 1024>, h.grid, h.threads, each, s, a);
+  }
+  return cudaErrorInvalidValue;
 }
 
 template <typename T, typename R>
@@ -652,13 +752,11 @@ cudaError_t forward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
 
 template <typename T, typename R, int V, int P>
 cudaError_t backward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  const dim3 grid(h.grid);
-  if (!h.block) return launch_following(k_residual_norm_grad<T, R, V, P, 0>, grid, 32 * h.rows, 0, s, a, h.slots);
-  if (h.threads <= 256)
-    return launch_following(k_residual_norm_grad<T, R, V, P, 256>, grid, h.threads, 0, s, a, h.slots);
-  if (h.threads <= 512)
-    return launch_following(k_residual_norm_grad<T, R, V, P, 512>, grid, h.threads, 0, s, a, h.slots);
-  return launch_following(k_residual_norm_grad<T, R, V, P, 1024>, grid, h.threads, 0, s, a, h.slots);
+  constexpr size_t each = BACKWARD_BYTES<T, R, V, P>;
+  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0>, h.grid, 32 * h.rows, each, s, a, h.slots);
+  if (h.threads <= 256) return start(k_residual_norm_grad<T, R, V, P, 256>, h.grid, h.threads, each, s, a, h.slots);
+  if (h.threads <= 512) return start(k_residual_norm_grad<T, R, V, P, 512>, h.grid, h.threads, each, s, a, h.slots);
+  return start(k_residual_norm_grad<T, R, V, P, 1024>, h.grid, h.threads, each, s, a, h.slots);
 }
 
 template <typename T, typename R>

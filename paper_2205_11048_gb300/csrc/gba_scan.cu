@@ -210,8 +210,11 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
 }
 
 // ---- launches ------------------------------------------------------------------------------
-constexpr int64_t WAVES = 1;    // blocks for each place on the SMs
 constexpr int64_t SHORT = 256;  // rows of a segment of whole sequences, about
+// Segments of ragged batches differ in work, so there are up to four for each place on the SMs, of at
+// least LONG rows: gradient of 65,536 x 2,048, padded, 394 us with one, 352 with four; of 20,003 x 501
+// (float32, packed) 126 with one, 152 with three.
+constexpr int64_t LONG = 512;
 
 struct Shape {
   ScanPlan p;
@@ -243,9 +246,10 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
   const int64_t ty = SCAN_THREADS / p.tx, slots = (int64_t)num_sms * ((grad ? GRAD_BLOCKS : SCAN_BLOCKS) - wide);
   const bool few = (a.n + ty * SCAN_STEPS - 1) / (ty * SCAN_STEPS) * p.n_cols < num_sms;
   p.steps = few && !p.loose && p.tx == 32 ? SCAN_FEW : SCAN_STEPS;
-  const int64_t tile = ty * p.steps, want = std::max<int64_t>(1, WAVES * slots / p.n_cols);
+  const int64_t tile = ty * p.steps, want = std::max<int64_t>(1, slots / p.n_cols);
   int64_t rows = std::max((a.n + want - 1) / want, tile);
   if (s.marks) {
+    rows = std::max(rows / 4, std::min(rows, LONG));
     rows = (rows + tile - 1) / tile * tile;
     p.chained = rows < a.n;
   } else if (a.n > 0) {
