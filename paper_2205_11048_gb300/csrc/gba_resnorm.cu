@@ -112,14 +112,8 @@ __device__ __forceinline__ T* at(const OutRows& m, int64_t row) {
 // ---- rows in shared memory -----------------------------------------------------------------
 // A thread's pieces of a row, under way while the row before is worked on.  Each thread copies what
 // it reads itself, so nothing is waited for but its own copies.
-template <int BYTES>
 __device__ __forceinline__ void copy_async(void* to, const void* from) {
-  if constexpr (BYTES == 2)
-    *static_cast<uint16_t*>(to) = *static_cast<const uint16_t*>(from);
-  else if constexpr (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_addr(to)), "l"(from), "n"(BYTES) : "memory");
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>  // all but the last N groups of this thread
@@ -143,12 +137,8 @@ struct Rowed {
       const int c = (k * pl.threads + pl.t) * V;
       if (c < d) {
         T* to = at + (size_t)k * blockDim.x * V;
-        if constexpr (B <= 16) {
-          copy_async<B>(to, p + c);
-        } else {
-          copy_async<16>(to, p + c);
-          copy_async<16>(to + 16 / sizeof(T), p + c + 16 / sizeof(T));
-        }
+        copy_async(to, p + c);
+        if constexpr (B > 16) copy_async(to + 16 / sizeof(T), p + c + 16 / sizeof(T));
       }
     }
   }
@@ -157,6 +147,22 @@ struct Rowed {
     w.load(at + (size_t)k * blockDim.x * V);
     w.get(x);
   }
+};
+// Single elements stay in registers: there are no asynchronous copies of two bytes, and of four they
+// took longer than loads (float32 5,003 x 1,001 backwards 213 us instead of 140).
+template <typename T, int P, bool BLOCK>
+struct Rowed<T, 1, P, BLOCK> {
+  T v[P];
+  __device__ __forceinline__ explicit Rowed(char*&) {}
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int d, const Place<BLOCK>& pl) {
+    const T* p = static_cast<const T*>(m.p) + row * m.stride;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const int c = k * pl.threads + pl.t;
+      if (c < d) v[k] = p[c];
+    }
+  }
+  __device__ __forceinline__ void get(int k, float (&x)[1]) const { x[0] = to_float(v[k]); }
 };
 
 // ---- forward -------------------------------------------------------------------------
@@ -211,16 +217,22 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
-  auto fetch = [&](int64_t row, int stage) {
-    char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
+  constexpr bool AHEAD = V > 1;
+  auto read = [&](int64_t row, Rowed<T, V, P, BLOCK>& x, Rowed<R, V, P, BLOCK>& r, Rowed<T, V, P, BLOCK>& g) {
     if (row < a.n) {
-      Rowed<R, V, P, BLOCK> r(base);
-      Rowed<T, V, P, BLOCK> x(base), g(base);
       x.fetch(a.x, row, a.d, pl);
       if (a.r.p) r.fetch(a.r, row, a.d, pl);
       if (a.g.p) g.fetch(a.g, row, a.d, pl);
     }
-    copies_begun();
+  };
+  auto fetch = [&](int64_t row, int stage) {
+    if constexpr (AHEAD) {
+      char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
+      Rowed<R, V, P, BLOCK> r(base);
+      Rowed<T, V, P, BLOCK> x(base), g(base);
+      read(row, x, r, g);
+      copies_begun();
+    }
   };
   fetch(pl.row, 0);
   int stage = 0;
@@ -228,8 +240,9 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
     fetch(row + pl.step, stage ^ 1);
     copies_done<1>();
     char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
-    const Rowed<R, V, P, BLOCK> rs(base);
-    const Rowed<T, V, P, BLOCK> xs(base), gs(base);
+    Rowed<R, V, P, BLOCK> rs(base);
+    Rowed<T, V, P, BLOCK> xs(base), gs(base);
+    if constexpr (!AHEAD) read(row, xs, rs, gs);
     const float2 sx = row_stats<V, P, BLOCK>([&](int p, float (&x)[V]) { xs.get(p, x); }, a.post, a, pl, red, turn);
     float z[P][V];
 #pragma unroll
@@ -398,8 +411,9 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
   }
 }
 
-template <typename T, typename R, int V, int P, int B>
-__global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
+// BIAS: the gradients of biases are wanted.  Without their sums three blocks of 256 fit an SM.
+template <typename T, typename R, int V, int P, int B, bool BIAS>
+__global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS || V == 1 ? 2 : 3)
     k_residual_norm_grad(ResNormArgs a, int slots) {
   constexpr bool BLOCK = B > 0;
   extern __shared__ __align__(16) char smem[];
@@ -418,20 +432,26 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
       for (int j = 0; j < V; ++j) acc[k][p][j] = 0.f;
   float* slot = a.parts + (int64_t)blockIdx.x * slots * 4 * a.d;
   int chain = 0, filled = 0;
-  auto fetch = [&](int64_t row, int stage) {
-    char* base = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
-    if (row < a.n) {
-      Rowed<R, V, P, BLOCK> z(base), dz(base);
-      Rowed<T, V, P, BLOCK> dy(base), x(base), g(base);
-      if (a.dy.p) {
-        dy.fetch(a.dy, row, a.d, pl);
-        z.fetch(a.zin, row, a.d, pl);
-      }
-      if (a.dz.p) dz.fetch(a.dz, row, a.d, pl);
-      x.fetch(a.x, row, a.d, pl);
-      if (a.g.p) g.fetch(a.g, row, a.d, pl);
+  constexpr bool AHEAD = V > 1;
+  using Tm = Rowed<T, V, P, BLOCK>;
+  using Rm = Rowed<R, V, P, BLOCK>;
+  auto read = [&](int64_t row, Rm& z, Rm& dz, Tm& dy, Tm& x, Tm& g) {
+    if (a.dy.p) {
+      dy.fetch(a.dy, row, a.d, pl);
+      z.fetch(a.zin, row, a.d, pl);
     }
-    copies_begun();
+    if (a.dz.p) dz.fetch(a.dz, row, a.d, pl);
+    x.fetch(a.x, row, a.d, pl);
+    if (a.g.p) g.fetch(a.g, row, a.d, pl);
+  };
+  auto fetch = [&](int64_t row, int stage) {
+    if constexpr (AHEAD) {
+      char* base = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
+      Rm z(base), dz(base);
+      Tm dy(base), x(base), g(base);
+      if (row < a.n) read(row, z, dz, dy, x, g);
+      copies_begun();
+    }
   };
   fetch(pl.row, 0);
   int stage = 0;
@@ -444,8 +464,9 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
       const float4 st = a.stats[row];
       copies_done<1>();
       char* from = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
-      const Rowed<R, V, P, BLOCK> zs(from), dzs(from);
-      const Rowed<T, V, P, BLOCK> dys(from), xs(from), gs(from);
+      Rm zs(from), dzs(from);
+      Tm dys(from), xs(from), gs(from);
+      if constexpr (!AHEAD) read(row, zs, dzs, dys, xs, gs);
       float D[P][V];  // the gradient of z; first gy
       float s[2] = {0.f, 0.f};
       if (a.dy.p) {
@@ -461,7 +482,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
             for (int j = 0; j < V; ++j) {
               const float zh = (z[j] - st.z) * st.w;
               acc[2][p][j] = fmaf(D[p][j], zh, acc[2][p][j]);
-              acc[3][p][j] += D[p][j];
+              if (BIAS) acc[3][p][j] += D[p][j];
               D[p][j] *= w[j];
               s[0] = fmaf(D[p][j], zh, s[0]);
               s[1] += D[p][j];
@@ -520,7 +541,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : 2)
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             acc[0][p][j] = fmaf(D[p][j], x[j], acc[0][p][j]);
-            acc[1][p][j] += D[p][j];
+            if (BIAS) acc[1][p][j] += D[p][j];
             D[p][j] *= w[j];  // gu
             q[0] = fmaf(D[p][j], x[j], q[0]);
             q[1] += D[p][j];
@@ -705,7 +726,8 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   s.rows = s.block ? 1 : 8;
   // two rows of each block lie in shared memory; wider ones are read again for each sum
   const size_t b = type_bytes(type), w = type_bytes(wide), room = 226 << 10;
-  const size_t bytes = 2 * (size_t)s.threads * s.rows * each * (grad ? 3 * b + 2 * w : 2 * b + w);
+  const size_t bytes = s.v == 1 ? 0 : 2 * (size_t)s.threads * s.rows * each * (grad ? 3 * b + 2 * w : 2 * b + w);
+  const size_t threads = !grad ? 1024 : s.v == 1 || a.sums[1] || a.sums[3] ? 512 : 768;  // that registers are for
   size_t most = 2;  // blocks of an SM
   if (s.threads > 1024 || bytes > room) {
     s.packs = 0;
@@ -713,7 +735,7 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
     s.block = true;
     s.rows = 1;
   } else {
-    most = std::max<size_t>(1, std::min(room / (bytes + 5120), (size_t)(grad ? 512 : 1024) / (s.threads * s.rows)));
+    most = std::max<size_t>(1, std::min(room / (bytes + 5120), threads / (s.threads * s.rows)));
   }
   s.grid = (unsigned)std::min<int64_t>((a.n + s.rows - 1) / s.rows, (int64_t)num_sms * (int64_t)most);
   const int64_t chain = (a.n + (int64_t)s.grid * s.rows - 1) / ((int64_t)s.grid * s.rows);
@@ -732,7 +754,7 @@ cudaError_t start(K kernel, unsigned grid, unsigned threads, size_t row_bytes, c
 
 template <typename T, typename R, int V, int P>
 cudaError_t forward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  constexpr size_t each = FORWARD_BYTES<T, R, V, P>;
+  constexpr size_t each = V == 1 ? 0 : FORWARD_BYTES<T, R, V, P>;
   if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, h.grid, 32 * h.rows, each, s, a);
   if constexpr (P <= 2 || V == 1) {  // four vectors a thread are a warp's
     if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, h.grid, h.threads, each, s, a);
@@ -750,13 +772,21 @@ cudaError_t forward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   return h.packs == 2 ? forward_in<T, R, V, 2>(a, h, s) : forward_in<T, R, V, 4>(a, h, s);
 }
 
+template <typename T, typename R, int V, int P, bool BIAS>
+cudaError_t backward_as(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
+  constexpr size_t each = V == 1 ? 0 : BACKWARD_BYTES<T, R, V, P>;
+  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0, BIAS>, h.grid, 32 * h.rows, each, s, a, h.slots);
+  if (h.threads <= 256)
+    return start(k_residual_norm_grad<T, R, V, P, 256, BIAS>, h.grid, h.threads, each, s, a, h.slots);
+  if (h.threads <= 512)
+    return start(k_residual_norm_grad<T, R, V, P, 512, BIAS>, h.grid, h.threads, each, s, a, h.slots);
+  return start(k_residual_norm_grad<T, R, V, P, 1024, BIAS>, h.grid, h.threads, each, s, a, h.slots);
+}
 template <typename T, typename R, int V, int P>
 cudaError_t backward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  constexpr size_t each = BACKWARD_BYTES<T, R, V, P>;
-  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0>, h.grid, 32 * h.rows, each, s, a, h.slots);
-  if (h.threads <= 256) return start(k_residual_norm_grad<T, R, V, P, 256>, h.grid, h.threads, each, s, a, h.slots);
-  if (h.threads <= 512) return start(k_residual_norm_grad<T, R, V, P, 512>, h.grid, h.threads, each, s, a, h.slots);
-  return start(k_residual_norm_grad<T, R, V, P, 1024>, h.grid, h.threads, each, s, a, h.slots);
+  if constexpr (V > 1)
+    if (!a.sums[1] && !a.sums[3]) return backward_as<T, R, V, P, false>(a, h, s);
+  return backward_as<T, R, V, P, true>(a, h, s);
 }
 
 template <typename T, typename R>
