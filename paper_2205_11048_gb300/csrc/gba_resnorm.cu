@@ -123,14 +123,13 @@ __device__ __forceinline__ void copies_done() {
 
 template <typename T, int V, int P, bool BLOCK>
 struct Rowed {
-  static constexpr int B = V * (int)sizeof(T);
   T* at;
   // the next matrix of a stage behind `base`, which moves on
-  __device__ __forceinline__ explicit Rowed(char*& base) {
+  __device__ __forceinline__ Rowed(char*& base, int, const Place<BLOCK>&) {
     at = reinterpret_cast<T*>(base) + threadIdx.x * V;
-    base += (size_t)blockDim.x * P * B;
+    base += (size_t)blockDim.x * P * V * sizeof(T);
   }
-  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int d, const Place<BLOCK>& pl) const {
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int64_t, int d, const Place<BLOCK>& pl) const {
     const T* p = static_cast<const T*>(m.p) + row * m.stride;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
@@ -138,32 +137,120 @@ struct Rowed {
       if (c < d) {
         T* to = at + (size_t)k * blockDim.x * V;
         copy_async(to, p + c);
-        if constexpr (B > 16) copy_async(to + 16 / sizeof(T), p + c + 16 / sizeof(T));
+        if constexpr (V * sizeof(T) > 16) copy_async(to + 16 / sizeof(T), p + c + 16 / sizeof(T));
       }
     }
   }
-  __device__ __forceinline__ void get(int k, float (&x)[V]) const {
+  __device__ __forceinline__ void aim(const Rows&, int64_t, int, const Place<BLOCK>&) {}
+  __device__ __forceinline__ void get(int k, const Place<BLOCK>&, float (&x)[V]) const {
     Pack<T, V> w;
     w.load(at + (size_t)k * blockDim.x * V);
     w.get(x);
   }
 };
-// Single elements stay in registers: there are no asynchronous copies of two bytes, and of four they
-// took longer than loads (float32 5,003 x 1,001 backwards 213 us instead of 140).
+// Rows that start anywhere: the aligned 16 bytes that hold them, copied by the row's threads together
+// (so a barrier is needed before they are read, and one before they are filled again).  By single
+// elements bf16 32,768 x 2,049 took 1,715 us backwards.
 template <typename T, int P, bool BLOCK>
 struct Rowed<T, 1, P, BLOCK> {
-  T v[P];
-  __device__ __forceinline__ explicit Rowed(char*&) {}
-  __device__ __forceinline__ void fetch(const Rows& m, int64_t row, int d, const Place<BLOCK>& pl) {
-    const T* p = static_cast<const T*>(m.p) + row * m.stride;
+  char* at;
+  const T* row;  // the row's first element
+  __host__ __device__ static constexpr size_t bytes(int d) { return ((size_t)d * sizeof(T) + 30) / 16 * 16; }
+  __device__ __forceinline__ Rowed(char*& base, int d, const Place<BLOCK>&) {
+    at = base + (BLOCK ? 0 : (threadIdx.x >> 5) * bytes(d));
+    base += (BLOCK ? 1 : blockDim.x >> 5) * bytes(d);
+  }
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t r, int64_t n, int d, const Place<BLOCK>& pl) const {
+    const uintptr_t lo = (uintptr_t)m.p, hi = lo + ((n - 1) * m.stride + d) * (int64_t)sizeof(T);  // of the matrix
+    const uintptr_t from = lo + r * m.stride * (int64_t)sizeof(T), to = from + (uintptr_t)d * sizeof(T);
+    for (uintptr_t p = (from & ~(uintptr_t)15) + pl.t * 16; p < to; p += pl.threads * 16) {
+      char* q = at + (p - (from & ~(uintptr_t)15));
+      if (p >= lo && p + 16 <= hi) {
+        copy_async(q, (const void*)p);
+      } else {
+        for (int b = 0; b < 16; b += (int)sizeof(T))
+          if (p + b >= lo && p + b < hi) *reinterpret_cast<T*>(q + b) = *(const T*)(p + b);
+      }
+    }
+  }
+  __device__ __forceinline__ void aim(const Rows& m, int64_t r, int, const Place<BLOCK>&) {
+    row = reinterpret_cast<const T*>(at + ((uintptr_t)(static_cast<const T*>(m.p) + r * m.stride) & 15));
+  }
+  __device__ __forceinline__ void get(int k, const Place<BLOCK>& pl, float (&x)[1]) const {
+    x[0] = to_float(row[k * pl.threads + pl.t]);
+  }
+};
+
+// Single float32 elements stay in registers: a warp's are 128 bytes as they lie (5,003 x 1,001 44 us
+// against 66 through shared memory).
+template <int P, bool BLOCK>
+struct Rowed<float, 1, P, BLOCK> {
+  float v[P];
+  __host__ __device__ static constexpr size_t bytes(int) { return 0; }
+  __device__ __forceinline__ Rowed(char*&, int, const Place<BLOCK>&) {}
+  __device__ __forceinline__ void fetch(const Rows&, int64_t, int64_t, int, const Place<BLOCK>&) const {}
+  __device__ __forceinline__ void aim(const Rows& m, int64_t row, int d, const Place<BLOCK>& pl) {
+    if (!m.p) return;
+    const float* p = static_cast<const float*>(m.p) + row * m.stride;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
       const int c = k * pl.threads + pl.t;
       if (c < d) v[k] = p[c];
     }
   }
-  __device__ __forceinline__ void get(int k, float (&x)[1]) const { x[0] = to_float(v[k]); }
+  __device__ __forceinline__ void get(int k, const Place<BLOCK>&, float (&x)[1]) const { x[0] = v[k]; }
 };
+
+// A thread's parameters.  Where it has single elements it keeps them as floats in shared memory, in
+// `most` arrays of P for each thread: their types are not asked for row by row.
+template <int V, int P, bool BLOCK>
+struct Params {
+  const ResNormArgs& a;
+  const float* held;
+  __device__ __forceinline__ Params(const ResNormArgs& args, char* at, const Place<BLOCK>& pl) : a(args) {
+    if constexpr (V == 1) {
+      float* to = reinterpret_cast<float*>(at) + threadIdx.x;
+      held = to;
+      for (int k = 0; k < 4; ++k)
+        for (int p = 0; p < P; ++p) {
+          const int c = p * pl.threads + pl.t;
+          float w[1] = {0.f};
+          if (c < a.d) params<1>(of(k), a.param_type, c, k & 1 ? 0.f : 1.f, w);
+          to[(k * P + p) * blockDim.x] = w[0];
+        }
+    }
+  }
+  __device__ __forceinline__ const void* of(int k) const {
+    return k == 0 ? a.post_weight : k == 1 ? a.post_bias : k == 2 ? a.pre_weight : a.pre_bias;
+  }
+  // piece p, from column c on, of the post weight and bias and the pre weight and bias
+  __device__ __forceinline__ void get(int k, int p, int c, float (&w)[V]) const {
+    if constexpr (V == 1)
+      w[0] = held[(k * P + p) * blockDim.x];
+    else
+      params<V>(of(k), a.param_type, c, k & 1 ? 0.f : 1.f, w);
+  }
+};
+template <int V, int P>
+constexpr size_t HELD_BYTES = V == 1 ? 4 * P * sizeof(float) : 0;  // of a thread
+
+// The threads of a row that read what others of them copied.
+template <typename T, int V, bool BLOCK>
+__device__ __forceinline__ void sync_row() {
+  if constexpr (V == 1 && sizeof(T) == 2) {
+    if constexpr (BLOCK)
+      __syncthreads();
+    else
+      __syncwarp();
+  }
+}
+
+// Shared memory of a block's rows: nt matrices of T and nr of R.
+template <typename T, typename R, int V, int P>
+__host__ __device__ constexpr size_t stage_bytes(int nt, int nr, int d, int threads, bool block) {
+  if (V == 1) return (block ? 1 : threads / 32) * (nt * Rowed<T, 1, P, true>::bytes(d) + nr * Rowed<R, 1, P, true>::bytes(d));
+  return (size_t)threads * V * P * (nt * sizeof(T) + nr * sizeof(R));
+}
 
 // ---- forward -------------------------------------------------------------------------
 // The mean and the reciprocal deviation of a row; value(p, x) gives piece p.
@@ -202,12 +289,6 @@ __device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNorm
   return make_float2(mean, 1.f / sqrtf(q[0] * inv + a.eps));
 }
 
-// Shared memory of one row of a thread, forward and backward.
-template <typename T, typename R, int V, int P>
-constexpr size_t FORWARD_BYTES = (size_t)V * P * (2 * sizeof(T) + sizeof(R));
-template <typename T, typename R, int V, int P>
-constexpr size_t BACKWARD_BYTES = (size_t)V * P * (3 * sizeof(T) + 2 * sizeof(R));
-
 // B: the most threads of a block that holds one row; 0: a row is a warp's
 template <typename T, typename R, int V, int P, int B>
 __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_norm(ResNormArgs a) {
@@ -217,33 +298,33 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
-  constexpr bool AHEAD = V > 1;
-  auto read = [&](int64_t row, Rowed<T, V, P, BLOCK>& x, Rowed<R, V, P, BLOCK>& r, Rowed<T, V, P, BLOCK>& g) {
-    if (row < a.n) {
-      x.fetch(a.x, row, a.d, pl);
-      if (a.r.p) r.fetch(a.r, row, a.d, pl);
-      if (a.g.p) g.fetch(a.g, row, a.d, pl);
-    }
-  };
+  using Tm = Rowed<T, V, P, BLOCK>;
+  using Rm = Rowed<R, V, P, BLOCK>;
+  const size_t bytes = stage_bytes<T, R, V, P>(2, 1, a.d, blockDim.x, BLOCK);
   auto fetch = [&](int64_t row, int stage) {
-    if constexpr (AHEAD) {
-      char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
-      Rowed<R, V, P, BLOCK> r(base);
-      Rowed<T, V, P, BLOCK> x(base), g(base);
-      read(row, x, r, g);
-      copies_begun();
+    char* base = smem + stage * bytes;
+    const Rm r(base, a.d, pl);
+    const Tm x(base, a.d, pl), g(base, a.d, pl);
+    if (row < a.n) {
+      x.fetch(a.x, row, a.n, a.d, pl);
+      if (a.r.p) r.fetch(a.r, row, a.n, a.d, pl);
+      if (a.g.p) g.fetch(a.g, row, a.n, a.d, pl);
     }
+    copies_begun();
   };
+  const Params<V, P, BLOCK> par(a, smem + 2 * bytes, pl);
   fetch(pl.row, 0);
   int stage = 0;
   for (int64_t row = pl.row; row < a.n; row += pl.step, stage ^= 1) {
+    sync_row<T, V, BLOCK>();
     fetch(row + pl.step, stage ^ 1);
     copies_done<1>();
-    char* base = smem + (size_t)stage * blockDim.x * FORWARD_BYTES<T, R, V, P>;
-    Rowed<R, V, P, BLOCK> rs(base);
-    Rowed<T, V, P, BLOCK> xs(base), gs(base);
-    if constexpr (!AHEAD) read(row, xs, rs, gs);
-    const float2 sx = row_stats<V, P, BLOCK>([&](int p, float (&x)[V]) { xs.get(p, x); }, a.post, a, pl, red, turn);
+    sync_row<T, V, BLOCK>();
+    char* base = smem + stage * bytes;
+    Rm rs(base, a.d, pl);
+    Tm xs(base, a.d, pl), gs(base, a.d, pl);
+    xs.aim(a.x, row, a.d, pl), rs.aim(a.r, row, a.d, pl), gs.aim(a.g, row, a.d, pl);
+    const float2 sx = row_stats<V, P, BLOCK>([&](int p, float (&x)[V]) { xs.get(p, pl, x); }, a.post, a, pl, red, turn);
     float z[P][V];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
@@ -252,17 +333,17 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
       for (int j = 0; j < V; ++j) z[p][j] = 0.f;
       if (c < a.d) {
         float x[V], w[V];
-        xs.get(p, x);
-        params<V>(a.post_weight, a.param_type, c, 1.f, w);
+        xs.get(p, pl, x);
+        par.get(0, p, c, w);
 #pragma unroll
         for (int j = 0; j < V; ++j) z[p][j] = (x[j] - sx.x) * sx.y * w[j];
         if (a.post_bias) {
-          params<V>(a.post_bias, a.param_type, c, 0.f, w);
+          par.get(1, p, c, w);
 #pragma unroll
           for (int j = 0; j < V; ++j) z[p][j] += w[j];
         }
         if (a.gate != GBA_GATE_NONE) {
-          gs.get(p, x);
+          gs.get(p, pl, x);
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             float slope;
@@ -272,7 +353,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
 #pragma unroll
         for (int j = 0; j < V; ++j) z[p][j] *= a.bscale;
         if (a.r.p) {
-          rs.get(p, x);
+          rs.get(p, pl, x);
 #pragma unroll
           for (int j = 0; j < V; ++j) z[p][j] = fmaf(a.rscale, x[j], z[p][j]);
         }
@@ -296,11 +377,11 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
         const int c = (p * pl.threads + pl.t) * V;
         if (c < a.d) {
           float w[V];
-          params<V>(a.pre_weight, a.param_type, c, 1.f, w);
+          par.get(2, p, c, w);
 #pragma unroll
           for (int j = 0; j < V; ++j) z[p][j] = (z[p][j] - sz.x) * sz.y * w[j];
           if (a.pre_bias) {
-            params<V>(a.pre_bias, a.param_type, c, 0.f, w);
+            par.get(3, p, c, w);
 #pragma unroll
             for (int j = 0; j < V; ++j) z[p][j] += w[j];
           }
@@ -432,41 +513,42 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
       for (int j = 0; j < V; ++j) acc[k][p][j] = 0.f;
   float* slot = a.parts + (int64_t)blockIdx.x * slots * 4 * a.d;
   int chain = 0, filled = 0;
-  constexpr bool AHEAD = V > 1;
   using Tm = Rowed<T, V, P, BLOCK>;
   using Rm = Rowed<R, V, P, BLOCK>;
-  auto read = [&](int64_t row, Rm& z, Rm& dz, Tm& dy, Tm& x, Tm& g) {
-    if (a.dy.p) {
-      dy.fetch(a.dy, row, a.d, pl);
-      z.fetch(a.zin, row, a.d, pl);
-    }
-    if (a.dz.p) dz.fetch(a.dz, row, a.d, pl);
-    x.fetch(a.x, row, a.d, pl);
-    if (a.g.p) g.fetch(a.g, row, a.d, pl);
-  };
+  const size_t bytes = stage_bytes<T, R, V, P>(3, 2, a.d, blockDim.x, BLOCK);
   auto fetch = [&](int64_t row, int stage) {
-    if constexpr (AHEAD) {
-      char* base = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
-      Rm z(base), dz(base);
-      Tm dy(base), x(base), g(base);
-      if (row < a.n) read(row, z, dz, dy, x, g);
-      copies_begun();
+    char* base = smem + stage * bytes;
+    const Rm z(base, a.d, pl), dz(base, a.d, pl);
+    const Tm dy(base, a.d, pl), x(base, a.d, pl), g(base, a.d, pl);
+    if (row < a.n) {
+      if (a.dy.p) {
+        dy.fetch(a.dy, row, a.n, a.d, pl);
+        z.fetch(a.zin, row, a.n, a.d, pl);
+      }
+      if (a.dz.p) dz.fetch(a.dz, row, a.n, a.d, pl);
+      x.fetch(a.x, row, a.n, a.d, pl);
+      if (a.g.p) g.fetch(a.g, row, a.n, a.d, pl);
     }
+    copies_begun();
   };
+  const Params<V, P, BLOCK> par(a, smem + 2 * bytes, pl);
   fetch(pl.row, 0);
   int stage = 0;
   // the block's threads go round together: flush() is for all of them
   const int64_t first = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5);
   int64_t row = pl.row;
   for (int64_t base = first; base < a.n; base += pl.step, row += pl.step, stage ^= 1) {
+    sync_row<T, V, BLOCK>();
     fetch(row + pl.step, stage ^ 1);
     if (row < a.n) {
       const float4 st = a.stats[row];
       copies_done<1>();
-      char* from = smem + (size_t)stage * blockDim.x * BACKWARD_BYTES<T, R, V, P>;
-      Rm zs(from), dzs(from);
-      Tm dys(from), xs(from), gs(from);
-      if constexpr (!AHEAD) read(row, zs, dzs, dys, xs, gs);
+      sync_row<T, V, BLOCK>();
+      char* from = smem + stage * bytes;
+      Rm zs(from, a.d, pl), dzs(from, a.d, pl);
+      Tm dys(from, a.d, pl), xs(from, a.d, pl), gs(from, a.d, pl);
+      zs.aim(a.zin, row, a.d, pl), dzs.aim(a.dz, row, a.d, pl);
+      dys.aim(a.dy, row, a.d, pl), xs.aim(a.x, row, a.d, pl), gs.aim(a.g, row, a.d, pl);
       float D[P][V];  // the gradient of z; first gy
       float s[2] = {0.f, 0.f};
       if (a.dy.p) {
@@ -475,9 +557,9 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
           const int c = (p * pl.threads + pl.t) * V;
           if (c < a.d) {
             float z[V], w[V];
-            dys.get(p, D[p]);
-            zs.get(p, z);
-            params<V>(a.pre_weight, a.param_type, c, 1.f, w);
+            dys.get(p, pl, D[p]);
+            zs.get(p, pl, z);
+            par.get(2, p, c, w);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               const float zh = (z[j] - st.z) * st.w;
@@ -500,7 +582,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
         if (c < a.d) {
           float x[V], v[V], w[V];
           if (a.dy.p) {
-            zs.get(p, v);
+            zs.get(p, pl, v);
 #pragma unroll
             for (int j = 0; j < V; ++j) D[p][j] = st.w * (D[p][j] - s[1] - (v[j] - st.z) * st.w * s[0]);
           } else {
@@ -508,7 +590,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
             for (int j = 0; j < V; ++j) D[p][j] = 0.f;
           }
           if (a.dz.p) {
-            dzs.get(p, v);
+            dzs.get(p, pl, v);
 #pragma unroll
             for (int j = 0; j < V; ++j) D[p][j] += v[j];
           }
@@ -519,14 +601,14 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
             o.set(v);
             o.store(at<R>(a.dr, row) + c);
           }
-          xs.get(p, x);
-          params<V>(a.post_weight, a.param_type, c, 1.f, w);
+          xs.get(p, pl, x);
+          par.get(0, p, c, w);
 #pragma unroll
           for (int j = 0; j < V; ++j) x[j] = (x[j] - st.x) * st.y, D[p][j] *= a.bscale;
           if (a.gate != GBA_GATE_NONE) {
             float b[V];
-            gs.get(p, v);
-            params<V>(a.post_bias, a.param_type, c, 0.f, b);
+            gs.get(p, pl, v);
+            par.get(1, p, c, b);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               float slope;
@@ -560,7 +642,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
         const int c = (p * pl.threads + pl.t) * V;
         if (c < a.d) {
           float x[V];
-          xs.get(p, x);
+          xs.get(p, pl, x);
 #pragma unroll
           for (int j = 0; j < V; ++j) x[j] = st.y * (D[p][j] - q[1] - (x[j] - st.x) * st.y * q[0]);
           Pack<T, V> o;
@@ -726,8 +808,15 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   s.rows = s.block ? 1 : 8;
   // two rows of each block lie in shared memory; wider ones are read again for each sum
   const size_t b = type_bytes(type), w = type_bytes(wide), room = 226 << 10;
-  const size_t bytes = s.v == 1 ? 0 : 2 * (size_t)s.threads * s.rows * each * (grad ? 3 * b + 2 * w : 2 * b + w);
-  const size_t threads = !grad ? 1024 : s.v == 1 || a.sums[1] || a.sums[3] ? 512 : 768;  // that registers are for
+  const size_t nt = grad ? 3 : 2, nr = grad ? 2 : 1;
+  size_t bytes = 2 * (size_t)s.threads * s.rows * each * (nt * b + nr * w);
+  if (s.v == 1) {  // those of 16 bits, and the parameters
+    bytes = b == 2 ? 2 * s.rows * nt * ((size_t)d * 2 + 32) : 0;
+    if (w == 2) bytes += 2 * s.rows * nr * ((size_t)d * 2 + 32);
+    bytes += (size_t)s.threads * s.rows * HELD_BYTES<1, 8>;
+  }
+  // that registers are for
+  const size_t threads = !grad ? 1024 : s.v == 1 || a.sums[1] || a.sums[3] ? 576 : 768;
   size_t most = 2;  // blocks of an SM
   if (s.threads > 1024 || bytes > room) {
     s.packs = 0;
@@ -743,22 +832,22 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   return s;
 }
 
-// Two rows of a block's threads lie in shared memory.
+// Two rows of each of a block's lie in shared memory.
 template <typename K, typename... A>
-cudaError_t start(K kernel, unsigned grid, unsigned threads, size_t row_bytes, cudaStream_t s, A... args) {
-  const size_t bytes = 2 * threads * row_bytes;
+cudaError_t start(K kernel, const Shape& h, size_t stage, size_t held, cudaStream_t s, A... args) {
+  const size_t bytes = 2 * stage + held * h.threads * h.rows;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   if (e != cudaSuccess) return e;
-  return launch_following(kernel, dim3(grid), threads, bytes, s, args...);
+  return launch_following(kernel, dim3(h.grid), h.threads * h.rows, bytes, s, args...);
 }
 
 template <typename T, typename R, int V, int P>
 cudaError_t forward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  constexpr size_t each = V == 1 ? 0 : FORWARD_BYTES<T, R, V, P>;
-  if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, h.grid, 32 * h.rows, each, s, a);
+  const size_t stage = stage_bytes<T, R, V, P>(2, 1, a.d, h.threads * h.rows, h.block);
+  if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, h, stage, HELD_BYTES<V, P>, s, a);
   if constexpr (P <= 2 || V == 1) {  // four vectors a thread are a warp's
-    if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, h.grid, h.threads, each, s, a);
-    return start(k_residual_norm<T, R, V, P, 1024>, h.grid, h.threads, each, s, a);
+    if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, h, stage, HELD_BYTES<V, P>, s, a);
+    return start(k_residual_norm<T, R, V, P, 1024>, h, stage, HELD_BYTES<V, P>, s, a);
   }
   return cudaErrorInvalidValue;
 }
@@ -774,13 +863,11 @@ cudaError_t forward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
 
 template <typename T, typename R, int V, int P, bool BIAS>
 cudaError_t backward_as(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  constexpr size_t each = V == 1 ? 0 : BACKWARD_BYTES<T, R, V, P>;
-  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0, BIAS>, h.grid, 32 * h.rows, each, s, a, h.slots);
-  if (h.threads <= 256)
-    return start(k_residual_norm_grad<T, R, V, P, 256, BIAS>, h.grid, h.threads, each, s, a, h.slots);
-  if (h.threads <= 512)
-    return start(k_residual_norm_grad<T, R, V, P, 512, BIAS>, h.grid, h.threads, each, s, a, h.slots);
-  return start(k_residual_norm_grad<T, R, V, P, 1024, BIAS>, h.grid, h.threads, each, s, a, h.slots);
+  const size_t stage = stage_bytes<T, R, V, P>(3, 2, a.d, h.threads * h.rows, h.block);
+  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
+  if (h.threads <= 256) return start(k_residual_norm_grad<T, R, V, P, 256, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
+  if (h.threads <= 512) return start(k_residual_norm_grad<T, R, V, P, 512, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
+  return start(k_residual_norm_grad<T, R, V, P, 1024, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
 }
 template <typename T, typename R, int V, int P>
 cudaError_t backward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
