@@ -155,12 +155,13 @@ template <typename T, int P, bool BLOCK>
 struct Rowed<T, 1, P, BLOCK> {
   char* at;
   const T* row;  // the row's first element
+  int d;
   __host__ __device__ static constexpr size_t bytes(int d) { return ((size_t)d * sizeof(T) + 30) / 16 * 16; }
-  __device__ __forceinline__ Rowed(char*& base, int d, const Place<BLOCK>&) {
+  __device__ __forceinline__ Rowed(char*& base, int cols, const Place<BLOCK>&) : d(cols) {
     at = base + (BLOCK ? 0 : (threadIdx.x >> 5) * bytes(d));
     base += (BLOCK ? 1 : blockDim.x >> 5) * bytes(d);
   }
-  __device__ __forceinline__ void fetch(const Rows& m, int64_t r, int64_t n, int d, const Place<BLOCK>& pl) const {
+  __device__ __forceinline__ void fetch(const Rows& m, int64_t r, int64_t n, int, const Place<BLOCK>& pl) const {
     const uintptr_t lo = (uintptr_t)m.p, hi = lo + ((n - 1) * m.stride + d) * (int64_t)sizeof(T);  // of the matrix
     const uintptr_t from = lo + r * m.stride * (int64_t)sizeof(T), to = from + (uintptr_t)d * sizeof(T);
     for (uintptr_t p = (from & ~(uintptr_t)15) + pl.t * 16; p < to; p += pl.threads * 16) {
@@ -177,7 +178,8 @@ struct Rowed<T, 1, P, BLOCK> {
     row = reinterpret_cast<const T*>(at + ((uintptr_t)(static_cast<const T*>(m.p) + r * m.stride) & 15));
   }
   __device__ __forceinline__ void get(int k, const Place<BLOCK>& pl, float (&x)[1]) const {
-    x[0] = to_float(row[k * pl.threads + pl.t]);
+    const int c = k * pl.threads + pl.t;
+    x[0] = c < d ? to_float(row[c]) : 0.f;
   }
 };
 
@@ -195,7 +197,7 @@ struct Rowed<float, 1, P, BLOCK> {
 #pragma unroll
     for (int k = 0; k < P; ++k) {
       const int c = k * pl.threads + pl.t;
-      if (c < d) v[k] = p[c];
+      v[k] = c < d ? p[c] : 0.f;
     }
   }
   __device__ __forceinline__ void get(int k, const Place<BLOCK>&, float (&x)[1]) const { x[0] = v[k]; }
@@ -234,6 +236,9 @@ struct Params {
 template <int V, int P>
 constexpr size_t HELD_BYTES = V == 1 ? 4 * P * sizeof(float) : 0;  // of a thread
 
+// Where a thread has single elements it goes through all its P, those past the row as zeros: a branch
+// at each would let it work on one at a time.
+
 // The threads of a row that read what others of them copied.
 template <typename T, int V, bool BLOCK>
 __device__ __forceinline__ void sync_row() {
@@ -264,7 +269,7 @@ __device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNorm
     float s[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if ((p * at.threads + at.t) * V < a.d) {
+      if (V == 1 || (p * at.threads + at.t) * V < a.d) {
         float x[V];
         value(p, x);
 #pragma unroll
@@ -276,12 +281,12 @@ __device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNorm
   float q[1] = {0.f};
 #pragma unroll
   for (int p = 0; p < P; ++p)
-    if ((p * at.threads + at.t) * V < a.d) {
+    if (V == 1 || (p * at.threads + at.t) * V < a.d) {
       float x[V];
       value(p, x);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float e = x[j] - mean;
+        const float e = V > 1 || p * at.threads + at.t < a.d ? x[j] - mean : 0.f;
         q[0] = fmaf(e, e, q[0]);
       }
     }
@@ -331,7 +336,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
       const int c = (p * pl.threads + pl.t) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j) z[p][j] = 0.f;
-      if (c < a.d) {
+      if (V == 1 || c < a.d) {
         float x[V], w[V];
         xs.get(p, pl, x);
         par.get(0, p, c, w);
@@ -360,7 +365,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
         if (a.z.p) {
           Pack<R, V> o;
           o.set(z[p]);
-          o.store(at<R>(a.z, row) + c);
+          if (V > 1 || c < a.d) o.store(at<R>(a.z, row) + c);
         }
       }
     }
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
-        if (c < a.d) {
+        if (V == 1 || c < a.d) {
           float w[V];
           par.get(2, p, c, w);
 #pragma unroll
@@ -387,7 +392,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
           }
           Pack<T, V> o;
           o.set(z[p]);
-          o.store(at<T>(a.y, row) + c);
+          if (V > 1 || c < a.d) o.store(at<T>(a.y, row) + c);
         }
       }
   }
@@ -555,7 +560,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const int c = (p * pl.threads + pl.t) * V;
-          if (c < a.d) {
+          if (V == 1 || c < a.d) {
             float z[V], w[V];
             dys.get(p, pl, D[p]);
             zs.get(p, pl, z);
@@ -579,12 +584,12 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
-        if (c < a.d) {
+        if (V == 1 || c < a.d) {
           float x[V], v[V], w[V];
           if (a.dy.p) {
             zs.get(p, pl, v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] = st.w * (D[p][j] - s[1] - (v[j] - st.z) * st.w * s[0]);
+            for (int j = 0; j < V; ++j) D[p][j] = V > 1 || c < a.d ? st.w * (D[p][j] - s[1] - (v[j] - st.z) * st.w * s[0]) : 0.f;
           } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) D[p][j] = 0.f;
@@ -599,7 +604,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
             for (int j = 0; j < V; ++j) v[j] = a.rscale * D[p][j];
             Pack<R, V> o;
             o.set(v);
-            o.store(at<R>(a.dr, row) + c);
+            if (V > 1 || c < a.d) o.store(at<R>(a.dr, row) + c);
           }
           xs.get(p, pl, x);
           par.get(0, p, c, w);
@@ -618,7 +623,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
             }
             Pack<T, V> o;
             o.set(v);
-            o.store(at<T>(a.dg, row) + c);
+            if (V > 1 || c < a.d) o.store(at<T>(a.dg, row) + c);
           }
 #pragma unroll
           for (int j = 0; j < V; ++j) {
@@ -640,14 +645,14 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
-        if (c < a.d) {
+        if (V == 1 || c < a.d) {
           float x[V];
           xs.get(p, pl, x);
 #pragma unroll
           for (int j = 0; j < V; ++j) x[j] = st.y * (D[p][j] - q[1] - (x[j] - st.x) * st.y * q[0]);
           Pack<T, V> o;
           o.set(x);
-          o.store(at<T>(a.dx, row) + c);
+          if (V > 1 || c < a.d) o.store(at<T>(a.dx, row) + c);
         }
       }
     }
