@@ -45,17 +45,11 @@ struct PartList {
   Part part[CAP];
 };
 
-template <int CAP>
-__device__ __forceinline__ int part_of(const PartList<CAP>& l, uint32_t piece) {
-  int lo = 0, hi = l.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (l.part[mid].first <= piece)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
+// The part that a piece belongs to, from that of an earlier one on: a block's pieces ascend, so all of
+// them together pass each part once.
+template <typename L>
+__device__ __forceinline__ void advance(const L& l, uint32_t piece, int& i) {
+  while (i + 1 < l.count && l.part[i + 1].first <= piece) ++i;
 }
 
 // Eight elements of a type known at run time, as they lie in memory; `n` of them exist, at
@@ -124,6 +118,28 @@ __device__ __forceinline__ float m_of(uint32_t code) {
   return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
 }
 __device__ __forceinline__ float v_of(uint32_t code) { return code ? __uint_as_float((code + 768u) << 20) : 0.f; }
+// Eight codes at once.
+__device__ __forceinline__ void m_of_8(uint2 c, float (&m)[V]) {
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int j = 0; j < V; j += 2) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j / 4] >> (j % 4 * 8) & 0xFFFFu), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    m[j] = f.x, m[j + 1] = f.y;
+  }
+}
+__device__ __forceinline__ void v_of_8(uint2 c, float (&v)[V]) {
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = v_of(w[j / 4] >> (j % 4 * 8) & 255u);
+}
+__device__ __forceinline__ uint2 m_codes(const float (&q)[V]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < V; j += 2)
+    w[j / 2] = __nv_cvt_float2_to_fp8x2(make_float2(q[j], q[j + 1]), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
 __device__ __forceinline__ uint32_t m_code(float q) { return __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ uint32_t v_code(float q) {
   const uint32_t b = __float_as_uint(q);
@@ -146,8 +162,12 @@ __device__ __forceinline__ void moments(const Step& h, float g, float& m, float&
   m = __fadd_rn(__fmul_rn(m, h.beta1), __fmul_rn(g, h.rest1));
   v = __fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2));
 }
+// The root and the quotient by the hardware's approximations (2^-23 of themselves; a v below the
+// normal numbers counts as 0, beside eps): what the moments round to does not depend on them.
 __device__ __forceinline__ float moved(const Step& h, float keep, float w, float m, float v) {
-  return fmaf(keep, w, -h.size * (m / fmaf(sqrtf(v), h.root, h.eps)));
+  float root;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v));
+  return fmaf(keep, w, -h.size * __fdividef(m, fmaf(root, h.root, h.eps)));
 }
 
 // A warp's block of 256 elements from `at` on, all of them there and in vectors.
@@ -169,11 +189,10 @@ __device__ __forceinline__ void whole_block(const Part& p, const Step& h, int64_
     const uint2 cv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.v) + i);
     ms = p.m_scale[at / BLOCK];
     vs = p.v_scale[at / BLOCK];
+    m_of_8(cm, m);
+    v_of_8(cv, v);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      m[j] = __fmul_rn(m_of(((j < 4 ? cm.x : cm.y) >> (j % 4 * 8)) & 255u), ms);
-      v[j] = __fmul_rn(v_of(((j < 4 ? cv.x : cv.y) >> (j % 4 * 8)) & 255u), vs);
-    }
+    for (int j = 0; j < V; ++j) m[j] = __fmul_rn(m[j], ms), v[j] = __fmul_rn(v[j], vs);
   }
   get_raw(rw, p.type, w);
   get_raw(rg, p.grad_type, g);
@@ -195,13 +214,13 @@ __device__ __forceinline__ void whole_block(const Part& p, const Step& h, int64_
     ms = block_scale(mm, (float)(1.0 / 448.0));
     vs = block_scale(mv, (float)(1.0 / 1.875));
     const float mi = __frcp_rn(ms), vi = __frcp_rn(vs);
-    uint32_t cm[2] = {0u, 0u}, cv[2] = {0u, 0u};
+    uint32_t cv[2] = {0u, 0u};
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      cm[j / 4] |= m_code(__fmul_rn(m[j], mi)) << (j % 4 * 8);
+      m[j] = __fmul_rn(m[j], mi);
       cv[j / 4] |= v_code(__fmul_rn(v[j], vi)) << (j % 4 * 8);
     }
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.m) + i) = make_uint2(cm[0], cm[1]);
+    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.m) + i) = m_codes(m);
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.v) + i) = make_uint2(cv[0], cv[1]);
     if (lane == 0) p.m_scale[at / BLOCK] = ms, p.v_scale[at / BLOCK] = vs;
   }
@@ -282,8 +301,10 @@ __global__ void __launch_bounds__(THREADS, BLOCKS)
   __syncthreads();
   if (s_skip) return;
   const Step h = s_step;
+  int i = 0;
   for (uint32_t c = blockIdx.x; c < l.pieces; c += gridDim.x) {
-    const Part& p = l.part[part_of(l, c)];
+    advance(l, c, i);
+    const Part& p = l.part[i];
     const int64_t at = (int64_t)(c - p.first) * PIECE + (threadIdx.x >> 5) * BLOCK;
     if (at >= p.n) continue;
     if (p.vec && at + BLOCK <= p.n)
@@ -313,35 +334,49 @@ struct ValueList {
     float* v_out;
     int64_t n;
     uint32_t first;
-    int32_t bits;
+    int16_t bits, vec;  // vec: every array lies on its vectors' boundary
   } part[CAP];
 };
 
+// A thread takes V elements that follow one another; past a part's last vector, or where an array does
+// not lie on its vectors' boundary, they go one by one.
 template <int CAP>
 __global__ void __launch_bounds__(THREADS) k_adamw_values(const __grid_constant__ ValueList<CAP> l) {
   follow();
+  int part = 0;
   for (uint32_t c = blockIdx.x; c < l.pieces; c += gridDim.x) {
-    int lo = 0, hi = l.count;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (l.part[mid].first <= c)
-        lo = mid;
-      else
-        hi = mid;
-    }
-    const auto& p = l.part[lo];
+    advance(l, c, part);
+    const auto& p = l.part[part];
     const int64_t at = (int64_t)(c - p.first) * PIECE;
+    const int64_t i = at + threadIdx.x * V;
+    if (p.vec && i + V <= p.n) {
+      if (p.bits == 32) {
+        Pack<float, V> m, v;
+        m.load(static_cast<const float*>(p.m) + i);
+        v.load(static_cast<const float*>(p.v) + i);
+        m.store(p.m_out + i);
+        v.store(p.v_out + i);
+      } else {
+        const uint2 cm = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.m) + i);
+        const uint2 cv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p.v) + i);
+        const float ms = p.m_scale[i / BLOCK], vs = p.v_scale[i / BLOCK];
+        float m[V], v[V];
+        m_of_8(cm, m);
+        v_of_8(cv, v);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int64_t i = at + j * THREADS + threadIdx.x;
-      if (i < p.n) {
-        if (p.bits == 32) {
-          p.m_out[i] = static_cast<const float*>(p.m)[i];
-          p.v_out[i] = static_cast<const float*>(p.v)[i];
-        } else {
-          p.m_out[i] = __fmul_rn(m_of(static_cast<const uint8_t*>(p.m)[i]), p.m_scale[i / BLOCK]);
-          p.v_out[i] = __fmul_rn(v_of(static_cast<const uint8_t*>(p.v)[i]), p.v_scale[i / BLOCK]);
-        }
+        for (int j = 0; j < V; ++j) m[j] = __fmul_rn(m[j], ms), v[j] = __fmul_rn(v[j], vs);
+        store_as(p.m_out, GBA_F32, i, m);
+        store_as(p.v_out, GBA_F32, i, v);
+      }
+      continue;
+    }
+    for (int64_t e = i; e < i + V && e < p.n; ++e) {
+      if (p.bits == 32) {
+        p.m_out[e] = static_cast<const float*>(p.m)[e];
+        p.v_out[e] = static_cast<const float*>(p.v)[e];
+      } else {
+        p.m_out[e] = __fmul_rn(m_of(static_cast<const uint8_t*>(p.m)[e]), p.m_scale[e / BLOCK]);
+        p.v_out[e] = __fmul_rn(v_of(static_cast<const uint8_t*>(p.v)[e]), p.v_scale[e / BLOCK]);
       }
     }
   }
@@ -351,10 +386,10 @@ constexpr int CAP_MOST = 384;
 static_assert(sizeof(PartList<CAP_MOST>) + sizeof(AdamWArgs) + 16 <= 32764, "the limit of a kernel's parameters");
 static_assert(sizeof(ValueList<CAP_MOST>) <= 32764, "the limit of a kernel's parameters");
 
+bool on(const void* q, size_t to) { return (uintptr_t)q % to == 0; }
 bool aligned(const gba_adamw_part& p) {
-  const auto ok = [](const void* q, size_t to) { return (uintptr_t)q % to == 0; };
-  return ok(p.weight, 16) && ok(p.grad, 16) && ok(p.copy, 16) && ok(p.m, p.bits == 32 ? 16 : 8) &&
-         ok(p.v, p.bits == 32 ? 16 : 8);
+  return on(p.weight, 16) && on(p.grad, 16) && on(p.copy, 16) && on(p.m, p.bits == 32 ? 16 : 8) &&
+         on(p.v, p.bits == 32 ? 16 : 8);
 }
 
 // The parts of `bits` from parts[at] on, as many as fit; at: the first that is left.
@@ -419,7 +454,8 @@ cudaError_t values_as(const gba_adamw_part* parts, int32_t n_parts, float* const
       if (l.count > 0 && pieces + more >= (1ull << 31)) break;
       auto& q = l.part[l.count++];
       q.m = p.m, q.v = p.v, q.m_scale = p.m_scale, q.v_scale = p.v_scale;
-      q.m_out = m_out[at], q.v_out = v_out[at], q.n = p.n, q.first = (uint32_t)pieces, q.bits = p.bits;
+      q.m_out = m_out[at], q.v_out = v_out[at], q.n = p.n, q.first = (uint32_t)pieces, q.bits = (int16_t)p.bits;
+      q.vec = on(p.m, p.bits == 32 ? 16 : 8) && on(p.v, p.bits == 32 ? 16 : 8) && on(m_out[at], 16) && on(v_out[at], 16);
       pieces += more;
     }
     l.pieces = (uint32_t)pieces;
