@@ -766,6 +766,11 @@ class AdamWStates:
                 _refuse("weights, states and step are on one GPU")
             if not t.is_contiguous():
                 _refuse("weights and states are contiguous")
+        at = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                    for ts in (self.weights, self.m, self.v, self.m_scale, self.v_scale, self.copies, [self.step])
+                    for t in ts or () if t.numel())
+        if any(b[0] < a[1] for a, b in zip(at, at[1:])):
+            _refuse("weights, states, copies or step overlap (a shared weight is listed once)")
 
     def parts(self, grads):
         """The list of weights with their gradients, made once for gradients that stay."""

@@ -250,14 +250,14 @@ def test_a_workspace_that_could_not_grow(F, w):
 def test_following_kernels_read_by_ordinary_loads():
     """As test_worker_host.py has it for the other operators."""
     found = 0
-    for name in ("gba_resnorm.cu", "gba_scan.cu", "gba_adamw.cu"):
+    for name in ("gba_resnorm.cu", "gba_scan.cuh", "gba_scan.cu", "gba_scan_grad.cu", "gba_adamw.cu"):
         code = code_of(os.path.join(BLD.CSRC, name))
         assert "__ldg" not in code and "ld.global.nc" not in code
         for kernel, params, body in kernels(code):
             found += 1
             assert re.search(r"\bfollow\(\)", body), kernel
             assert not [p for p in params.split(",") if "const" in p and "__restrict__" in p], kernel
-    assert found >= 3
+    assert found >= 10
 
 
 # ---- the Python side ----------------------------------------------------------------------
@@ -326,6 +326,7 @@ def test_tensors_of_the_workers_device_are_taken(worker, op):
 
 
 T = lambda *s, dtype=torch.float32: on(1, *s, dtype=dtype)  # noqa: E731
+STEP = lambda: T(1, dtype=torch.int64)  # noqa: E731
 BAD = {
     "norm kind": lambda w: B.residual_norm(post_norm="batch"),
     "gate kind": lambda w: B.residual_norm(gate="tanh"),
@@ -355,6 +356,8 @@ BAD = {
     "decays": lambda w: B.adamw_states([T(8)], m=[T(8)], v=[T(8)], weight_decay=[0.0, 0.1]),
     "copies' size": lambda w: B.adamw_states([T(8)], m=[T(8)], v=[T(8)], copies=[T(9)]),
     "step's type": lambda w: B.adamw_states([T(8)], m=[T(8)], v=[T(8)], step=T(1)),
+    "a weight twice": lambda w: (lambda t: B.adamw_states([t, t], m=[T(8), T(8)], v=[T(8), T(8)], step=STEP()))(T(8)),
+    "a weight that is a state": lambda w: (lambda t: B.adamw_states([T(8)], m=[t], v=[t], step=STEP()))(T(8)),
     "norm without bound": lambda w: w.adamw(states().parts([T(8)]), 1e-3, norm=T(1)),
     "bound without norm": lambda w: w.adamw(states().parts([T(8)]), 1e-3, max_norm=1.0),
     "lr's type": lambda w: w.adamw(states().parts([T(8)]), T(1, dtype=torch.float64)),
