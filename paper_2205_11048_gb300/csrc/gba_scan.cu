@@ -73,6 +73,16 @@ __global__ void __launch_bounds__(MARK_THREADS)
   }
 }
 
+// Sets the incoming states aside where the outgoing ones take their place: a sequence's last row may be
+// written by another block than the one that reads its first.
+__global__ void __launch_bounds__(MARK_THREADS) k_scan_states(ScanArgs a, float* to, int64_t stride) {
+  follow();
+  const int lane = threadIdx.x & 31;
+  const int64_t all = (int64_t)gridDim.x * (MARK_THREADS / 32);
+  for (int64_t s = (int64_t)blockIdx.x * (MARK_THREADS / 32) + (threadIdx.x >> 5); s < a.n_seq; s += all)
+    for (int c = lane; c < a.d; c += 32) to[s * stride + c] = a.state[s * a.state_stride + c];
+}
+
 // ---- the scan ------------------------------------------------------------------------------
 constexpr int STAGES = 2;  // tiles whose rows are in shared memory or under way
 
@@ -219,7 +229,8 @@ constexpr int64_t LONG = 512;
 struct Shape {
   ScanPlan p;
   bool marks;
-  size_t words, bytes;  // of the workspace: the pairs, and with the marks behind them
+  int64_t aside;        // floats of a row of the states that are set aside, or 0
+  size_t words, states, bytes;  // of the workspace: the pairs, then the marks, from `states` on the states
 };
 
 Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int num_sms) {
@@ -267,7 +278,11 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
   p.rows = rows;
   p.n_segs = (uint32_t)((a.n + rows - 1) / std::max<int64_t>(rows, 1));
   s.words = p.chained ? (size_t)p.n_segs * p.pad * 8 : 0;
-  s.bytes = s.words + (s.marks ? (size_t)a.n * 4 : 0);
+  s.states = (s.words + (s.marks ? (size_t)a.n * 4 : 0) + 15) / 16 * 16;
+  // Forwards a block reads a state before the barrier behind which it writes one; backwards it reads it
+  // behind that barrier once more, while another warp may write.
+  if (a.n > 0 && a.state && a.state == a.last && (grad || p.chained)) s.aside = ((int64_t)a.d + V - 1) / V * V;
+  s.bytes = s.states + (size_t)(a.n_seq * s.aside) * 4;
   return s;
 }
 
@@ -301,8 +316,9 @@ size_t scan_workspace(const ScanArgs& a, int32_t type, int32_t out_type, bool gr
   return shape_of(a, type, out_type, grad, num_sms).bytes;
 }
 
-cudaError_t launch_scan(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, char* ws, int num_sms,
+cudaError_t launch_scan(const ScanArgs& args, int32_t type, int32_t out_type, bool grad, char* ws, int num_sms,
                         cudaStream_t s) {
+  ScanArgs a = args;
   Shape h = shape_of(a, type, out_type, grad, num_sms);
   h.p.words = reinterpret_cast<uint64_t*>(ws);
   int32_t* marks = h.marks ? reinterpret_cast<int32_t*>(ws + h.words) : nullptr;
@@ -313,6 +329,14 @@ cudaError_t launch_scan(const ScanArgs& a, int32_t type, int32_t out_type, bool 
     const cudaError_t e = launch_following(k_scan_marks, dim3(std::max(1u, grid)), MARK_THREADS, 0, s, a, marks,
                                            a.n_seq > 0 ? a.n / a.n_seq : 0);
     if (e != cudaSuccess || a.n == 0) return e;
+  }
+  if (h.aside) {
+    float* const to = reinterpret_cast<float*>(ws + h.states);
+    const unsigned grid = (unsigned)std::min<int64_t>((a.n_seq + MARK_THREADS / 32 - 1) / (MARK_THREADS / 32), (int64_t)num_sms * 8);
+    const cudaError_t e = launch_following(k_scan_states, dim3(grid), MARK_THREADS, 0, s, a, to, h.aside);
+    if (e != cudaSuccess) return e;
+    a.state = to;
+    a.state_stride = h.aside;
   }
   return grad ? start_scan_grad(a, type, out_type, h.p, s) : start_scan_forward(a, type, out_type, h.p, s);
 }

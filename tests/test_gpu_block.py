@@ -607,6 +607,35 @@ def test_steps_with_the_state_in_place_follow_the_sequence(w, n, d):
     assert torch.equal(at, dstate) and torch.equal(dx, dx2) and torch.equal(df, df2)
 
 
+@pytest.mark.parametrize("d", [64, 513])
+@pytest.mark.parametrize("n,rows,kind", [(1, 60_000, "equal"), (2, 30_001, "packed"), (700, 5, "equal"), (300, 40, "packed")])
+def test_states_in_place_of_split_and_of_short_sequences(w, n, rows, kind, d):
+    """A sequence whose rows several blocks, or several warps of one, go through: the state that one of them
+    writes is not read by another."""
+    g = gen(d + n)
+    total = n * rows
+    x, f, dy = rand(g, total, d), rand(g, total, d, mean=2.0), rand(g, total, d)
+    s0, ds = rand(g, n, d), rand(g, n, d)
+    if kind == "equal":
+        seq, x, f, dy = B.sequences(n), x.view(n, rows, d), f.view(n, rows, d), dy.view(n, rows, d)
+        offsets = None
+    else:
+        offsets = torch.tensor([0] + [i * rows + (i * 7) % rows for i in range(1, n)] + [total], device="cuda")
+        seq = B.sequences(n, offsets=offsets)
+    y, last = w.gated_scan(x, f, seq, state=s0)
+    dx, df, dstate = w.gated_scan_grad(dy, x, f, y, seq, state=s0, dstate=ds)
+    m = lambda t: B._matrix(t.view(-1, d))  # noqa: E731
+    for _ in range(3):
+        state = s0.clone()
+        y2, st = w.gated_scan(x, f, seq, state=state, state_out=state)
+        assert st is state and torch.equal(state, last) and torch.equal(y, y2)
+        at = ds.clone()
+        dx2, df2 = torch.empty_like(dx), torch.empty_like(df)
+        w._call("gba_gated_scan_grad", B.gba_scan(0, 1, n, None, None if offsets is None else offsets.data_ptr()), m(dy),
+                m(at), m(x), m(f), m(s0), m(y), m(dx2), m(df2), m(at))
+        assert torch.equal(at, dstate) and torch.equal(dx, dx2) and torch.equal(df, df2)
+
+
 @pytest.mark.parametrize("d", [8, 33])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 def test_infinities_and_nan_stay_in_their_sequence(w, d, value):
