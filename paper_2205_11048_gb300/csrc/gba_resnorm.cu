@@ -10,6 +10,7 @@
 // held in the registers of a warp or a block; the rows of wider calls than those hold are
 // read again from L2 by one block each.
 #include <algorithm>
+#include <cfloat>
 
 #include "gba_worker.cuh"
 
@@ -40,22 +41,119 @@ __device__ __forceinline__ void params(const void* p, int32_t type, int c, float
   }
 }
 
-// The gate's factor, and its derivative.  1 / (1 + exp(-g)) and one minus it are formed from
-// exp(-|g|), which neither overflows nor cancels.
-__device__ __forceinline__ float gate_of(int32_t kind, float g, float& slope) {
+// V floats, two in one instruction where there are two: backwards the arithmetic of single floats took
+// bf16 32,768 x 2,048 from HBM's bound to the instructions' (283 us).
+template <int V>
+struct Vals {
+  using E = std::conditional_t<V == 1, float, f2>;
+  static constexpr int N = V == 1 ? 1 : V / 2;
+  E v[N];
+  Vals() = default;
+  __device__ __forceinline__ explicit Vals(const float (&x)[V]) {
+    if constexpr (V == 1) {
+      v[0] = x[0];
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = pair(x[2 * j], x[2 * j + 1]);
+    }
+  }
+  __device__ __forceinline__ explicit Vals(float x) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if constexpr (V == 1)
+        v[j] = x;
+      else
+        v[j] = pair(x, x);
+  }
+  __device__ __forceinline__ void get(float (&x)[V]) const {
+    if constexpr (V == 1) {
+      x[0] = v[0];
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) split(v[j], x[2 * j], x[2 * j + 1]);
+    }
+  }
+  __device__ __forceinline__ float sum() const {
+    if constexpr (V == 1) {
+      return v[0];
+    } else {
+      f2 s = v[0];
+#pragma unroll
+      for (int j = 1; j < N; ++j) s = add2(s, v[j]);
+      return both(s);
+    }
+  }
+};
+template <int V>
+__device__ __forceinline__ Vals<V> operator+(const Vals<V>& a, const Vals<V>& b) {
+  Vals<V> r;
+#pragma unroll
+  for (int j = 0; j < Vals<V>::N; ++j)
+    if constexpr (V == 1)
+      r.v[j] = a.v[j] + b.v[j];
+    else
+      r.v[j] = add2(a.v[j], b.v[j]);
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vals<V> operator*(const Vals<V>& a, const Vals<V>& b) {
+  Vals<V> r;
+#pragma unroll
+  for (int j = 0; j < Vals<V>::N; ++j)
+    if constexpr (V == 1)
+      r.v[j] = a.v[j] * b.v[j];
+    else
+      r.v[j] = mul2(a.v[j], b.v[j]);
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vals<V> fma_v(const Vals<V>& a, const Vals<V>& b, const Vals<V>& c) {
+  Vals<V> r;
+#pragma unroll
+  for (int j = 0; j < Vals<V>::N; ++j)
+    if constexpr (V == 1)
+      r.v[j] = fmaf(a.v[j], b.v[j], c.v[j]);
+    else
+      r.v[j] = fma2(a.v[j], b.v[j], c.v[j]);
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vals<V> operator+(const Vals<V>& a, float b) { return a + Vals<V>(b); }
+template <int V>
+__device__ __forceinline__ Vals<V> operator*(const Vals<V>& a, float b) { return a * Vals<V>(b); }
+
+// The gates' factors, and their derivatives.  With t = exp(-g), s = 1 / (1 + t) and 1 - s = t s, which
+// does not cancel.  A t that overflows (g below -88.7) gives s = 0 and derivatives of 0: 4e-37 off.  The
+// reciprocal is that of (1 + t) / 4, which is not below the least normal number.  NaNs stay.
+template <int V>
+__device__ __forceinline__ Vals<V> gate_of(int32_t kind, const Vals<V>& g, Vals<V>& slope) {
   if (kind == GBA_GATE_MUL) {
-    slope = 1.f;
+    slope = Vals<V>(1.f);
     return g;
   }
-  const float t = __expf(-fabsf(g)), q = __fdividef(1.f, 1.f + t);
-  const float sig = g >= 0.f ? q : t * q, rest = g >= 0.f ? t * q : q;
-  const float nan = g != g ? g : 0.f;
-  if (kind == GBA_GATE_SIGMOID) {
-    slope = sig * rest + nan;
-    return sig + nan;
+  float t[V], q[V];
+  (g * -1.4426950408889634f).get(t);
+#pragma unroll
+  for (int j = 0; j < V; ++j) asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(t[j]));
+  fma_v(Vals<V>(t), Vals<V>(0.25f), Vals<V>(0.25f)).get(q);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(q[j]));
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(t[j]) : "f"(FLT_MAX));
   }
-  slope = sig * (1.f + g * rest);
+  const Vals<V> sig = Vals<V>(q) * 0.25f, rest = Vals<V>(t) * sig;
+  if (kind == GBA_GATE_SIGMOID) {
+    slope = sig * rest;
+    return sig;
+  }
+  slope = sig * fma_v(g, rest, Vals<V>(1.f));
   return g * sig;
+}
+__device__ __forceinline__ float gate_of(int32_t kind, float g, float& slope) {
+  Vals<1> d;
+  const Vals<1> f = gate_of<1>(kind, Vals<1>(g), d);
+  slope = d.v[0];
+  return f.v[0];
 }
 
 // Sums over a row's threads: a warp, or the block.  red: 2 x 32 x N floats of shared memory,
@@ -74,11 +172,20 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& turn) {
 #pragma unroll
       for (int i = 0; i < N; ++i) buf[i * 32 + warp] = v[i];
     __syncthreads();
+    if (warps <= 8) {  // adding eight takes less than five exchanges
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = lane < warps ? buf[i * 32 + lane] : 0.f;
+      for (int i = 0; i < N; ++i) {
+        const float4 lo = reinterpret_cast<const float4*>(buf + i * 32)[0], hi = reinterpret_cast<const float4*>(buf + i * 32)[1];
+        v[i] = ((lo.x + (warps > 1 ? lo.y : 0.f)) + ((warps > 2 ? lo.z : 0.f) + (warps > 3 ? lo.w : 0.f))) +
+               (((warps > 4 ? hi.x : 0.f) + (warps > 5 ? hi.y : 0.f)) + ((warps > 6 ? hi.z : 0.f) + (warps > 7 ? hi.w : 0.f)));
+      }
+    } else {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      for (int i = 0; i < N; ++i) {
+        v[i] = lane < warps ? buf[i * 32 + lane] : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      }
     }
   }
 }
@@ -107,6 +214,15 @@ __device__ __forceinline__ const T* at(const Rows& m, int64_t row) {
 template <typename T>
 __device__ __forceinline__ T* at(const OutRows& m, int64_t row) {
   return static_cast<T*>(m.p) + row * m.stride;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void put(T* to, const Vals<V>& v) {
+  float x[V];
+  v.get(x);
+  Pack<T, V> o;
+  o.set(x);
+  o.store(to);
 }
 
 // ---- rows in shared memory -----------------------------------------------------------------
@@ -142,10 +258,12 @@ struct Rowed {
     }
   }
   __device__ __forceinline__ void aim(const Rows&, int64_t, int, const Place<BLOCK>&) {}
-  __device__ __forceinline__ void get(int k, const Place<BLOCK>&, float (&x)[V]) const {
+  __device__ __forceinline__ Vals<V> get(int k, const Place<BLOCK>&) const {
+    float x[V];
     Pack<T, V> w;
     w.load(at + (size_t)k * blockDim.x * V);
     w.get(x);
+    return Vals<V>(x);
   }
 };
 // Rows that start anywhere: the aligned 16 bytes that hold them, copied by the row's threads together
@@ -177,9 +295,9 @@ struct Rowed<T, 1, P, BLOCK> {
   __device__ __forceinline__ void aim(const Rows& m, int64_t r, int, const Place<BLOCK>&) {
     row = reinterpret_cast<const T*>(at + ((uintptr_t)(static_cast<const T*>(m.p) + r * m.stride) & 15));
   }
-  __device__ __forceinline__ void get(int k, const Place<BLOCK>& pl, float (&x)[1]) const {
+  __device__ __forceinline__ Vals<1> get(int k, const Place<BLOCK>& pl) const {
     const int c = k * pl.threads + pl.t;
-    x[0] = c < d ? to_float(row[c]) : 0.f;
+    return Vals<1>(c < d ? to_float(row[c]) : 0.f);
   }
 };
 
@@ -200,7 +318,7 @@ struct Rowed<float, 1, P, BLOCK> {
       v[k] = c < d ? p[c] : 0.f;
     }
   }
-  __device__ __forceinline__ void get(int k, const Place<BLOCK>&, float (&x)[1]) const { x[0] = v[k]; }
+  __device__ __forceinline__ Vals<1> get(int k, const Place<BLOCK>&) const { return Vals<1>(v[k]); }
 };
 
 // A thread's parameters.  Where it has single elements it keeps them as floats in shared memory, in
@@ -226,11 +344,14 @@ struct Params {
     return k == 0 ? a.post_weight : k == 1 ? a.post_bias : k == 2 ? a.pre_weight : a.pre_bias;
   }
   // piece p, from column c on, of the post weight and bias and the pre weight and bias
-  __device__ __forceinline__ void get(int k, int p, int c, float (&w)[V]) const {
-    if constexpr (V == 1)
-      w[0] = held[(k * P + p) * blockDim.x];
-    else
+  __device__ __forceinline__ Vals<V> get(int k, int p, int c) const {
+    if constexpr (V == 1) {
+      return Vals<V>(held[(k * P + p) * blockDim.x]);
+    } else {
+      float w[V];
       params<V>(of(k), a.param_type, c, k & 1 ? 0.f : 1.f, w);
+      return Vals<V>(w);
+    }
   }
 };
 template <int V, int P>
@@ -251,14 +372,20 @@ __device__ __forceinline__ void sync_row() {
 }
 
 // Shared memory of a block's rows: nt matrices of T and nr of R.
+template <typename T, int V, int P>
+__host__ __device__ constexpr size_t matrix_bytes(int d, int threads, bool block) {
+  if constexpr (V == 1)
+    return (block ? 1 : threads / 32) * Rowed<T, 1, P, true>::bytes(d);
+  else
+    return (size_t)threads * V * P * sizeof(T);
+}
 template <typename T, typename R, int V, int P>
 __host__ __device__ constexpr size_t stage_bytes(int nt, int nr, int d, int threads, bool block) {
-  if (V == 1) return (block ? 1 : threads / 32) * (nt * Rowed<T, 1, P, true>::bytes(d) + nr * Rowed<R, 1, P, true>::bytes(d));
-  return (size_t)threads * V * P * (nt * sizeof(T) + nr * sizeof(R));
+  return nt * matrix_bytes<T, V, P>(d, threads, block) + nr * matrix_bytes<R, V, P>(d, threads, block);
 }
 
 // ---- forward -------------------------------------------------------------------------
-// The mean and the reciprocal deviation of a row; value(p, x) gives piece p.
+// The mean and the reciprocal deviation of a row; value(p) gives piece p.
 template <int V, int P, bool BLOCK, typename F>
 __device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNormArgs& a, const Place<BLOCK>& at,
                                             float* red, int& turn) {
@@ -269,29 +396,21 @@ __device__ __forceinline__ float2 row_stats(F value, int32_t kind, const ResNorm
     float s[1] = {0.f};
 #pragma unroll
     for (int p = 0; p < P; ++p)
-      if (V == 1 || (p * at.threads + at.t) * V < a.d) {
-        float x[V];
-        value(p, x);
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[0] += x[j];
-      }
+      if (V == 1 || (p * at.threads + at.t) * V < a.d) s[0] += value(p).sum();
     row_sums<1, BLOCK>(s, red, turn);
     mean = s[0] * inv;
   }
-  float q[1] = {0.f};
+  Vals<V> q(0.f);
 #pragma unroll
   for (int p = 0; p < P; ++p)
     if (V == 1 || (p * at.threads + at.t) * V < a.d) {
-      float x[V];
-      value(p, x);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float e = V > 1 || p * at.threads + at.t < a.d ? x[j] - mean : 0.f;
-        q[0] = fmaf(e, e, q[0]);
-      }
+      Vals<V> e = value(p) + -mean;
+      if (V == 1 && p * at.threads + at.t >= a.d) e = Vals<V>(0.f);
+      q = fma_v(e, e, q);
     }
-  row_sums<1, BLOCK>(q, red, turn);
-  return make_float2(mean, 1.f / sqrtf(q[0] * inv + a.eps));
+  float sum[1] = {q.sum()};
+  row_sums<1, BLOCK>(sum, red, turn);
+  return make_float2(mean, 1.f / sqrtf(sum[0] * inv + a.eps));
 }
 
 // B: the most threads of a block that holds one row; 0: a row is a warp's
@@ -299,7 +418,7 @@ template <typename T, typename R, int V, int P, int B>
 __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_norm(ResNormArgs a) {
   constexpr bool BLOCK = B > 0;
   extern __shared__ __align__(16) char smem[];
-  __shared__ float red[2 * 64];
+  __shared__ __align__(16) float red[2 * 64];
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
@@ -329,70 +448,34 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 ? 1 : 4) k_residual_nor
     Rm rs(base, a.d, pl);
     Tm xs(base, a.d, pl), gs(base, a.d, pl);
     xs.aim(a.x, row, a.d, pl), rs.aim(a.r, row, a.d, pl), gs.aim(a.g, row, a.d, pl);
-    const float2 sx = row_stats<V, P, BLOCK>([&](int p, float (&x)[V]) { xs.get(p, pl, x); }, a.post, a, pl, red, turn);
-    float z[P][V];
+    const float2 sx = row_stats<V, P, BLOCK>([&](int p) { return xs.get(p, pl); }, a.post, a, pl, red, turn);
+    Vals<V> z[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int c = (p * pl.threads + pl.t) * V;
-#pragma unroll
-      for (int j = 0; j < V; ++j) z[p][j] = 0.f;
+      z[p] = Vals<V>(0.f);
       if (V == 1 || c < a.d) {
-        float x[V], w[V];
-        xs.get(p, pl, x);
-        par.get(0, p, c, w);
-#pragma unroll
-        for (int j = 0; j < V; ++j) z[p][j] = (x[j] - sx.x) * sx.y * w[j];
-        if (a.post_bias) {
-          par.get(1, p, c, w);
-#pragma unroll
-          for (int j = 0; j < V; ++j) z[p][j] += w[j];
-        }
+        z[p] = (xs.get(p, pl) + -sx.x) * sx.y * par.get(0, p, c);
+        if (a.post_bias) z[p] = z[p] + par.get(1, p, c);
         if (a.gate != GBA_GATE_NONE) {
-          gs.get(p, pl, x);
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            float slope;
-            z[p][j] *= gate_of(a.gate, x[j], slope);
-          }
+          Vals<V> slope;
+          z[p] = z[p] * gate_of<V>(a.gate, gs.get(p, pl), slope);
         }
-#pragma unroll
-        for (int j = 0; j < V; ++j) z[p][j] *= a.bscale;
-        if (a.r.p) {
-          rs.get(p, pl, x);
-#pragma unroll
-          for (int j = 0; j < V; ++j) z[p][j] = fmaf(a.rscale, x[j], z[p][j]);
-        }
-        if (a.z.p) {
-          Pack<R, V> o;
-          o.set(z[p]);
-          if (V > 1 || c < a.d) o.store(at<R>(a.z, row) + c);
-        }
+        z[p] = z[p] * a.bscale;
+        if (a.r.p) z[p] = fma_v(rs.get(p, pl), Vals<V>(a.rscale), z[p]);
+        if (a.z.p && (V > 1 || c < a.d)) put<R, V>(at<R>(a.z, row) + c, z[p]);
       }
     }
-    const float2 sz = row_stats<V, P, BLOCK>(
-        [&](int p, float (&x)[V]) {
-#pragma unroll
-          for (int j = 0; j < V; ++j) x[j] = z[p][j];
-        },
-        a.pre, a, pl, red, turn);
+    const float2 sz = row_stats<V, P, BLOCK>([&](int p) { return z[p]; }, a.pre, a, pl, red, turn);
     if (a.stats && pl.t == 0) a.stats[row] = make_float4(sx.x, sx.y, sz.x, sz.y);
     if (a.y.p)
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
         if (V == 1 || c < a.d) {
-          float w[V];
-          par.get(2, p, c, w);
-#pragma unroll
-          for (int j = 0; j < V; ++j) z[p][j] = (z[p][j] - sz.x) * sz.y * w[j];
-          if (a.pre_bias) {
-            par.get(3, p, c, w);
-#pragma unroll
-            for (int j = 0; j < V; ++j) z[p][j] += w[j];
-          }
-          Pack<T, V> o;
-          o.set(z[p]);
-          if (V > 1 || c < a.d) o.store(at<T>(a.y, row) + c);
+          z[p] = (z[p] + -sz.x) * sz.y * par.get(2, p, c);
+          if (a.pre_bias) z[p] = z[p] + par.get(3, p, c);
+          if (V > 1 || c < a.d) put<T, V>(at<T>(a.y, row) + c, z[p]);
         }
       }
   }
@@ -404,7 +487,7 @@ constexpr int WIDE = 1024;
 // Rows of any width: a block goes over its row once for each sum and once for the outputs.
 template <typename T, typename R>
 __global__ void __launch_bounds__(WIDE) k_residual_norm_wide(ResNormArgs a) {
-  __shared__ float red[2 * 64];
+  __shared__ __align__(16) float red[2 * 64];
   int turn = 0;
   follow();
   const float inv = 1.f / (float)a.d;
@@ -457,7 +540,7 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_wide(ResNormArgs a) {
 // ---- gradient --------------------------------------------------------------------------
 // Writes a block's partial sums of the parameters' gradients (4 x d) to its slot.
 template <int V, int P, bool BLOCK>
-__device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& pl, float (&acc)[4][P][V],
+__device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& pl, Vals<V> (&acc)[4][P],
                                       float* slot, float* joined) {
   if constexpr (BLOCK) {
 #pragma unroll
@@ -466,11 +549,12 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const int c = (p * pl.threads + pl.t) * V;
+          float v[V];
+          acc[k][p].get(v);
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            if (c + j < a.d) slot[(int64_t)k * a.d + c + j] = acc[k][p][j];
-            acc[k][p][j] = 0.f;
-          }
+          for (int j = 0; j < V; ++j)
+            if (c + j < a.d) slot[(int64_t)k * a.d + c + j] = v[j];
+          acc[k][p] = Vals<V>(0.f);
         }
   } else {
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
@@ -480,13 +564,16 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int p = 0; p < P; ++p)
+          for (int p = 0; p < P; ++p) {
+            float v[V];
+            acc[k][p].get(v);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
               float* q = joined + k * COLS + (p * 32 + pl.t) * V + j;
-              *q = i ? *q + acc[k][p][j] : acc[k][p][j];
-              acc[k][p][j] = 0.f;
+              *q = i ? *q + v[j] : v[j];
             }
+            acc[k][p] = Vals<V>(0.f);
+          }
       __syncthreads();
     }
     for (int i = threadIdx.x; i < 4 * a.d; i += blockDim.x) {
@@ -497,25 +584,28 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
   }
 }
 
-// BIAS: the gradients of biases are wanted.  Without their sums three blocks of 256 fit an SM.
+// Blocks of an SM, by the registers: the sums of biases' gradients (BIAS) take a third.
+constexpr int grad_blocks(int v, int p, int b, bool bias) {
+  if (b >= 512) return 1;
+  if (v == 8 && p == 2) return b == 128 ? 4 : 2;
+  return bias || v == 1 ? 2 : 3;
+}
 template <typename T, typename R, int V, int P, int B, bool BIAS>
-__global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS || V == 1 ? 2 : 3)
+__global__ void __launch_bounds__(B ? B : 256, grad_blocks(V, P, B, BIAS))
     k_residual_norm_grad(ResNormArgs a, int slots) {
   constexpr bool BLOCK = B > 0;
   extern __shared__ __align__(16) char smem[];
-  __shared__ float red[2 * 64];
+  __shared__ __align__(16) float red[2 * 64];
   __shared__ float joined[BLOCK ? 1 : 4 * 32 * P * V];
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
   const float inv = 1.f / (float)a.d;
-  float acc[4][P][V];
+  Vals<V> acc[4][P];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-#pragma unroll
-      for (int j = 0; j < V; ++j) acc[k][p][j] = 0.f;
+    for (int p = 0; p < P; ++p) acc[k][p] = Vals<V>(0.f);
   float* slot = a.parts + (int64_t)blockIdx.x * slots * 4 * a.d;
   int chain = 0, filled = 0;
   using Tm = Rowed<T, V, P, BLOCK>;
@@ -554,105 +644,70 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
       Tm dys(from, a.d, pl), xs(from, a.d, pl), gs(from, a.d, pl);
       zs.aim(a.zin, row, a.d, pl), dzs.aim(a.dz, row, a.d, pl);
       dys.aim(a.dy, row, a.d, pl), xs.aim(a.x, row, a.d, pl), gs.aim(a.g, row, a.d, pl);
-      float D[P][V];  // the gradient of z; first gy
+      Vals<V> D[P];  // the gradient of z; first gy
       float s[2] = {0.f, 0.f};
       if (a.dy.p) {
+        Vals<V> sh(0.f), sg(0.f);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           const int c = (p * pl.threads + pl.t) * V;
           if (V == 1 || c < a.d) {
-            float z[V], w[V];
-            dys.get(p, pl, D[p]);
-            zs.get(p, pl, z);
-            par.get(2, p, c, w);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float zh = (z[j] - st.z) * st.w;
-              acc[2][p][j] = fmaf(D[p][j], zh, acc[2][p][j]);
-              if (BIAS) acc[3][p][j] += D[p][j];
-              D[p][j] *= w[j];
-              s[0] = fmaf(D[p][j], zh, s[0]);
-              s[1] += D[p][j];
-            }
+            const Vals<V> zh = (zs.get(p, pl) + -st.z) * st.w;
+            D[p] = dys.get(p, pl);
+            acc[2][p] = fma_v(D[p], zh, acc[2][p]);
+            if (BIAS) acc[3][p] = acc[3][p] + D[p];
+            D[p] = D[p] * par.get(2, p, c);
+            sh = fma_v(D[p], zh, sh);
+            sg = sg + D[p];
           }
         }
+        s[0] = sh.sum(), s[1] = sg.sum();
         row_sums<2, BLOCK>(s, red, turn);
-        s[0] *= inv;
-        s[1] = a.pre == GBA_NORM_LAYER ? s[1] * inv : 0.f;
+        s[0] *= -inv * st.w;
+        s[1] = a.pre == GBA_NORM_LAYER ? -s[1] * inv : 0.f;
+      }
+      Vals<V> qh(0.f), qg(0.f);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const int c = (p * pl.threads + pl.t) * V;
+        if (V == 1 || c < a.d) {
+          if (a.dy.p) {
+            D[p] = fma_v(zs.get(p, pl) + -st.z, Vals<V>(s[0]), D[p] + s[1]) * st.w;
+            if (V == 1 && c >= a.d) D[p] = Vals<V>(0.f);
+          } else {
+            D[p] = Vals<V>(0.f);
+          }
+          if (a.dz.p) D[p] = D[p] + dzs.get(p, pl);
+          if (a.dr.p && (V > 1 || c < a.d)) put<R, V>(at<R>(a.dr, row) + c, D[p] * a.rscale);
+          const Vals<V> xh = (xs.get(p, pl) + -st.x) * st.y, w = par.get(0, p, c);
+          D[p] = D[p] * a.bscale;
+          if (a.gate != GBA_GATE_NONE) {
+            Vals<V> slope;
+            const Vals<V> act = gate_of<V>(a.gate, gs.get(p, pl), slope);
+            const Vals<V> dg = D[p] * fma_v(xh, w, par.get(1, p, c)) * slope;
+            if (V > 1 || c < a.d) put<T, V>(at<T>(a.dg, row) + c, dg);
+            D[p] = D[p] * act;
+          }
+          acc[0][p] = fma_v(D[p], xh, acc[0][p]);
+          if (BIAS) acc[1][p] = acc[1][p] + D[p];
+          D[p] = D[p] * w;  // gu
+          qh = fma_v(D[p], xh, qh);
+          qg = qg + D[p];
+        }
       }
       float q[2] = {0.f, 0.f};
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const int c = (p * pl.threads + pl.t) * V;
-        if (V == 1 || c < a.d) {
-          float x[V], v[V], w[V];
-          if (a.dy.p) {
-            zs.get(p, pl, v);
-#pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] = V > 1 || c < a.d ? st.w * (D[p][j] - s[1] - (v[j] - st.z) * st.w * s[0]) : 0.f;
-          } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] = 0.f;
-          }
-          if (a.dz.p) {
-            dzs.get(p, pl, v);
-#pragma unroll
-            for (int j = 0; j < V; ++j) D[p][j] += v[j];
-          }
-          if (a.dr.p) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = a.rscale * D[p][j];
-            Pack<R, V> o;
-            o.set(v);
-            if (V > 1 || c < a.d) o.store(at<R>(a.dr, row) + c);
-          }
-          xs.get(p, pl, x);
-          par.get(0, p, c, w);
-#pragma unroll
-          for (int j = 0; j < V; ++j) x[j] = (x[j] - st.x) * st.y, D[p][j] *= a.bscale;
-          if (a.gate != GBA_GATE_NONE) {
-            float b[V];
-            gs.get(p, pl, v);
-            par.get(1, p, c, b);
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-              float slope;
-              const float act = gate_of(a.gate, v[j], slope);
-              v[j] = D[p][j] * fmaf(x[j], w[j], b[j]) * slope;
-              D[p][j] *= act;
-            }
-            Pack<T, V> o;
-            o.set(v);
-            if (V > 1 || c < a.d) o.store(at<T>(a.dg, row) + c);
-          }
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            acc[0][p][j] = fmaf(D[p][j], x[j], acc[0][p][j]);
-            if (BIAS) acc[1][p][j] += D[p][j];
-            D[p][j] *= w[j];  // gu
-            q[0] = fmaf(D[p][j], x[j], q[0]);
-            q[1] += D[p][j];
-          }
-        }
-      }
       if (a.post != GBA_NORM_NONE) {
+        q[0] = qh.sum(), q[1] = qg.sum();
         row_sums<2, BLOCK>(q, red, turn);
-        q[0] *= inv;
-        q[1] = a.post == GBA_NORM_LAYER ? q[1] * inv : 0.f;
-      } else {
-        q[0] = q[1] = 0.f;
+        q[0] *= -inv * st.y;
+        q[1] = a.post == GBA_NORM_LAYER ? -q[1] * inv : 0.f;
       }
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const int c = (p * pl.threads + pl.t) * V;
         if (V == 1 || c < a.d) {
-          float x[V];
-          xs.get(p, pl, x);
-#pragma unroll
-          for (int j = 0; j < V; ++j) x[j] = st.y * (D[p][j] - q[1] - (x[j] - st.x) * st.y * q[0]);
-          Pack<T, V> o;
-          o.set(x);
-          if (V > 1 || c < a.d) o.store(at<T>(a.dx, row) + c);
+          const Vals<V> dx = fma_v(xs.get(p, pl) + -st.x, Vals<V>(q[0]), D[p] + q[1]) * st.y;
+          if (V > 1 || c < a.d) put<T, V>(at<T>(a.dx, row) + c, dx);
         }
       }
     }
@@ -669,7 +724,7 @@ __global__ void __launch_bounds__(B ? B : 256, B == 1024 || B == 512 ? 1 : BIAS 
 // sums lie in the block's slots, each column added to by one thread.
 template <typename T, typename R>
 __global__ void __launch_bounds__(WIDE) k_residual_norm_grad_wide(ResNormArgs a, int slots) {
-  __shared__ float red[2 * 64];
+  __shared__ __align__(16) float red[2 * 64];
   int turn = 0;
   follow();
   const float inv = 1.f / (float)a.d;
@@ -801,8 +856,11 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   Shape s{};
   s.v = vector_for(a, type, wide, grad);
   const int d = a.d, vecs = (d + s.v - 1) / s.v;
+  // sixteen where registers hold them: 32,768 x 2,048 236 us, 65,536 x 1,024 235, with eight 255 and 250
+  const bool biases = a.sums[1] || a.sums[3];
+  const bool two = grad && s.v == 8 && type_bytes(wide) == 2 && !biases && d >= 1024 && d <= 8192;
   if (grad || s.v == 1) {  // eight elements a thread; the gradient's go with four sums of parameters' gradients
-    s.packs = 8 / s.v;
+    s.packs = two ? 2 : 8 / s.v;
     s.block = d > 256;
   } else {
     s.block = vecs > 128;
@@ -814,14 +872,14 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   // two rows of each block lie in shared memory; wider ones are read again for each sum
   const size_t b = type_bytes(type), w = type_bytes(wide), room = 226 << 10;
   const size_t nt = grad ? 3 : 2, nr = grad ? 2 : 1;
-  size_t bytes = 2 * (size_t)s.threads * s.rows * each * (nt * b + nr * w);
-  if (s.v == 1) {  // those of 16 bits, and the parameters
-    bytes = b == 2 ? 2 * s.rows * nt * ((size_t)d * 2 + 32) : 0;
-    if (w == 2) bytes += 2 * s.rows * nr * ((size_t)d * 2 + 32);
-    bytes += (size_t)s.threads * s.rows * HELD_BYTES<1, 8>;
-  }
+  auto matrix = [&](size_t of) {  // the bytes of two rows
+    if (s.v == 1) return of == 2 ? 2 * s.rows * ((size_t)d * 2 + 32) : 0;
+    return 2 * (size_t)s.threads * s.rows * each * of;
+  };
+  const size_t held = s.v == 1 ? HELD_BYTES<1, 8> : 0;
+  const size_t bytes = nt * matrix(b) + nr * matrix(w) + (size_t)s.threads * s.rows * held;
   // that registers are for
-  const size_t threads = !grad ? 1024 : s.v == 1 || a.sums[1] || a.sums[3] ? 576 : 768;
+  const size_t threads = !grad ? 1024 : two ? 512 : s.v == 1 || biases ? 576 : 768;
   size_t most = 2;  // blocks of an SM
   if (s.threads > 1024 || bytes > room) {
     s.packs = 0;
@@ -866,26 +924,32 @@ cudaError_t forward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   return h.packs == 2 ? forward_in<T, R, V, 2>(a, h, s) : forward_in<T, R, V, 4>(a, h, s);
 }
 
-template <typename T, typename R, int V, int P, bool BIAS>
-cudaError_t backward_as(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
+template <typename T, typename R, int V, int P, int B, bool BIAS>
+cudaError_t backward_of(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   const size_t stage = stage_bytes<T, R, V, P>(3, 2, a.d, h.threads * h.rows, h.block);
-  if (!h.block) return start(k_residual_norm_grad<T, R, V, P, 0, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
-  if (h.threads <= 256) return start(k_residual_norm_grad<T, R, V, P, 256, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
-  if (h.threads <= 512) return start(k_residual_norm_grad<T, R, V, P, 512, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
-  return start(k_residual_norm_grad<T, R, V, P, 1024, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
+  return start(k_residual_norm_grad<T, R, V, P, B, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
 }
-template <typename T, typename R, int V, int P>
-cudaError_t backward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
-  if constexpr (V > 1)
-    if (!a.sums[1] && !a.sums[3]) return backward_as<T, R, V, P, false>(a, h, s);
-  return backward_as<T, R, V, P, true>(a, h, s);
+template <typename T, typename R, int V, bool BIAS>
+cudaError_t backward_as(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
+  constexpr int P = 8 / V;
+  if constexpr (V == 8 && sizeof(R) == 2 && !BIAS)
+    if (h.packs == 2) {
+      if (h.threads <= 128) return backward_of<T, R, V, 2, 128, BIAS>(a, h, s);
+      if (h.threads <= 256) return backward_of<T, R, V, 2, 256, BIAS>(a, h, s);
+      return backward_of<T, R, V, 2, 512, BIAS>(a, h, s);
+    }
+  if (!h.block) return backward_of<T, R, V, P, 0, BIAS>(a, h, s);
+  if (h.threads <= 256) return backward_of<T, R, V, P, 256, BIAS>(a, h, s);
+  if (h.threads <= 512) return backward_of<T, R, V, P, 512, BIAS>(a, h, s);
+  return backward_of<T, R, V, P, 1024, BIAS>(a, h, s);
 }
 
 template <typename T, typename R>
 cudaError_t backward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   constexpr int V = 16 / (int)sizeof(T);
   if (h.packs == 0) return launch_following(k_residual_norm_grad_wide<T, R>, dim3(h.grid), WIDE, 0, s, a, h.slots);
-  return h.v == 1 ? backward_in<T, R, 1, 8>(a, h, s) : backward_in<T, R, V, 8 / V>(a, h, s);
+  if (h.v == 1) return backward_as<T, R, 1, true>(a, h, s);
+  return a.sums[1] || a.sums[3] ? backward_as<T, R, V, true>(a, h, s) : backward_as<T, R, V, false>(a, h, s);
 }
 
 }  // namespace
