@@ -8,6 +8,10 @@
 // scales over 256.  The moments are formed by one IEEE operation after another (no fused
 // multiply-add), so that which code a moment is rounded to follows from its formula; the weight
 // is rounded once.
+// 64 10^6 float32 weights in 148 tensors with bf16 gradients and copies: 314 us, 5.70 TB/s; with 8-bit
+// states 178 us, 5.77 TB/s, and 164 us for reading them as float32 (3.9 TB/s: 128 MB in, 512 MB out, the
+// bandwidth of writes alone).  306,496 weights: 6 us, a launch.  Four blocks an SM: three took 323 us,
+// five 312 and, in 8 bits, 198.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -323,7 +327,6 @@ __global__ void __launch_bounds__(THREADS, BLOCKS)
 template <int CAP>
 struct ValueList {
   int32_t count;
-  int32_t bits;
   uint32_t pieces;
   struct {
     const void* m;

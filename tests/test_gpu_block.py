@@ -233,13 +233,14 @@ def test_residual_norm_and_its_gradient(w, dtype, wide, n, d, extra, offset):
         check_gradient(w, t, how, block, dtype, wide, z, stats, g)
 
 
-@pytest.mark.parametrize("n,d,dtype", [(100_000, 64, torch.bfloat16), (30_000, 520, torch.bfloat16),
-                                       (20_000, 301, torch.float32), (3_000_000, 8, torch.float32)])
-def test_many_rows(w, n, d, dtype):
+@pytest.mark.parametrize("n,d,dtype,post", [(100_000, 64, torch.bfloat16, "layer"), (30_000, 520, torch.bfloat16, "layer"),
+                                            (20_000, 301, torch.float32, "layer"), (3_000_000, 8, torch.float32, "layer"),
+                                            (9_000, 2048, torch.float16, "rms")])
+def test_many_rows(w, n, d, dtype, post):
     """More rows than blocks, and (the last) more than a thread adds in one chain: the bounds of
     the parameters' gradients do not grow with the rows."""
     g = gen(d)
-    t, how, block = make(g, n, d, dtype, dtype, "layer", "rms", "silu")
+    t, how, block = make(g, n, d, dtype, dtype, post, "rms", "silu")
     _, z, stats = check_forward(w, t, how, block, dtype, dtype)
     check_gradient(w, t, how, block, dtype, dtype, z, stats, g)
 
