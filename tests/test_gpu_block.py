@@ -574,7 +574,8 @@ def test_long_sequences(w, kind, n, rows, d):
     check_scan(w, kind, n, rows, d, torch.bfloat16, "log", False, False)
 
 
-@pytest.mark.parametrize("kind,n,rows,d", [("equal", 2, 60_000, 1024), ("packed", 100, 50_000, 1020)])
+@pytest.mark.parametrize("kind,n,rows,d", [("equal", 2, 60_000, 1024), ("packed", 100, 50_000, 1020),
+                                           ("equal", 16, 16 * 1001, 2044), ("equal", 300, 300 * 130, 132)])
 def test_many_tiles(w, kind, n, rows, d):
     check_scan(w, kind, n, rows, d, torch.bfloat16, "sigmoid", True, True, mean=4.0)
 
