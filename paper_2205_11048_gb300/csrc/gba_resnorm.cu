@@ -822,10 +822,19 @@ __global__ void __launch_bounds__(32 * SUM_LANES) k_residual_norm_sums(ResNormAr
   if (!out) return;
   float sum = 0.f, off = 0.f;
   if (c < a.d)
-    for (int i = threadIdx.y; i < slots; i += SUM_LANES) {
-      const float v = a.parts[((int64_t)i * 4 + k) * a.d + c], s = sum + v, bb = s - sum;
-      off += (sum - (s - bb)) + (v - bb);
-      sum = s;
+    for (int i = threadIdx.y; i < slots; i += 8 * SUM_LANES) {
+      float v[8];  // on their way together: one after another 608 slots took 18 us
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int j = i + u * SUM_LANES;
+        v[u] = j < slots ? a.parts[((int64_t)j * 4 + k) * a.d + c] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float s = sum + v[u], bb = s - sum;
+        off += (sum - (s - bb)) + (v[u] - bb);
+        sum = s;
+      }
     }
   // a sum that is infinite is its plain sum: the correction of an infinity is a NaN
   part[threadIdx.y][threadIdx.x] = isfinite(sum) ? sum + off : sum;
