@@ -258,11 +258,18 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
   p.pad = p.n_cols * cols;
   p.each = (uint32_t)(a.n_seq > 0 ? a.n / a.n_seq : 0);
   s.marks = a.offsets || a.lengths;
-  // blocks that run at a time: 16-bit rows of four (the gradient: three) fit an SM, float32 rows of one less
+  // blocks that run at a time: 16-bit rows of four (the gradient: three) fit an SM, float32 rows of one less.
+  // The gradient's float32 rows of ragged or of many sequences go half as many at a time, of which three
+  // blocks fit: 256 x 128 x 2,048 237 us against 408, packed 20,003 x 501 111 and 126; but one sequence of
+  // 131,072 x 512 390 against 326.
   const bool wide = grad ? b == 4 || ob == 4 : b == 4;
-  const int64_t ty = SCAN_THREADS / p.tx, slots = (int64_t)num_sms * ((grad ? GRAD_BLOCKS : SCAN_BLOCKS) - wide);
-  const bool few = (a.n + ty * SCAN_STEPS - 1) / (ty * SCAN_STEPS) * p.n_cols < num_sms;
-  p.steps = few && !p.loose && p.tx == 32 ? SCAN_FEW : SCAN_STEPS;
+  const bool many = a.n_seq * p.n_cols >= (int64_t)num_sms * (grad ? 8 : 5) / 4;
+  const bool half = grad && wide && p.tx == 32 && (s.marks || many);
+  const int64_t ty = SCAN_THREADS / p.tx;
+  const int64_t slots = (int64_t)num_sms * ((grad ? GRAD_BLOCKS : SCAN_BLOCKS) - (wide && !half));
+  const int steps = half ? SCAN_WIDE : SCAN_STEPS;
+  const bool few = (a.n + ty * steps - 1) / (ty * steps) * p.n_cols < num_sms;
+  p.steps = few && !p.loose && p.tx == 32 ? SCAN_FEW : steps;
   const int64_t tile = ty * p.steps, want = std::max<int64_t>(1, slots / p.n_cols);
   int64_t rows = std::max((a.n + want - 1) / want, tile);
   if (s.marks) {
@@ -271,7 +278,7 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
     p.chained = rows < a.n;
   } else if (a.n > 0) {
     const int64_t each = p.each;
-    if (each <= 2 * rows || a.n_seq * p.n_cols >= (int64_t)num_sms * (grad ? 8 : 5) / 4) {
+    if (each <= 2 * rows || many) {
       // whole sequences, which need nothing of one another, so the segments may be short
       rows = std::max(tile, std::min(rows, SHORT));
       rows = std::max<int64_t>(1, (rows + each / 2) / each) * each;

@@ -514,6 +514,7 @@ inline cudaError_t start_scan(K kernel, unsigned blocks, const ScanArgs& a, cons
 
 constexpr int SCAN_STEPS = 8;  // positions of a thread; few where there is little work
 constexpr int SCAN_FEW = 2;
+constexpr int SCAN_WIDE = 4;   // backwards, of float32 rows of many sequences
 constexpr int SCAN_BLOCKS = 4, GRAD_BLOCKS = 3;  // of an SM
 
 cudaError_t start_scan_grad(const ScanArgs& a, int32_t type, int32_t out_type, const ScanPlan& p, cudaStream_t s);

@@ -201,6 +201,9 @@ template <typename T, typename O>
 cudaError_t launch_as(const ScanArgs& a, const ScanPlan& p, cudaStream_t s) {
   if (p.tx == 8)
     return p.loose ? start<T, O, 8, SCAN_STEPS, true>(a, p, s) : start<T, O, 8, SCAN_STEPS, false>(a, p, s);
+  if constexpr (sizeof(T) == 4 || sizeof(O) == 4)
+    if (p.steps == SCAN_WIDE)
+      return p.loose ? start<T, O, 32, SCAN_WIDE, true>(a, p, s) : start<T, O, 32, SCAN_WIDE, false>(a, p, s);
   if (p.loose) return start<T, O, 32, SCAN_STEPS, true>(a, p, s);
   return p.steps == SCAN_STEPS ? start<T, O, 32, SCAN_STEPS, false>(a, p, s) : start<T, O, 32, SCAN_FEW, false>(a, p, s);
 }

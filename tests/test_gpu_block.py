@@ -580,6 +580,12 @@ def test_many_tiles(w, kind, n, rows, d):
     check_scan(w, kind, n, rows, d, torch.bfloat16, "sigmoid", True, True, mean=4.0)
 
 
+@pytest.mark.parametrize("kind,n,rows,d", [("equal", 64, 64 * 70, 1024), ("packed", 40, 9000, 501), ("padded", 20, 20 * 150, 516)])
+def test_many_sequences_in_float32(w, kind, n, rows, d):
+    for dtype, out in ((torch.float32, None), (torch.bfloat16, torch.float32)):
+        check_scan(w, kind, n, rows, d, dtype, "sigmoid", True, True, out=out, mean=4.0)
+
+
 @pytest.mark.parametrize("n,d", [(1, 64), (33, 1024), (256, 77)])
 def test_steps_with_the_state_in_place_follow_the_sequence(w, n, d):
     """A sequence a row at a time gives what it gives at once, within the rounding of both."""
