@@ -9,8 +9,8 @@
 // multiply-add), so that which code a moment is rounded to follows from its formula; the weight
 // is rounded once.
 // 64 10^6 float32 weights in 148 tensors with bf16 gradients and copies: 314 us, 5.70 TB/s; with 8-bit
-// states 178 us, 5.77 TB/s, and 164 us for reading them as float32 (3.9 TB/s: 128 MB in, 512 MB out, the
-// bandwidth of writes alone).  306,496 weights: 6 us, a launch.  Four blocks an SM: three took 323 us,
+// states 178 us, 5.77 TB/s, and 147 us for reading them as float32 (4.4 TB/s: 128 MB in, 512 MB out).
+// 306,496 weights: 6 us, a launch.  Four blocks an SM: three took 323 us,
 // five 312 and, in 8 bits, 198.
 #include <cuda_fp8.h>
 

@@ -11,11 +11,11 @@
 // or a block's; the next row's pieces are copied to shared memory while a row is worked on, and z or D stays
 // in registers between the sums.  Rows that do not fit so are read again from L2 by one block each.
 //   forward  bf16 32,768 x 4,096, float32 residual, one norm   260 us, 6.2 TB/s: HBM
-//            bf16 32,768 x 2,048, two norms and a gate         145 us, 4.6 TB/s: half the issue slots, and two
+//            bf16 32,768 x 2,048, two norms and a gate         145 us, 4.6 TB/s: 73% of the issue slots, and two
 //            sums over the block one after another
-//   gradient bf16 32,768 x 2,048, the same                     238 us, 4.5 TB/s: 75 instructions an element
-//            (55% of the issue slots), of which a third widen 16 bits or build pairs of floats
-//            float32 5,003 x 1,001, layer norms with biases     86 us, 1.9 TB/s: single elements, and 4 rows an SM
+//   gradient bf16 32,768 x 2,048, the same                     237 us, 4.5 TB/s: 76 instructions an element
+//            (58% of the issue slots): 16-bit values are widened in every pass, and pairs of floats built
+//            float32 5,003 x 1,001, layer norms with biases     82 us, 1.9 TB/s: single elements, and 4 rows an SM
 //            at a time, because the sums of four parameters' gradients take the registers
 // Single elements (rows or parameters that do not lie on 16 bytes): reading 16-bit rows by vectors that are
 // brought into place, with outputs through shared memory, took bf16 32,768 x 2,049 787 us against 1,110

@@ -15,12 +15,14 @@
 // segment, from the last entry in it on, which reads those rows once more; a block joins the
 // pairs of the segments before its own.  Every order is fixed by the sizes: equal calls give
 // equal bits.
-//   bf16 65,536 x 2,048   16 sequences 177 us, 64 136 us (5.9 TB/s), one 236 us: half of it the rows read for
-//                         the pairs; in blocks that waited for one another's pairs 606 us
-//   bf16 262,144 x 256    one sequence 127 us, of which 50 the pairs
-//   gradient, bf16 65,536 x 2,048, 64 sequences 364 us, 32 padded ones 352 us; float32 20,003 x 501, packed, 126 us
-// Forward the full calls are within a sixth of HBM's time.  The gradient has 60 instructions an element and
-// three blocks an SM, by its shared memory (four matrices, two tiles each): latency, not bandwidth.
+//   bf16 65,536 x 2,048   64 sequences 138 us (5.8 TB/s), 16 164 us: few blocks, each a latency a tile; one
+//                         237 us; in blocks that waited for one another's pairs 16 took 606 us
+//   bf16 262,144 x 256    one sequence 127 us, of which the pairs' kernel takes two fifths: it reads both
+//                         inputs once more, of which L2 keeps half for the kernel after it
+//   gradient              bf16 65,536 x 2,048, 64 sequences 368 us, 32 padded ones 352 us; float32 20,003 x 501,
+//                         packed, 107 us
+// The gradient has 40 to 55 instructions an element and three blocks of four warps an SM, by its shared memory
+// (four matrices, two tiles each): 44% of the issue slots, 3.9 TB/s, latency before bandwidth.
 #include <algorithm>
 
 #include "gba_scan.cuh"
