@@ -595,6 +595,10 @@ __device__ __forceinline__ void flush(const ResNormArgs& a, const Place<BLOCK>& 
   }
 }
 
+// Floats through which the warps of a block join their sums.
+template <int V, int P, bool BLOCK>
+constexpr size_t JOINED = BLOCK ? 1 : 4 * 32 * P * V;
+
 // Blocks of an SM, by the registers: the sums of biases' gradients (BIAS) take a third.
 constexpr int grad_blocks(int v, int p, int b, bool bias) {
   if (b >= 512) return 1;
@@ -607,7 +611,7 @@ __global__ void __launch_bounds__(B ? B : 256, grad_blocks(V, P, B, BIAS))
   constexpr bool BLOCK = B > 0;
   extern __shared__ __align__(16) char smem[];
   __shared__ __align__(16) float red[2 * 64];
-  __shared__ float joined[BLOCK ? 1 : 4 * 32 * P * V];
+  __shared__ float joined[JOINED<V, P, BLOCK>];
   int turn = 0;
   follow();
   const Place<BLOCK> pl;
@@ -848,6 +852,10 @@ __global__ void __launch_bounds__(32 * SUM_LANES) k_residual_norm_sums(ResNormAr
 }
 
 // ---- launches ------------------------------------------------------------------------------
+// Dynamic shared memory that a block may have; with the few hundred bytes of the kernels' own it is what
+// an SM gives to one.
+constexpr size_t ROOM = 226 << 10;
+
 // Elements of an access, packs of a thread, threads of a row; 0 packs: the wide form.
 struct Shape {
   int v, packs, threads;
@@ -890,7 +898,7 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   s.threads = s.block ? ((d + each - 1) / each + 31) / 32 * 32 : 32;
   s.rows = s.block ? 1 : 8;
   // two rows of each block lie in shared memory; wider ones are read again for each sum
-  const size_t b = type_bytes(type), w = type_bytes(wide), room = 226 << 10;
+  const size_t b = type_bytes(type), w = type_bytes(wide);
   const size_t nt = grad ? 3 : 2, nr = grad ? 2 : 1;
   auto matrix = [&](size_t of) {  // the bytes of two rows
     if (s.v == 1) return of == 2 ? 2 * s.rows * ((size_t)d * 2 + 32) : 0;
@@ -901,13 +909,13 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   // that registers are for
   const size_t threads = !grad ? 1024 : two ? 512 : s.v == 1 || biases ? 576 : 768;
   size_t most = 2;  // blocks of an SM
-  if (s.threads > 1024 || bytes > room) {
+  if (s.threads > 1024 || bytes > ROOM) {
     s.packs = 0;
     s.threads = WIDE;
     s.block = true;
     s.rows = 1;
   } else {
-    most = std::max<size_t>(1, std::min(room / (bytes + 5120), threads / (s.threads * s.rows)));
+    most = std::max<size_t>(1, std::min(ROOM / (bytes + 5120), threads / (s.threads * s.rows)));
   }
   s.grid = (unsigned)std::min<int64_t>((a.n + s.rows - 1) / s.rows, (int64_t)num_sms * (int64_t)most);
   const int64_t chain = (a.n + (int64_t)s.grid * s.rows - 1) / ((int64_t)s.grid * s.rows);
@@ -915,11 +923,12 @@ Shape shape_of(const ResNormArgs& a, int32_t type, int32_t wide, bool grad, int 
   return s;
 }
 
-// Two rows of each of a block's lie in shared memory.
+// Two rows of each of a block's lie in shared memory.  own: what the kernel has without asking.  The limit is
+// the kernel's on the device and not the call's, so it is the same each time, whatever other threads launch.
 template <typename K, typename... A>
-cudaError_t start(K kernel, const Shape& h, size_t stage, size_t held, cudaStream_t s, A... args) {
+cudaError_t start(K kernel, size_t own, const Shape& h, size_t stage, size_t held, cudaStream_t s, A... args) {
   const size_t bytes = 2 * stage + held * h.threads * h.rows;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(ROOM - own));
   if (e != cudaSuccess) return e;
   return launch_following(kernel, dim3(h.grid), h.threads * h.rows, bytes, s, args...);
 }
@@ -927,10 +936,10 @@ cudaError_t start(K kernel, const Shape& h, size_t stage, size_t held, cudaStrea
 template <typename T, typename R, int V, int P>
 cudaError_t forward_in(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   const size_t stage = stage_bytes<T, R, V, P>(2, 1, a.d, h.threads * h.rows, h.block);
-  if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, h, stage, HELD_BYTES<V, P>, s, a);
+  if (!h.block) return start(k_residual_norm<T, R, V, P, 0>, 0, h, stage, HELD_BYTES<V, P>, s, a);
   if constexpr (P <= 2 || V == 1) {  // four vectors a thread are a warp's
-    if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, h, stage, HELD_BYTES<V, P>, s, a);
-    return start(k_residual_norm<T, R, V, P, 1024>, h, stage, HELD_BYTES<V, P>, s, a);
+    if (h.threads <= 256) return start(k_residual_norm<T, R, V, P, 256>, 0, h, stage, HELD_BYTES<V, P>, s, a);
+    return start(k_residual_norm<T, R, V, P, 1024>, 0, h, stage, HELD_BYTES<V, P>, s, a);
   }
   return cudaErrorInvalidValue;
 }
@@ -947,7 +956,7 @@ cudaError_t forward(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
 template <typename T, typename R, int V, int P, int B, bool BIAS>
 cudaError_t backward_of(const ResNormArgs& a, const Shape& h, cudaStream_t s) {
   const size_t stage = stage_bytes<T, R, V, P>(3, 2, a.d, h.threads * h.rows, h.block);
-  return start(k_residual_norm_grad<T, R, V, P, B, BIAS>, h, stage, HELD_BYTES<V, P>, s, a, h.slots);
+  return start(k_residual_norm_grad<T, R, V, P, B, BIAS>, JOINED<V, P, (B > 0)> * sizeof(float), h, stage, HELD_BYTES<V, P>, s, a, h.slots);
 }
 template <typename T, typename R, int V, bool BIAS>
 cudaError_t backward_as(const ResNormArgs& a, const Shape& h, cudaStream_t s) {

@@ -2,6 +2,8 @@
 // through which they are joined, the gates, and the copies of rows into shared memory.
 #pragma once
 
+#include <algorithm>
+
 #include "gba_worker.cuh"
 
 namespace gba {
@@ -503,11 +505,13 @@ __device__ __forceinline__ void into_segment(Joint<TX, STEPS>& j, const ScanPlan
   __syncthreads();
 }
 
+// at_least, at_most: the shared memory of this launch, where it is more than S, and of any of the kernel's.  The limit is
+// the kernel's on the device and not the call's, so it is the same each time, whatever other threads launch.
 template <typename S, typename K>
 inline cudaError_t start_scan(K kernel, unsigned blocks, const ScanArgs& a, const ScanPlan& p, cudaStream_t s,
-                              size_t at_least = 0) {
-  const size_t bytes = at_least > sizeof(S) ? at_least : sizeof(S);
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+                              size_t at_least = 0, size_t at_most = 0) {
+  const size_t bytes = std::max(at_least, sizeof(S)), limit = std::max(at_most, sizeof(S));
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
   if (e != cudaSuccess) return e;
   return launch_following(kernel, dim3(blocks), SCAN_THREADS, bytes, s, a, p);
 }

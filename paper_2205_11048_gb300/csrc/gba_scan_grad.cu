@@ -192,9 +192,10 @@ cudaError_t start(const ScanArgs& a, const ScanPlan& p, cudaStream_t s) {
   }
   // One or two blocks for each SM ask for so much shared memory that they are spread evenly: 256 blocks,
   // of which three fit an SM, took 522 us, and two an SM 413.
+  constexpr size_t ONE = 226 << 10;
   const uint32_t blocks = p.n_segs * p.n_cols, each = (blocks + p.num_sms - 1) / p.num_sms;
   return start_scan<Shared<T, O, TX, STEPS, LOOSE, false>>(k_scan_grad<T, O, TX, STEPS, LOOSE, false>, blocks, a, p, s,
-                                                           each == 1 ? 226 << 10 : each == 2 ? 112 << 10 : 0);
+                                                           each == 1 ? ONE : each == 2 ? 112 << 10 : 0, ONE);
 }
 
 template <typename T, typename O>
