@@ -750,14 +750,17 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_grad_wide(ResNormArgs a,
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
     const float4 st = a.stats[row];
     float s[2] = {0.f, 0.f}, q[2] = {0.f, 0.f};
-    float w[1], b[1];
+    auto param = [&](const void* p, int c, float fill) {
+      float w[1];
+      params<1>(p, a.param_type, c, fill, w);
+      return w[0];
+    };
     if (a.dy.p) {
       for (int c = threadIdx.x; c < a.d; c += WIDE) {
-        params<1>(a.pre_weight, a.param_type, c, 1.f, w);
-        const float dy = to_float(at<T>(a.dy, row)[c]);
+        const float dy = to_float(at<T>(a.dy, row)[c]), gy = dy * param(a.pre_weight, c, 1.f);
         const float zh = (to_float(at<R>(a.zin, row)[c]) - st.z) * st.w;
-        s[0] = fmaf(dy * w[0], zh, s[0]);
-        s[1] += dy * w[0];
+        s[0] = fmaf(gy, zh, s[0]);
+        s[1] += gy;
         if (a.sums[2]) slot[2 * (int64_t)a.d + c] += dy * zh;
         if (a.sums[3]) slot[3 * (int64_t)a.d + c] += dy;
       }
@@ -768,20 +771,18 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_grad_wide(ResNormArgs a,
     auto D_of = [&](int c) {
       float D = 0.f;
       if (a.dy.p) {
-        params<1>(a.pre_weight, a.param_type, c, 1.f, w);
         const float zh = (to_float(at<R>(a.zin, row)[c]) - st.z) * st.w;
-        D = st.w * (to_float(at<T>(a.dy, row)[c]) * w[0] - s[1] - zh * s[0]);
+        D = st.w * (to_float(at<T>(a.dy, row)[c]) * param(a.pre_weight, c, 1.f) - s[1] - zh * s[0]);
       }
       return a.dz.p ? D + to_float(at<R>(a.dz, row)[c]) : D;
     };
-    auto e_of = [&](int c, float D, float& dg, float xh) {
+    // e and dg of column c, whose post weight is w
+    auto e_of = [&](int c, float D, float xh, float w, float& dg) {
       float e = a.bscale * D;
-      params<1>(a.post_weight, a.param_type, c, 1.f, w);
       if (a.gate != GBA_GATE_NONE) {
-        params<1>(a.post_bias, a.param_type, c, 0.f, b);
         float slope;
         const float act = gate_of(a.gate, to_float(at<T>(a.g, row)[c]), slope);
-        dg = e * fmaf(xh, w[0], b[0]) * slope;
+        dg = e * fmaf(xh, w, param(a.post_bias, c, 0.f)) * slope;
         e *= act;
       }
       return e;
@@ -789,8 +790,8 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_grad_wide(ResNormArgs a,
     float dg = 0.f;
     if (a.post != GBA_NORM_NONE) {
       for (int c = threadIdx.x; c < a.d; c += WIDE) {
-        const float xh = (to_float(at<T>(a.x, row)[c]) - st.x) * st.y;
-        const float gu = e_of(c, D_of(c), dg, xh) * w[0];
+        const float w = param(a.post_weight, c, 1.f), xh = (to_float(at<T>(a.x, row)[c]) - st.x) * st.y;
+        const float gu = e_of(c, D_of(c), xh, w, dg) * w;
         q[0] = fmaf(gu, xh, q[0]);
         q[1] += gu;
       }
@@ -800,13 +801,13 @@ __global__ void __launch_bounds__(WIDE) k_residual_norm_grad_wide(ResNormArgs a,
     }
     // dr may be dz: an element is read for the last time before it is written
     for (int c = threadIdx.x; c < a.d; c += WIDE) {
-      const float D = D_of(c), xh = (to_float(at<T>(a.x, row)[c]) - st.x) * st.y;
-      const float e = e_of(c, D, dg, xh);
+      const float D = D_of(c), w = param(a.post_weight, c, 1.f), xh = (to_float(at<T>(a.x, row)[c]) - st.x) * st.y;
+      const float e = e_of(c, D, xh, w, dg);
       if (a.sums[0]) slot[c] += e * xh;
       if (a.sums[1]) slot[(int64_t)a.d + c] += e;
       if (a.dr.p) at<R>(a.dr, row)[c] = from_float<R>(a.rscale * D);
       if (a.g.p) at<T>(a.dg, row)[c] = from_float<T>(dg);
-      at<T>(a.dx, row)[c] = from_float<T>(st.y * (e * w[0] - q[1] - xh * q[0]));
+      at<T>(a.dx, row)[c] = from_float<T>(st.y * (e * w - q[1] - xh * q[0]));
     }
     if (++chain == CHAIN) {
       slot += 4 * (int64_t)a.d;
