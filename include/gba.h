@@ -640,7 +640,7 @@ typedef struct {
 typedef struct {
   double lr; /* >= 0 */
   double beta1, beta2; /* within [0, 1) */
-  double eps;          /* > 0 */
+  double eps;          /* >= 2^-126 */
   const float* lr_now; /* device float32 that takes lr's place (NULL: lr), for captured calls */
   const float* norm;   /* device float32, the norm of all gradients (NULL: no clipping) */
   float max_norm;      /* >= 0; with norm */

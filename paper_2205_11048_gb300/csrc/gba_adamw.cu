@@ -166,11 +166,12 @@ __device__ __forceinline__ void moments(const Step& h, float g, float& m, float&
   m = __fadd_rn(__fmul_rn(m, h.beta1), __fmul_rn(g, h.rest1));
   v = __fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2));
 }
-// The root and the quotient by the hardware's approximations (2^-23 of themselves; a v below the
-// normal numbers counts as 0, beside eps): what the moments round to does not depend on them.
+// The root and the quotient by the hardware's approximations (2^-23 and 2^-22 of themselves, with a
+// denominator of at least eps, which is a normal number): what the moments round to does not depend on
+// them.  A v below the normal numbers has its root, because eps may be smaller than that.
 __device__ __forceinline__ float moved(const Step& h, float keep, float w, float m, float v) {
   float root;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
   return fmaf(keep, w, -h.size * __fdividef(m, fmaf(root, h.root, h.eps)));
 }
 

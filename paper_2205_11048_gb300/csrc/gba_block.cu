@@ -2,6 +2,7 @@
 // kernels are in gba_resnorm.cu, gba_scan.cu and gba_adamw.cu.
 #include <cuda_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <initializer_list>
 
@@ -350,7 +351,7 @@ gba_status gba_adamw(gba_worker* w, const gba_adamw_part* parts, int32_t n_parts
   if (!bad && !d) bad = "the description is NULL";
   if (!bad && !(d->lr >= 0.0 && std::isfinite((float)d->lr))) bad = "lr is negative or not finite";
   if (!bad && !(d->beta1 >= 0.0 && d->beta1 < 1.0 && d->beta2 >= 0.0 && d->beta2 < 1.0)) bad = "a beta outside [0, 1)";
-  if (!bad && !((float)d->eps > 0.f && std::isfinite((float)d->eps))) bad = "eps is not positive";
+  if (!bad && !((float)d->eps >= FLT_MIN && std::isfinite((float)d->eps))) bad = "eps is below 2^-126 or not finite";
   if (!bad && d->norm && !(d->max_norm >= 0.f)) bad = "max_norm is negative or NaN";
   if (!bad) bad = bad_floats(d->norm);
   if (!bad) bad = bad_floats(d->lr_now);
