@@ -167,9 +167,12 @@ __global__ void __launch_bounds__(SCAN_THREADS, SCAN_BLOCKS) k_scan(ScanArgs a, 
     if (a.decay == GBA_DECAY_SIGMOID) {
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], B[i]);
+    } else if (a.tied) {
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) log_gates<true>(here.f.get(i, at), A[i], B[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) log_gates(here.f.get(i, at), a.tied, A[i], B[i]);
+      for (int i = 0; i < STEPS; ++i) log_gates<false>(here.f.get(i, at), A[i], B[i]);
     }
     if (a.tied) {
 #pragma unroll

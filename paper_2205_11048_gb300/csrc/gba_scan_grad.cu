@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
       for (int i = 0; i < STEPS && row - i >= lo; ++i) {
         const int32_t m = here.marks.get(plan, at, i, row - i);
         Vec g, rest, dy = here.dy.get(i, at);
-        gates(a.decay, false, here.f.get(i, at), g, rest);
+        gates(a.decay, here.f.get(i, at), g, rest);
         if (m >= 0 && (m & LAST) && a.state && in) dy = dy + state_row<TX, LOOSE>(a.state, a.state_stride, m, at.c, a.d);
         dy = g * dy;
         if (m < 0) dy.fill(0.f);
@@ -107,9 +107,12 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
       if (a.decay == GBA_DECAY_SIGMOID) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], R[i]);
+      } else if (a.tied) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) log_gates<true>(here.f.get(i, at), A[i], R[i]);
       } else {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) log_gates(here.f.get(i, at), a.tied, A[i], R[i]);
+        for (int i = 0; i < STEPS; ++i) log_gates<false>(here.f.get(i, at), A[i], R[i]);
       }
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) mine.then(A[i], A[i] * here.dy.get(i, at), false);
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
             continue;
           }
           Vec g, rest, h = here.y.get(i, at);
-          gates(a.decay, a.tied, here.f.get(i, at), g, rest);
+          gates(a.decay, here.f.get(i, at), g, rest);
           if ((m & FIRST) && in) h = state_row<TX, LOOSE>(a.h0, a.h0_stride, m, at.c, a.d);
           if ((m & LAST) && in) v = state_row<TX, LOOSE>(a.state, a.state_stride, m, at.c, a.d);
           outputs(i, g, rest, h);
