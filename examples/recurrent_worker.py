@@ -49,7 +49,8 @@ class Recurrent:
         self.before = B.residual_norm(pre_norm="rms", pre_weight=self.first)
         self.weights = [self.first] + [b[k] for b in self.blocks for k in ("into", "out", "post", "pre")]
         decays = [0.01 if w.dim() == 2 else 0.0 for w in self.weights]
-        self.states = B.adamw_states(self.weights, bits=8, betas=(0.9, 0.99), weight_decay=decays)
+        self.states = B.adamw_states(self.weights, bits=8, betas=(0.9, 0.99), weight_decay=decays,
+                                     rounding="chance")
 
     def forward(self, ids, seq, states=None):
         """The last block's normed output, the blocks' last states, and what the gradient needs."""

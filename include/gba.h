@@ -637,6 +637,14 @@ typedef struct {
   float weight_decay; /* >= 0 */
 } gba_adamw_part;
 
+/* How gba_adamw rounds states to 8 bits.  NEAREST: to the nearest code.  A step that moves a value by less
+ * than half of a code's (3% of it) is then lost for good: where a gradient gets smaller while the largest of
+ * its 256 elements does not, v (and with beta1 above 0.93 or so, and for the smallest values, m) stays up to
+ * its old size, and its weights move too slowly.  CHANCE: up or down to one of the two codes next to it, at
+ * chances that give the value on average, so nothing is lost.  Chances come from the step, the part's place
+ * in the list and the element, so equal calls give equal bits. */
+typedef enum { GBA_ROUND_NEAREST = 0, GBA_ROUND_CHANCE = 1 } gba_rounding;
+
 typedef struct {
   double lr; /* >= 0 */
   double beta1, beta2; /* within [0, 1) */
@@ -644,6 +652,7 @@ typedef struct {
   const float* lr_now; /* device float32 that takes lr's place (NULL: lr), for captured calls */
   const float* norm;   /* device float32, the norm of all gradients (NULL: no clipping) */
   float max_norm;      /* >= 0; with norm */
+  int32_t rounding;    /* gba_rounding, of states in 8 bits */
 } gba_adamw_desc;
 
 /*
@@ -654,8 +663,8 @@ typedef struct {
  * step       device int64, the steps taken so far; the call adds 1.
  * With a norm that is infinite or NaN the call changes nothing, *step neither (copies are
  * not written).  Without norm a gradient that is infinite or NaN spoils its element, in 8
- * bits up to the 256 elements that share its scales.  *step >= 0.  8-bit states are rounded to the nearest code; the weights move by m and v
- * from before that rounding, and a v above 0 does not become 0.  The description may be
+ * bits up to the 256 elements that share its scales.  *step >= 0.  The weights move by m and v from before
+ * their rounding to 8 bits, and a v above 0 does not become 0.  The description may be
  * reused or freed when the call returns (a captured call keeps the addresses in it).  No
  * array may overlap another.
  * gba_adamw_values - the states of the parts as float32: m_out[i] and v_out[i] receive

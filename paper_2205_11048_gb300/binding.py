@@ -33,6 +33,7 @@ F32, BF16, F16 = 0, 1, 2
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 GATES = {"none": 0, "mul": 1, "sigmoid": 2, "silu": 3}
 DECAYS = {"sigmoid": 0, "log": 1}
+ROUNDINGS = {"nearest": 0, "chance": 1}
 NO_PAD = -2**63
 INT32_MAX = 2**31 - 1
 KERNEL_NAMES = ["weights", "sort_hist", "sort_pass", "seg_scan", "row_long", "row_apply",
@@ -116,7 +117,7 @@ class gba_adamw_part(ctypes.Structure):
 class gba_adamw_desc(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("lr_now", ctypes.c_void_p), ("norm", ctypes.c_void_p),
-                ("max_norm", ctypes.c_float)]
+                ("max_norm", ctypes.c_float), ("rounding", ctypes.c_int32)]
 
 
 _P = ctypes.c_void_p
@@ -715,14 +716,20 @@ def sequences(n, lengths=None, offsets=None):
 class AdamWStates:
     """AdamW's states of a list of weights, which it holds: m and v (lists of float32 tensors, or
     of uint8 with 8 bits and their m_scale and v_scale), step (a device int64) and, if given,
-    copies of the weights that follow them.  States that are not given start as zeros."""
+    copies of the weights that follow them.  States that are not given start as zeros.  With 8
+    bits and rounding "nearest" a state does not follow changes of a few per cent a step, so
+    where a weight's gradient gets small beside those of its 256 neighbours its second moment
+    stays large; with "chance" states are right on average (see gba_rounding in include/gba.h)."""
 
     def __init__(self, weights, bits=32, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, copies=None, m=None, v=None,
-                 m_scale=None, v_scale=None, step=None):
+                 m_scale=None, v_scale=None, step=None, rounding="nearest"):
         import torch
         self.weights = list(weights)
         if bits not in (32, 8):
             _refuse("states have 32 or 8 bits")
+        if rounding not in ROUNDINGS or (bits == 32 and rounding != "nearest"):
+            _refuse(f"roundings of states in 8 bits are one of {list(ROUNDINGS)}")
+        self.rounding = rounding
         self.bits, self.betas, self.eps = bits, (float(betas[0]), float(betas[1])), float(eps)
         n = len(self.weights)
         self.device = self.weights[0].get_device() if n else None
@@ -1128,7 +1135,7 @@ class Worker:
         self._mine(now, norm)
         desc = gba_adamw_desc(0.0 if now is not None else lr, *st.betas, st.eps,
                               None if now is None else now.data_ptr(), None if norm is None else norm.data_ptr(),
-                              0.0 if max_norm is None else max_norm)
+                              0.0 if max_norm is None else max_norm, ROUNDINGS[st.rounding])
         self._call("gba_adamw", parts.array, parts.n, desc, st.step.data_ptr())
 
     def adamw_values(self, parts, m_out=None, v_out=None):

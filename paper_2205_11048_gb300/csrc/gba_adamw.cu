@@ -10,6 +10,8 @@
 // is rounded once.
 // 64 10^6 float32 weights in 148 tensors with bf16 gradients and copies: 314 us, 5.70 TB/s; with 8-bit
 // states 178 us, 5.77 TB/s, and 147 us for reading them as float32 (4.4 TB/s: 128 MB in, 512 MB out).
+// States rounded by chance: 239 us against 176 to the nearest (64 tensors), for a counter's hash an element;
+// instructions bound it then.
 // 306,496 weights: 6 us, a launch.  Four blocks an SM: three took 323 us,
 // five 312 and, in 8 bits, 198.
 #include <cuda_fp8.h>
@@ -40,6 +42,7 @@ struct Part {
   uint32_t first;  // its first piece
   float decay;
   int8_t type, grad_type, copy_type, vec;  // vec: every array lies on 16-byte boundaries
+  uint32_t number;  // its place in the caller's list
 };
 
 template <int CAP>
@@ -150,6 +153,22 @@ __device__ __forceinline__ uint32_t v_code(float q) {
   const int c = (int)((b + 0x7FFFFu + ((b >> 20) & 1u)) >> 20) - 768;
   return q > 0.f ? (uint32_t)min(max(c, 1), 255) : 0u;
 }
+// To one of the two codes next to a value, up or down, so that it is the value on average: a code's step is
+// added `by` 2^20ths and what is left over is cut off.  Below 2^-6 the steps of m are 2^-9; what is above its
+// largest value, infinite or no number is left to m_code.
+__device__ __forceinline__ float m_cut(float q, uint32_t by) {
+  const float a = fabsf(q);
+  float x = a;
+  if (a < 0x1p-6f)
+    x = floorf(fmaf((float)by, 0x1p-20f, a * 512.f)) * 0x1p-9f;
+  else if (a <= 448.f)
+    x = __uint_as_float((__float_as_uint(a) + by) & ~0xFFFFFu);
+  return copysignf(x, q);
+}
+__device__ __forceinline__ uint32_t v_code_cut(float q, uint32_t by) {
+  const int c = (int)((__float_as_uint(q) + by) >> 20) - 768;
+  return q > 0.f ? (uint32_t)min(max(c, 1), 255) : 0u;
+}
 __device__ __forceinline__ float block_scale(float most, float share) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -159,7 +178,15 @@ __device__ __forceinline__ float block_scale(float most, float share) {
 struct Step {
   float c, size, root, eps, lr;
   float beta1, rest1, beta2, rest2;
+  uint64_t key;  // of this step's chances
 };
+
+// The chances of element i of a part, 20 bits for m and for v: by counters, so a call has no state of its own.
+__device__ __forceinline__ void chances(const Step& h, const Part& p, int64_t i, uint32_t& m, uint32_t& v) {
+  const uint64_t r = splitmix64(h.key ^ ((uint64_t)p.number << 40 | (uint64_t)i));
+  m = (uint32_t)r & 0xFFFFFu;
+  v = (uint32_t)(r >> 44);
+}
 
 __device__ __forceinline__ void moments(const Step& h, float g, float& m, float& v) {
   g = __fmul_rn(g, h.c);
@@ -176,7 +203,7 @@ __device__ __forceinline__ float moved(const Step& h, float keep, float w, float
 }
 
 // A warp's block of 256 elements from `at` on, all of them there and in vectors.
-template <int BITS>
+template <int BITS, bool CHANCE>
 __device__ __forceinline__ void whole_block(const Part& p, const Step& h, int64_t at) {
   const int lane = threadIdx.x & 31;
   const int64_t i = at + lane * V;
@@ -223,7 +250,17 @@ __device__ __forceinline__ void whole_block(const Part& p, const Step& h, int64_
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       m[j] = __fmul_rn(m[j], mi);
-      cv[j / 4] |= v_code(__fmul_rn(v[j], vi)) << (j % 4 * 8);
+      v[j] = __fmul_rn(v[j], vi);
+      uint32_t c;
+      if constexpr (CHANCE) {
+        uint32_t bm, bv;
+        chances(h, p, i + j, bm, bv);
+        m[j] = m_cut(m[j], bm);
+        c = v_code_cut(v[j], bv);
+      } else {
+        c = v_code(v[j]);
+      }
+      cv[j / 4] |= c << (j % 4 * 8);
     }
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.m) + i) = m_codes(m);
     *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.v) + i) = make_uint2(cv[0], cv[1]);
@@ -233,7 +270,7 @@ __device__ __forceinline__ void whole_block(const Part& p, const Step& h, int64_
 
 // The same of a part's last elements, and of parts that lie anywhere: element by element,
 // neighbouring lanes at neighbouring ones.
-template <int BITS>
+template <int BITS, bool CHANCE>
 __device__ __forceinline__ void loose_block(const Part& p, const Step& h, int64_t at) {
   const int lane = threadIdx.x & 31;
   const float keep = fmaf(-h.lr, p.decay, 1.f);
@@ -273,8 +310,15 @@ __device__ __forceinline__ void loose_block(const Part& p, const Step& h, int64_
         static_cast<float*>(p.m)[i] = m[j];
         static_cast<float*>(p.v)[i] = v[j];
       } else {
-        static_cast<uint8_t*>(p.m)[i] = (uint8_t)m_code(__fmul_rn(m[j], mi));
-        static_cast<uint8_t*>(p.v)[i] = (uint8_t)v_code(__fmul_rn(v[j], vi));
+        m[j] = __fmul_rn(m[j], mi);
+        v[j] = __fmul_rn(v[j], vi);
+        uint32_t bm = 0u, bv = 0u;
+        if constexpr (CHANCE) {
+          chances(h, p, i, bm, bv);
+          m[j] = m_cut(m[j], bm);
+        }
+        static_cast<uint8_t*>(p.m)[i] = (uint8_t)m_code(m[j]);
+        static_cast<uint8_t*>(p.v)[i] = (uint8_t)(CHANCE ? v_code_cut(v[j], bv) : v_code(v[j]));
       }
     }
   }
@@ -283,7 +327,7 @@ __device__ __forceinline__ void loose_block(const Part& p, const Step& h, int64_
 constexpr int PIECE = THREADS * V;  // elements of a block of threads
 
 // last: the last launch of the call, whose last block counts the step
-template <int CAP, int BITS>
+template <int CAP, int BITS, bool CHANCE>
 __global__ void __launch_bounds__(THREADS, BLOCKS)
     k_adamw(const __grid_constant__ PartList<CAP> l, AdamWArgs a, bool last) {
   __shared__ Step s_step;
@@ -301,6 +345,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS)
     h.root = 1.f / sqrtf(-expm1f((float)((double)t * a.log2)));
     h.eps = a.eps;
     h.beta1 = a.beta1, h.rest1 = a.rest1, h.beta2 = a.beta2, h.rest2 = a.rest2;
+    h.key = CHANCE ? splitmix64((uint64_t)t) : 0u;
     s_step = h;
   }
   __syncthreads();
@@ -313,9 +358,9 @@ __global__ void __launch_bounds__(THREADS, BLOCKS)
     const int64_t at = (int64_t)(c - p.first) * PIECE + (threadIdx.x >> 5) * BLOCK;
     if (at >= p.n) continue;
     if (p.vec && at + BLOCK <= p.n)
-      whole_block<BITS>(p, h, at);
+      whole_block<BITS, CHANCE>(p, h, at);
     else
-      loose_block<BITS>(p, h, at);
+      loose_block<BITS, CHANCE>(p, h, at);
   }
   if (!last) return;
   __syncthreads();
@@ -387,6 +432,7 @@ __global__ void __launch_bounds__(THREADS) k_adamw_values(const __grid_constant_
 }
 
 constexpr int CAP_MOST = 384;
+static_assert(sizeof(Part) == 80, "no more than an aligned one has to be");
 static_assert(sizeof(PartList<CAP_MOST>) + sizeof(AdamWArgs) + 16 <= 32764, "the limit of a kernel's parameters");
 static_assert(sizeof(ValueList<CAP_MOST>) <= 32764, "the limit of a kernel's parameters");
 
@@ -409,7 +455,7 @@ PartList<CAP> list_of(const gba_adamw_part* parts, int32_t n_parts, int32_t bits
     if (l.count == CAP || (l.count > 0 && pieces + more >= (1ull << 31))) break;
     l.part[l.count++] = Part{p.weight, p.grad, p.m, p.v, p.m_scale, p.v_scale, p.copy, p.n, (uint32_t)pieces,
                              p.weight_decay, (int8_t)p.type, (int8_t)p.grad_type, (int8_t)p.copy_type,
-                             (int8_t)aligned(p)};
+                             (int8_t)aligned(p), (uint32_t)at};
     pieces += more;
   }
   l.pieces = (uint32_t)pieces;
@@ -422,7 +468,7 @@ bool any_left(const gba_adamw_part* parts, int32_t n_parts, int32_t bits, int32_
   return false;
 }
 
-template <int CAP, int BITS>
+template <int CAP, int BITS, bool CHANCE>
 cudaError_t run_as(const gba_adamw_part* parts, int32_t n_parts, const AdamWArgs& a, bool last, int num_sms,
                    cudaStream_t s) {
   int32_t at = 0;
@@ -430,18 +476,18 @@ cudaError_t run_as(const gba_adamw_part* parts, int32_t n_parts, const AdamWArgs
     const PartList<CAP> l = list_of<CAP>(parts, n_parts, BITS, at);
     const unsigned grid = std::min(std::max(l.pieces, 1u), (unsigned)(num_sms * BLOCKS));
     const bool end = last && !any_left(parts, n_parts, BITS, at);
-    const cudaError_t e = launch_following(k_adamw<CAP, BITS>, dim3(grid), THREADS, 0, s, l, a, end);
+    const cudaError_t e = launch_following(k_adamw<CAP, BITS, CHANCE>, dim3(grid), THREADS, 0, s, l, a, end);
     if (e != cudaSuccess) return e;
   } while (any_left(parts, n_parts, BITS, at));
   return cudaSuccess;
 }
 
-template <int BITS>
+template <int BITS, bool CHANCE>
 cudaError_t run(const gba_adamw_part* parts, int32_t n_parts, const AdamWArgs& a, bool last, int num_sms,
                 cudaStream_t s) {
-  return n_parts <= 16 ? run_as<16, BITS>(parts, n_parts, a, last, num_sms, s)
-                       : n_parts <= 160 ? run_as<160, BITS>(parts, n_parts, a, last, num_sms, s)
-                                        : run_as<CAP_MOST, BITS>(parts, n_parts, a, last, num_sms, s);
+  return n_parts <= 16 ? run_as<16, BITS, CHANCE>(parts, n_parts, a, last, num_sms, s)
+                       : n_parts <= 160 ? run_as<160, BITS, CHANCE>(parts, n_parts, a, last, num_sms, s)
+                                        : run_as<CAP_MOST, BITS, CHANCE>(parts, n_parts, a, last, num_sms, s);
 }
 
 template <int CAP>
@@ -476,10 +522,12 @@ cudaError_t values_as(const gba_adamw_part* parts, int32_t n_parts, float* const
 cudaError_t launch_adamw(const gba_adamw_part* parts, int32_t n_parts, AdamWArgs a, int num_sms, cudaStream_t s) {
   const bool wide = any_left(parts, n_parts, 32, 0), narrow = any_left(parts, n_parts, 8, 0);
   if (wide || !narrow) {
-    const cudaError_t e = run<32>(parts, n_parts, a, !narrow, num_sms, s);
+    const cudaError_t e = run<32, false>(parts, n_parts, a, !narrow, num_sms, s);
     if (e != cudaSuccess) return e;
   }
-  return narrow ? run<8>(parts, n_parts, a, true, num_sms, s) : cudaSuccess;
+  if (!narrow) return cudaSuccess;
+  return a.rounding == GBA_ROUND_CHANCE ? run<8, true>(parts, n_parts, a, true, num_sms, s)
+                                        : run<8, false>(parts, n_parts, a, true, num_sms, s);
 }
 
 cudaError_t launch_adamw_values(const gba_adamw_part* parts, int32_t n_parts, float* const* m_out,

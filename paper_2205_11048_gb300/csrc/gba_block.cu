@@ -353,6 +353,7 @@ gba_status gba_adamw(gba_worker* w, const gba_adamw_part* parts, int32_t n_parts
   if (!bad && !(d->beta1 >= 0.0 && d->beta1 < 1.0 && d->beta2 >= 0.0 && d->beta2 < 1.0)) bad = "a beta outside [0, 1)";
   if (!bad && !((float)d->eps >= FLT_MIN && std::isfinite((float)d->eps))) bad = "eps is below 2^-126 or not finite";
   if (!bad && d->norm && !(d->max_norm >= 0.f)) bad = "max_norm is negative or NaN";
+  if (!bad && d->rounding != GBA_ROUND_NEAREST && d->rounding != GBA_ROUND_CHANCE) bad = "unknown rounding";
   if (!bad) bad = bad_floats(d->norm);
   if (!bad) bad = bad_floats(d->lr_now);
   if (!bad && (!step || (uintptr_t)step % 8 != 0)) bad = "step is NULL or not 8-byte aligned";
@@ -380,6 +381,7 @@ gba_status gba_adamw(gba_worker* w, const gba_adamw_part* parts, int32_t n_parts
   a.norm = d->norm;
   a.max_norm = d->max_norm;
   a.step = step;
+  a.rounding = d->rounding;
   a.ticket = w->words + 1;
   const cudaError_t e = launch_adamw(parts, n_parts, a, w->num_sms, w->stream);
   return e == cudaSuccess ? GBA_OK : cuda_fail(w, e, "launch AdamW");

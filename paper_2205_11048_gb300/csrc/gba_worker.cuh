@@ -369,6 +369,7 @@ struct AdamWArgs {
   const float* norm;
   float max_norm;
   int64_t* step;
+  int32_t rounding;
   uint32_t* ticket;  // a zero word that is zero again afterwards
 };
 cudaError_t launch_adamw(const gba_adamw_part* parts, int32_t n_parts, AdamWArgs a, int num_sms, cudaStream_t s);
