@@ -492,7 +492,8 @@ gba_status gba_layer_norm_grad(gba_worker* w, const gba_matrix* dy, const gba_ma
  * information along the sequences, gba_residual_norm joins a block's output into the
  * residual stream and takes the norm for the next block, and gba_adamw updates the
  * weights that a worker keeps itself.  The conventions are those of the operators
- * above.
+ * above; matrices of one stride (in bytes) whose rows lie beside one another's, as columns
+ * of one wider matrix do, do not overlap.
  */
 
 /* The norm of a row: NONE; RMS, x / sqrt(mean(x^2) + eps); LAYER, the same of x minus

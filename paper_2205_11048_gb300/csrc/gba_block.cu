@@ -19,17 +19,31 @@ constexpr int64_t MAX_SEQUENCES = (1ll << 29) - 1;
 Rows in_rows(const gba_matrix* m) { return m ? Rows{m->data, m->stride} : Rows{nullptr, 0}; }
 OutRows out_rows(const gba_matrix* m) { return m ? OutRows{m->data, m->stride} : OutRows{nullptr, 0}; }
 
-// Memory that a call reads or writes.
+// Memory that a call reads or writes: rows of `row` bytes, `stride` bytes apart, of a matrix (0: bytes that follow
+// one another), `bytes` from the first to the end of the last.
 struct Range {
   const void* p;
-  uint64_t bytes;
+  uint64_t bytes, row = 0, stride = 0;
 };
-Range range(const gba_matrix* m) { return m ? Range{m->data, span(m)} : Range{nullptr, 0}; }
+Range range(const gba_matrix* m) {
+  if (!m) return Range{nullptr, 0};
+  const uint64_t b = type_bytes(m->type);
+  return Range{m->data, span(m), m->cols * b, m->stride * b};
+}
+
+// Do the rows of two matrices lie beside one another's, as those of columns of a wider matrix do?
+bool beside(const Range& a, const Range& b) {
+  if (a.row == 0 || a.stride != b.stride || b.row == 0) return false;
+  // where b's rows start from a's on, modulo the stride
+  const uint64_t ahead = (uintptr_t)b.p >= (uintptr_t)a.p ? ((uintptr_t)b.p - (uintptr_t)a.p) % a.stride
+                                                          : a.stride - 1 - ((uintptr_t)a.p - (uintptr_t)b.p - 1) % a.stride;
+  return ahead >= a.row && ahead + b.row <= a.stride;
+}
 
 // Does out overlap one of the others?
 bool meets(const Range& out, std::initializer_list<Range> others) {
   for (const Range& o : others)
-    if (out.p && o.p && overlap(out.p, out.bytes, o.p, o.bytes)) return true;
+    if (out.p && o.p && overlap(out.p, out.bytes, o.p, o.bytes) && !beside(out, o)) return true;
   return false;
 }
 
