@@ -127,7 +127,7 @@ void set_scan(ScanArgs& a, const gba_worker* w, const gba_scan* s, const gba_mat
 }
 
 gba_status run_scan(gba_worker* w, const ScanArgs& a, int32_t type, int32_t out_type, bool grad) {
-  if (a.n == 0 && (a.n_seq == 0 || !a.last)) return GBA_OK;
+  if (a.n == 0 && (a.n_seq == 0 || !(a.last || a.offsets || a.lengths))) return GBA_OK;
   const gba_status st = reserve(w, scan_workspace(a, type, out_type, grad, w->num_sms));
   if (st != GBA_OK) return st;
   const cudaError_t e = launch_scan(a, type, out_type, grad, w->ws, w->num_sms, w->stream);

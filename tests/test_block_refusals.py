@@ -3,7 +3,7 @@ test_block_host.py, whose library it uses)."""
 import pytest
 
 from paper_2205_11048_gb300 import binding as B
-from tests.test_block_host import AT, F, T, adamw, mat, narrow, norm, norm_grad, part, place, scan, scan_grad, w  # noqa: F401
+from tests.test_block_host import AT, F, T, adamw, mat, narrow, norm, norm_grad, part, place, scan, scan_grad, scan_of, w  # noqa: F401
 
 
 @pytest.mark.parametrize("eps,status", [(2.0**-126, B.GBA_OK), (2.0**-127, B.GBA_E_ARG), (1e-44, B.GBA_E_ARG)])
@@ -59,3 +59,17 @@ def test_columns_of_one_matrix_are_apart(F, w, a, b, apart):  # noqa: F811
 def test_columns_are_not_apart_from_arrays(F, w):  # noqa: F811
     assert norm_grad(F, w, dx=column(0), sums=(WIDE + 32, None, None, None)) == B.GBA_E_ARG
     assert norm(F, w, y=column(0), stats=WIDE + 32) == B.GBA_E_ARG
+
+
+def test_the_sequences_of_a_call_without_rows_are_looked_at(F, w):  # noqa: F811
+    """Their offsets and lengths may be bad all the same, which only a kernel can see."""
+    e = dict(rows=0, data=None)
+    rows = {k: mat(0, **e) for k in ("x", "f", "y")}
+    back = {**rows, **{k: mat(0, **e) for k in ("dy", "dx", "df")}}
+    n = F.fake_block_launches()
+    for i, how in enumerate((dict(offsets=place(50)), dict(lengths=place(50)))):
+        assert scan(F, w, scan_of(**how), **rows, state=None, out=None) == B.GBA_OK
+        assert scan_grad(F, w, scan_of(**how), **back, ds=None, state=None, out=None) == B.GBA_OK
+        assert F.fake_block_launches() == n + 2 * i + 2
+    assert scan(F, w, scan_of(), **rows, state=None, out=None) == B.GBA_OK  # nothing to see and nothing to write
+    assert F.fake_block_launches() == n + 4
