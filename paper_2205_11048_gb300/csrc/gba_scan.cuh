@@ -109,40 +109,54 @@ __device__ __forceinline__ void sigmoid_gates(const Vec& forget, Vec& a, Vec& re
   a = fma_v(qv, ev, qv);
   rest = tv * a;
 }
-// The same of its logarithm g = min(f, 0).  Down to -0.69, from e = exp(g) - 1 = g / (1 - g/2 + g^2/12 - g^4/720 +
-// g^6/30240) (the series of Bernoulli's numbers, of which g^8 / 1,209,600 is left out: 0.5 U): one minus the decay
-// is -e, within 5.2 U of itself (U = 2^-24: 2.1 for the denominator, 2 for the hardware's reciprocal, 1 for the
-// product), and the decay 1 + e, rounded once.  By the hardware's power of two, off by 2^-22 of itself, a decay near
-// one forgot its memory by up to 1.6 U more or less a row, and the two did not add up to one.  Below -0.69 the power
-// of two is enough: what it is off does not add up.
-// bf16, 64 sequences of 1,024 x 2,048, untied 141 us against 135 without the series, tied 154 against 158 with a
-// polynomial for one minus the decay; split (262,144 x 256) 138 and 128, tied 151 and 152.  RESTS asked for at run
-// time cost 8 us; single floats instead of pairs 3.
+// The same of its logarithm g = min(f, 0).  By the hardware's power of two alone, off by 2^-22 of itself, a decay near
+// one forgets its memory by up to 1.6 U (U = 2^-24) more or less a row, and it and one minus it do not add up to one.
+// With RESTS (tied): down to -0.69 from e = exp(g) - 1 = g / (1 - g/2 + g^2/12 - g^4/720 + g^6/30240) (the series of
+// Bernoulli's numbers, of which g^8 / 1,209,600 is left out: 0.5 U).  One minus the decay is -e, within 5.2 U of itself
+// (2.1 for the denominator, 2 for the hardware's reciprocal, 1 for the product), and the decay 1 + e, rounded once.
+// Without: down to -1/16 exp's own series up to g^4, within 3 U of 1 - a, and rounded.
+// Further down the power of two is enough: what it is off adds up to 66 U at most.
+// bf16, with the power of two alone (and a polynomial of ten terms for one minus the decay) and so: 64 sequences of
+// 1,024 x 2,048 untied 135 and 134 us, tied 158 and 154; one of 262,144 x 256 128 and 130, 152 and 151.  The tied form
+// for both took 141 and 138 untied; RESTS asked for at run time 8 us more; single floats instead of pairs 3.
 template <bool RESTS>
 __device__ __forceinline__ void log_gates(const Vec& forget, Vec& a, Vec& rest) {
-  constexpr float NEAR = -0.69f;
+  constexpr float NEAR = RESTS ? -0.69f : -0.0625f;
   float f[V], e[V], g[V];
   forget.get(f);
 #pragma unroll
   for (int j = 0; j < V; ++j) f[j] = min_nan(f[j], 0.f);
 #pragma unroll
   for (int j = 0; j < V; j += 2) {
-    const f2 x = pair(f[j], f[j + 1]), s = mul2(x, x);
-    f2 p = fma2(s, pair(1.f / 30240.f, 1.f / 30240.f), pair(-1.f / 720.f, -1.f / 720.f));
-    p = fma2(s, p, pair(1.f / 12.f, 1.f / 12.f));
-    p = fma2(s, p, pair(1.f, 1.f));
-    p = fma2(x, pair(-0.5f, -0.5f), p);
+    const f2 x = pair(f[j], f[j + 1]);
+    f2 p;
+    if constexpr (RESTS) {
+      const f2 s = mul2(x, x);
+      p = fma2(s, pair(1.f / 30240.f, 1.f / 30240.f), pair(-1.f / 720.f, -1.f / 720.f));
+      p = fma2(s, p, pair(1.f / 12.f, 1.f / 12.f));
+      p = fma2(s, p, pair(1.f, 1.f));
+      p = fma2(x, pair(-0.5f, -0.5f), p);
+    } else {
+      p = fma2(x, pair(1.f / 24.f, 1.f / 24.f), pair(1.f / 6.f, 1.f / 6.f));
+      p = fma2(x, p, pair(0.5f, 0.5f));
+      p = fma2(x, p, pair(1.f, 1.f));
+      p = fma2(x, p, pair(1.f, 1.f));
+    }
     split(p, e[j], e[j + 1]);
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const float far = exp2_fast(f[j] * LOG2E);
-    e[j] = f[j] * rcp_fast(e[j]);
-    g[j] = f[j] < NEAR ? far : 1.f + e[j];
-    e[j] = f[j] < NEAR ? 1.f - far : -e[j];
+    if constexpr (RESTS) {
+      e[j] = f[j] * rcp_fast(e[j]);
+      g[j] = f[j] < NEAR ? far : 1.f + e[j];
+      e[j] = f[j] < NEAR ? 1.f - far : -e[j];
+    } else {
+      g[j] = f[j] < NEAR ? far : e[j];
+    }
   }
   a.set(g);
-  if (RESTS) rest.set(e);
+  if constexpr (RESTS) rest.set(e);
 }
 
 __device__ __forceinline__ void gates(int32_t decay, const Vec& forget, Vec& a, Vec& rest) {

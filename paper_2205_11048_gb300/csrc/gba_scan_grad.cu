@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, GRAD_BLOCKS) k_scan_grad(ScanArg
       if (a.decay == GBA_DECAY_SIGMOID) {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) sigmoid_gates(here.f.get(i, at), A[i], R[i]);
-      } else if (a.tied) {
+      } else if (!TAIL && a.tied) {  // a segment's pair has nothing of one minus the decay
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) log_gates<true>(here.f.get(i, at), A[i], R[i]);
       } else {
