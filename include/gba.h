@@ -366,8 +366,8 @@ typedef struct {
 /* gba_worker_create - a worker handle on the current device.  cuda_stream: the
  * stream of all its work (NULL: the legacy default stream).
  * gba_worker_sync - wait for the stream, then report what the kernels latched since
- * the last gba_worker_sync: GBA_E_ID_RANGE (an id out of range) or
- * GBA_E_DEVICE_TIMEOUT; the handle can be used on.
+ * the last gba_worker_sync: GBA_E_ID_RANGE (an id out of range), GBA_E_ARG (offsets or
+ * lengths of sequences) or GBA_E_DEVICE_TIMEOUT; the handle can be used on.
  * gba_worker_last_error - text of the handle's last failure ("" if none).
  * gba_worker_destroy - wait for the stream and free the workspaces (NULL: no-op);
  * graphs that hold calls of the handle must not run any more. */
@@ -524,7 +524,9 @@ typedef struct {
  *   u = post_norm(x) * post_weight + post_bias       (a scale per channel with NONE)
  *   z = residual_scale * residual + block_scale * act(gate) * u
  *   y = pre_norm(z) * pre_weight + pre_bias
- * y is formed from z before its rounding.
+ * y is formed from z before its rounding.  A gate's exponential is the hardware's: sigmoid
+ * and silu are within (1.3 |gate| + 10) 2^-24 of themselves (their slopes, in the gradient,
+ * of the sum of their terms), and below -86 within 1e-36.
  * x          the block's output.
  * residual   of x's shape, of x's type or float32 (NULL: no such term; then
  *            residual_scale is not used).
@@ -564,8 +566,10 @@ gba_status gba_residual_norm_grad(gba_worker* w, const gba_block* b, const gba_m
                                   const gba_matrix* dx, const gba_matrix* dresidual,
                                   const gba_matrix* dgate, const gba_block_grads* grads);
 
-/* How a forget gate f is given: SIGMOID, the decay is a = 1 / (1 + exp(-f)); LOG, it is
- * a = exp(min(f, 0)). */
+/* How a forget gate f is given: SIGMOID, the decay is a = 1 / (1 + exp(-f)), and f below -87
+ * counts as -87, whose decay is 1.6e-38; LOG, it is a = exp(min(f, 0)).  Exponentials are the
+ * hardware's, within (1.3 |f| + 5) 2^-24 of themselves, but what multiplies itself over a long
+ * memory, a decay near one, is rounded to the nearest or nearly so. */
 typedef enum { GBA_DECAY_SIGMOID = 0, GBA_DECAY_LOG = 1 } gba_decay;
 
 /* The gates of a gba_gated_scan and its sequences.  Without arrays every sequence has

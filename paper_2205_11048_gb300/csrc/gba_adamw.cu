@@ -8,10 +8,10 @@
 // scales over 256.  The moments are formed by one IEEE operation after another (no fused
 // multiply-add), so that which code a moment is rounded to follows from its formula; the weight
 // is rounded once.
-// 64 10^6 float32 weights in 148 tensors with bf16 gradients and copies: 314 us, 5.70 TB/s; with 8-bit
-// states 178 us, 5.77 TB/s, and 147 us for reading them as float32 (4.4 TB/s: 128 MB in, 512 MB out).
-// States rounded by chance: 239 us against 176 to the nearest (64 tensors), for a counter's hash an element;
-// instructions bound it then.
+// 64 10^6 float32 weights in 148 tensors with bf16 gradients and copies: 315 us, 5.70 TB/s; with 8-bit
+// states 179 us, 5.74 TB/s, and 147 us for reading them as float32 (4.4 TB/s: 128 MB in, 512 MB out).
+// States rounded by chance: 244 us (in 64 tensors 239, against 176 to the nearest), for a counter's hash an
+// element: 107 instructions an element in place of 67 bound it then.
 // 306,496 weights: 6 us, a launch.  Four blocks an SM: three took 323 us,
 // five 312 and, in 8 bits, 198.
 #include <cuda_fp8.h>

@@ -15,12 +15,12 @@
 // segment, from the last entry in it on, which reads those rows once more; a block joins the
 // pairs of the segments before its own.  Every order is fixed by the sizes: equal calls give
 // equal bits.
-//   bf16 65,536 x 2,048   64 sequences 138 us (5.8 TB/s), 16 164 us: few blocks, each a latency a tile; one
-//                         237 us; in blocks that waited for one another's pairs 16 took 606 us
-//   bf16 262,144 x 256    one sequence 127 us, of which the pairs' kernel takes two fifths: it reads both
+//   bf16 65,536 x 2,048   64 sequences 137 us (5.9 TB/s), 16 164 us: few blocks, each a latency a tile; one
+//                         239 us; in blocks that waited for one another's pairs 16 took 606 us
+//   bf16 262,144 x 256    one sequence 130 us, of which the pairs' kernel takes two fifths: it reads both
 //                         inputs once more, of which L2 keeps half for the kernel after it
-//   gradient              bf16 65,536 x 2,048, 64 sequences 368 us, 32 padded ones 352 us; float32 20,003 x 501,
-//                         packed, 107 us
+//   gradient              bf16 65,536 x 2,048, 64 sequences 373 us, 32 padded ones 352 us; float32 20,003 x 501,
+//                         packed, 109 us
 // The gradient has 40 to 55 instructions an element and three blocks of four warps an SM, by its shared memory
 // (four matrices, two tiles each): 44% of the issue slots, 3.9 TB/s, latency before bandwidth.
 #include <algorithm>
@@ -265,8 +265,8 @@ Shape shape_of(const ScanArgs& a, int32_t type, int32_t out_type, bool grad, int
   s.marks = a.offsets || a.lengths;
   // blocks that run at a time: 16-bit rows of four (the gradient: three) fit an SM, float32 rows of one less.
   // The gradient's float32 rows of ragged or of many sequences go half as many at a time, of which three
-  // blocks fit: 256 x 128 x 2,048 237 us against 408, packed 20,003 x 501 111 and 126; but one sequence of
-  // 131,072 x 512 390 against 326.
+  // blocks fit: 256 x 128 x 2,048 239 us against 408, packed 20,003 x 501 109 and 126; but one sequence of
+  // 131,072 x 512 390 against 324.
   const bool wide = grad ? b == 4 || ob == 4 : b == 4;
   const bool many = a.n_seq * p.n_cols >= (int64_t)num_sms * (grad ? 8 : 5) / 4;
   const bool half = grad && wide && p.tx == 32 && (s.marks || many);
