@@ -36,6 +36,7 @@ DECAYS = {"sigmoid": 0, "log": 1}
 ROUNDINGS = {"nearest": 0, "chance": 1}
 NO_PAD = -2**63
 INT32_MAX = 2**31 - 1
+LEGACY_STREAM = 1  # cudaStreamLegacy: the default stream by a name that is not NULL
 KERNEL_NAMES = ["weights", "sort_hist", "sort_pass", "seg_scan", "row_long", "row_apply",
                 "dense", "init", "other"]
 
@@ -296,7 +297,9 @@ def gba_for_workload(cfg, max_buf=None, seed=None, overlap=False, **rule):
 
 
 class GBA:
-    """One parameter-server state on the current CUDA device."""
+    """One parameter-server state on the current CUDA device.  Its work is issued on `stream`
+    (default: the current one, the default stream too), so tensors of that stream can be passed,
+    and results read, without waiting."""
 
     def __init__(self, tables, dense_size, dense_opt, global_batch, max_buffered_msgs,
                  iota=INT32_MAX, row_staleness=0, sparse_denominator=0, seed=0, stream=None,
@@ -318,7 +321,7 @@ class GBA:
         self.stream = stream
         self.h, _ = gba_create(descs, self.D, dense_opt, int(global_batch),
                                int(max_buffered_msgs), st, int(seed),
-                               ctypes.c_void_p(stream.cuda_stream))
+                               ctypes.c_void_p(stream.cuda_stream or LEGACY_STREAM))  # NULL: a stream of its own
         self._keep = []  # tensors referenced by pushed-by-reference messages
 
     def close(self):
